@@ -10,3 +10,6 @@ from .api import (GinexError, FeatureCache, SampleResult, ChangesetResult,  # no
                   changeset_resume, static_select,
                   library_path, version)
 from .pipeline import Executor, InspectorPipeline  # noqa: F401
+from .training import (Compressed, Route, activate, activate_backward, combine,  # noqa: F401
+                       combine_backward, compress, dispatch, dispatch_backward, restore, route,
+                       weight_gradient)

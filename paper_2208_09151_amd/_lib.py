@@ -1,4 +1,4 @@
-"""ctypes loader for libginex.so; declares every entry point of include/ginex.h."""
+"""ctypes loader for libginex.so; declares every entry point of include/ginex.h and ginex_train.h."""
 from __future__ import annotations
 
 import ctypes as C
@@ -18,6 +18,19 @@ class CsrDesc(C.Structure):
 class CacheDesc(C.Structure):
     _fields_ = [("rows", vp), ("cap", i64), ("row_bytes", i64), ("addr", vp),
                 ("num_nodes", i64), ("slow", vp)]
+
+
+class RowsDesc(C.Structure):
+    _fields_ = [("data", vp), ("rows", i64), ("width", i64), ("stride", i64), ("type", i32)]
+
+
+class RoutingDesc(C.Structure):
+    _fields_ = [("rows", i64), ("top", i32), ("experts", i32), ("offsets", vp), ("slot", vp),
+                ("source", vp)]
+
+
+class CodesDesc(C.Structure):
+    _fields_ = [("rows", i64), ("width", i64), ("codes", vp), ("scales", vp)]
 
 
 SIGNATURES = {
@@ -48,6 +61,22 @@ SIGNATURES = {
     "ginex_cache_count_misses": (i32, [C.POINTER(CacheDesc), vp, i64, vp, vp]),
 }
 
+_ROWS, _ROUTING, _CODES = C.POINTER(RowsDesc), C.POINTER(RoutingDesc), C.POINTER(CodesDesc)
+
+# include/ginex_train.h
+TRAIN_SIGNATURES = {
+    "ginex_route_workspace_bytes": (sz, [i64, i32, i32]),
+    "ginex_route": (i32, [vp, i32, i64, _ROUTING, vp, sz, vp]),
+    "ginex_dispatch": (i32, [_ROUTING, _ROWS, _ROWS, vp]),
+    "ginex_combine": (i32, [_ROUTING, _ROWS, vp, _ROWS, vp]),
+    "ginex_combine_backward": (i32, [_ROUTING, _ROWS, _ROWS, vp, _ROWS, vp, vp]),
+    "ginex_compress": (i32, [_ROWS, i32, _ROWS, _CODES, vp]),
+    "ginex_restore": (i32, [_CODES, _ROWS, vp]),
+    "ginex_activate_backward": (i32, [_CODES, i32, _ROWS, _ROWS, vp]),
+    "ginex_weight_gradient_workspace_bytes": (sz, [i64, i32, i64, i64]),
+    "ginex_weight_gradient": (i32, [_CODES, _ROUTING, _ROWS, vp, vp, sz, vp]),
+}
+
 _lib = None
 
 
@@ -59,13 +88,14 @@ def stale() -> bool:
     csrc = os.path.join(_PKG, "csrc")
     sources = [os.path.join(csrc, f) for f in os.listdir(csrc)
                if f.endswith((".hip", ".hpp", ".cpp"))]
-    sources.append(os.path.join(os.path.dirname(_PKG), "include", "ginex.h"))
+    include = os.path.join(os.path.dirname(_PKG), "include")
+    sources += [os.path.join(include, f) for f in ("ginex.h", "ginex_train.h")]
     return any(os.path.getmtime(s) > built for s in sources if os.path.exists(s))
 
 
 def load():
     """Loads the built library.  A library that is missing, or older than one of its sources
-    (csrc/*, include/ginex.h), is rebuilt first where the compiler is installed; where it is
+    (csrc/*, include/*), is rebuilt first where the compiler is installed; where it is
     not, a stale library is an error rather than a silent run of old kernels."""
     global _lib
     if _lib is None:
@@ -79,7 +109,7 @@ def load():
             else:
                 raise RuntimeError(f"{LIB_PATH} has not been built and {HIPCC} is not installed")
         lib = C.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in [*SIGNATURES.items(), *TRAIN_SIGNATURES.items()]:
             fn = getattr(lib, name)     # AttributeError if the library lacks a declared symbol
             fn.restype = res
             fn.argtypes = args

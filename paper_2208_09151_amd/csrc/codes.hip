@@ -1,0 +1,218 @@
+// Activations kept in 8 bits: compress (with the activation in the same pass), restore, and the
+// activation's gradient from the codes.
+//
+// Elementwise, bound by HBM.  A thread has one chunk of 16 bytes of the wide side and its 4 (f32) or 8
+// codes; 8 or 4 neighbouring lanes share a block of 32 channels and find its largest magnitude by
+// exchanging lanes.  Chunks are numbered through all rows, padded to whole blocks, so that no lane idles
+// for a width that is no power of two.
+#include "codes.hpp"
+
+namespace ginex {
+namespace {
+
+constexpr int THREADS = 256;
+
+template <int ACT>
+__device__ __forceinline__ float activated(float x) {
+  if (ACT == GINEX_ACT_RELU) return x < 0.f ? 0.f : x;
+  if (ACT == GINEX_ACT_SILU) return x / (1.f + expf(-x));
+  if (ACT == GINEX_ACT_GELU) return 0.5f * x * erfcf(x * -0.70710678118654752f);
+  return x;
+}
+
+// dy f'(x)
+template <int ACT>
+__device__ __forceinline__ float sloped(float x, float dy) {
+  if (ACT == GINEX_ACT_RELU) return x > 0.f ? dy : (x <= 0.f ? 0.f : x);
+  if (ACT == GINEX_ACT_SILU) {
+    const float sigma = 1.f / (1.f + expf(-x));
+    return dy * (sigma * (1.f + x * (1.f - sigma)));
+  }
+  const float below = 0.5f * erfcf(x * -0.70710678118654752f);
+  return dy * (below + x * expf(-0.5f * x * x) * 0.39894228040143268f);
+}
+
+// The codes of a chunk, as one word of N bytes.
+template <int N>
+struct Word;
+template <>
+struct Word<4> {
+  typedef uint32_t type;
+};
+template <>
+struct Word<8> {
+  typedef uint64_t type;
+};
+
+template <typename T, int ACT>
+__global__ __launch_bounds__(THREADS) void k_compress(RowsOf<const T> x, RowsOf<T> y, int8_t* __restrict__ codes,
+                                                      uint8_t* __restrict__ scales, int64_t first, uint32_t chunks,
+                                                      Divisor cpr, int32_t width) {
+  constexpr int N = Chunk<T>::N, LANES = GINEX_CODE_BLOCK / N;
+  const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
+  if (t >= chunks) return;            // (whole blocks: chunks is a multiple of LANES)
+  const uint32_t row = cpr.of(t);
+  const uint32_t at = t - row * cpr.d;
+  const int32_t c = (int32_t)at * N;
+  const int64_t r = first + row;
+  float v[N];
+  load_chunk(x.at(r, c), width - c, v);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t magnitude = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+    top = top > magnitude ? top : magnitude;
+  }
+#pragma unroll
+  for (int step = 1; step < LANES; step *= 2) {
+    const uint32_t other = __shfl_xor(top, step, WAVE);
+    top = top > other ? top : other;
+  }
+  const uint32_t scale = scale_byte(top);
+  const float by = to_codes(scale);
+  typename Word<N>::type word = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float q = scale == NO_NUMBER ? 0.f : rintf(v[i] * by);
+    const int32_t code = (int32_t)fminf(fmaxf(q, -127.f), 127.f);
+    word |= (typename Word<N>::type)(uint8_t)code << (8 * i);
+  }
+  const int64_t chunk = r * cpr.d + at;
+  reinterpret_cast<typename Word<N>::type*>(codes)[chunk] = word;
+  if (at % LANES == 0) scales[chunk / LANES] = (uint8_t)scale;
+  if (ACT != GINEX_ACT_NONE && c < width) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = activated<ACT>(v[i]);
+    store_chunk(y.at(r, c), width - c, v);
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void restored(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                         int64_t chunk, float (&v)[N]) {
+  typename Word<N>::type word = reinterpret_cast<const typename Word<N>::type*>(codes)[chunk];
+  const float step = code_step(scales[chunk / (GINEX_CODE_BLOCK / N)]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (float)(int8_t)(word >> (8 * i)) * step;
+}
+
+// ACT < 0: out = the restored values; else out = dy f'(restored).
+template <typename T, int ACT>
+__global__ __launch_bounds__(THREADS) void k_restore(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                     RowsOf<const T> dy, RowsOf<T> out, int64_t first, uint32_t chunks,
+                                                     Divisor cpr, int32_t width) {
+  constexpr int N = Chunk<T>::N;
+  const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
+  if (t >= chunks) return;
+  const uint32_t row = cpr.of(t);
+  const uint32_t at = t - row * cpr.d;
+  const int32_t c = (int32_t)at * N;
+  if (c >= width) return;
+  const int64_t r = first + row;
+  float v[N];
+  restored<N>(codes, scales, r * cpr.d + at, v);
+  if (ACT >= 0) {
+    float g[N];
+    load_chunk(dy.at(r, c), width - c, g);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = sloped<ACT>(v[i], g[i]);
+  }
+  store_chunk(out.at(r, c), width - c, v);
+}
+
+// Calls go(first row, chunks, chunks of a row) for the launches that cover `rows` rows, chunks numbered in 31 bits.
+template <typename T, typename Go>
+int32_t by_launches(int64_t rows, int64_t width, Go go) {
+  const int64_t cpr = code_blocks(width) * (GINEX_CODE_BLOCK / Chunk<T>::N);
+  const int64_t step = (((int64_t)1 << 31) - THREADS) / cpr;
+  for (int64_t r = 0; r < rows; r += step) {
+    go(r, (uint32_t)((rows - r < step ? rows - r : step) * cpr), Divisor((uint32_t)cpr));
+    GINEX_LAUNCH_CHECK();
+  }
+  return GINEX_OK;
+}
+
+int32_t check_activation(int32_t activation, int32_t least) {
+  if (activation < least || activation > GINEX_ACT_GELU) return fail(GINEX_ERR_ARG, "unknown activation %d", activation);
+  return GINEX_OK;
+}
+
+int32_t check_kept(const char* what, const ginex_rows_t* r, const ginex_codes_t* kept) {
+  if (r->rows != kept->rows || r->width != kept->width)
+    return fail(GINEX_ERR_ARG, "%s is %lld x %lld, the codes %lld x %lld", what, (long long)r->rows, (long long)r->width,
+                (long long)kept->rows, (long long)kept->width);
+  return GINEX_OK;
+}
+
+template <typename T>
+RowsOf<const T> read_rows(const ginex_rows_t* r) {
+  return {static_cast<const T*>(r->data), r->stride};
+}
+
+}  // namespace
+}  // namespace ginex
+
+using namespace ginex;
+
+extern "C" int32_t ginex_compress(const ginex_rows_t* x, int32_t activation, const ginex_rows_t* y,
+                                  const ginex_codes_t* kept, void* stream) {
+  if (int32_t rc = check_rows("x", x, false)) return rc;
+  if (int32_t rc = check_codes(kept)) return rc;
+  if (int32_t rc = check_kept("x", x, kept)) return rc;
+  if (int32_t rc = check_activation(activation, GINEX_ACT_NONE)) return rc;
+  if ((activation != GINEX_ACT_NONE) != (y != nullptr)) return fail(GINEX_ERR_ARG, "y goes with an activation, and only with one");
+  if (y) {
+    if (int32_t rc = check_rows("y", y, true)) return rc;
+    if (int32_t rc = check_same("x", x, "y", y)) return rc;
+    if (int32_t rc = check_kept("y", y, kept)) return rc;
+  }
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return with_type(x->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    const RowsOf<T> to = y ? rows_of<T>(y) : RowsOf<T>{nullptr, 0};
+    const auto kernel = activation == GINEX_ACT_NONE   ? k_compress<T, GINEX_ACT_NONE>
+                        : activation == GINEX_ACT_RELU ? k_compress<T, GINEX_ACT_RELU>
+                        : activation == GINEX_ACT_SILU ? k_compress<T, GINEX_ACT_SILU>
+                                                       : k_compress<T, GINEX_ACT_GELU>;
+    return by_launches<T>(x->rows, x->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, read_rows<T>(x), to,
+                         kept->codes, kept->scales, r, chunks, cpr, (int32_t)x->width);
+    });
+  });
+}
+
+extern "C" int32_t ginex_restore(const ginex_codes_t* kept, const ginex_rows_t* out, void* stream) {
+  if (int32_t rc = check_codes(kept)) return rc;
+  if (int32_t rc = check_rows("out", out, true)) return rc;
+  if (int32_t rc = check_kept("out", out, kept)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return with_type(out->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    return by_launches<T>(out->rows, out->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
+      hipLaunchKernelGGL((k_restore<T, -1>), dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes,
+                         kept->scales, RowsOf<const T>{nullptr, 0}, rows_of<T>(out), r, chunks, cpr, (int32_t)out->width);
+    });
+  });
+}
+
+extern "C" int32_t ginex_activate_backward(const ginex_codes_t* kept, int32_t activation, const ginex_rows_t* dy,
+                                           const ginex_rows_t* dx, void* stream) {
+  if (int32_t rc = check_codes(kept)) return rc;
+  if (int32_t rc = check_activation(activation, GINEX_ACT_RELU)) return rc;
+  if (int32_t rc = check_rows("dy", dy, false)) return rc;
+  if (int32_t rc = check_rows("dx", dx, true)) return rc;
+  if (int32_t rc = check_same("dy", dy, "dx", dx)) return rc;
+  if (int32_t rc = check_kept("dy", dy, kept)) return rc;
+  if (int32_t rc = check_kept("dx", dx, kept)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return with_type(dy->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    const auto kernel = activation == GINEX_ACT_RELU   ? k_restore<T, GINEX_ACT_RELU>
+                        : activation == GINEX_ACT_SILU ? k_restore<T, GINEX_ACT_SILU>
+                                                       : k_restore<T, GINEX_ACT_GELU>;
+    return by_launches<T>(dy->rows, dy->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes, kept->scales,
+                         read_rows<T>(dy), rows_of<T>(dx), r, chunks, cpr, (int32_t)dx->width);
+    });
+  });
+}

@@ -1,0 +1,266 @@
+"""Python names for include/ginex_train.h, the operators of the training step on gathered rows: rows
+sorted by expert and back, activations kept in 8 bits, and their use in the backward pass.
+
+Tensors in, tensors out, nothing computed here.  Rows are f32, bf16 or f16 tensors of two dimensions whose
+last one is dense; any stride from row to row will do.  Every call enqueues on the current stream and
+returns at once.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass, field
+
+import torch
+
+from . import _lib
+from ._lib import CodesDesc, RoutingDesc, RowsDesc
+from .api import GinexError, _check, _workspace
+
+CODE_BLOCK = 32                 # channels that share a scale
+ACTIVATIONS = {"relu": 1, "silu": 2, "gelu": 3}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _here(t, what, dtype=None):
+    """A tensor in the memory of the current GPU."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what}: expected a tensor in GPU memory")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on {t.device}, which is not the current GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    return t
+
+
+def _dense(t, what, shape, dtype):
+    _here(t, what, dtype)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what}: expected shape {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor")
+    return t
+
+
+def _rows(t, what):
+    """The descriptor of a matrix of rows."""
+    _here(t, what)
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what}: expected float32, bfloat16 or float16, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: expected two dimensions, got {t.dim()}")
+    n, width = t.shape
+    stride, step = t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"{what}: the elements of a row must be dense")
+    if n <= 1:
+        stride = width          # (a single row may have any)
+    return RowsDesc(t.data_ptr(), n, width, stride, kind)
+
+
+def _out(out, what, shape, dtype, device):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _here(out, what, dtype)
+    if tuple(out.shape) != shape:
+        raise ValueError(f"{what}: expected shape {shape}, got {tuple(out.shape)}")
+    return out
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {name!r}: one of {sorted(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
+
+
+@dataclass(frozen=True)
+class Route:
+    """Where the rows go: pair (r, j) is in slot ``slot[r, j]`` or in none (-1), the slots of expert e are
+    ``offsets[e]`` .. ``offsets[e + 1] - 1``, and slot s holds row ``source[s]`` (-1 behind the last one)."""
+    offsets: torch.Tensor       # int64 [experts + 1]
+    slot: torch.Tensor          # int32 [rows, top]
+    source: torch.Tensor        # int32 [rows * top]
+    _desc: RoutingDesc = field(init=False, repr=False, compare=False)
+
+    def __post_init__(self):
+        _here(self.slot, "slot", torch.int32)
+        if self.slot.dim() != 2 or self.offsets.dim() != 1 or self.offsets.numel() < 2:
+            raise ValueError("expected offsets [experts + 1] and slot [rows, top]")
+        rows, top = self.slot.shape
+        _dense(self.offsets, "offsets", (self.offsets.numel(),), torch.int64)
+        _dense(self.slot, "slot", (rows, top), torch.int32)
+        _dense(self.source, "source", (rows * top,), torch.int32)
+        object.__setattr__(self, "_desc", RoutingDesc(rows, top, self.experts, self.offsets.data_ptr(),
+                                                      self.slot.data_ptr(), self.source.data_ptr()))
+
+    @property
+    def rows(self) -> int:
+        return self.slot.shape[0]
+
+    @property
+    def top(self) -> int:
+        return self.slot.shape[1]
+
+    @property
+    def experts(self) -> int:
+        return self.offsets.numel() - 1
+
+
+def route(chosen, experts, capacity=None, workspace=None) -> Route:
+    """ginex_route: sorts the pairs (row, choice) of ``chosen`` [rows, top] (int32 or int64) by expert.  A
+    value outside 0 .. experts - 1 means no expert; an expert gets ``capacity`` slots at most."""
+    lib = _lib.load()
+    _here(chosen, "chosen")
+    if chosen.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"chosen: expected int32 or int64, got {chosen.dtype}")
+    if chosen.dim() != 2 or not chosen.is_contiguous():
+        raise ValueError("chosen: expected a contiguous tensor [rows, top]")
+    if capacity is not None and capacity < 0:
+        raise ValueError(f"capacity={capacity}")
+    rows, top = chosen.shape
+    need = lib.ginex_route_workspace_bytes(rows, top, experts)
+    if need == 0:
+        raise GinexError(-1, lib.ginex_last_error().decode())
+    dev = chosen.device
+    ws = workspace if workspace is not None and workspace.numel() >= need else _workspace(need, dev)
+    made = Route(torch.empty(experts + 1, dtype=torch.int64, device=dev),
+                 torch.empty((rows, top), dtype=torch.int32, device=dev),
+                 torch.empty(rows * top, dtype=torch.int32, device=dev))
+    _check(lib.ginex_route(chosen.data_ptr(), int(chosen.dtype == torch.int64),
+                           -1 if capacity is None else min(capacity, (1 << 31) - 1), C.byref(made._desc),
+                           ws.data_ptr(), ws.numel(), _stream()))
+    return made
+
+
+def dispatch(x, route: Route, out=None):
+    """ginex_dispatch: the rows of ``x`` in their slots, [rows * top, width]; slots without a row are 0."""
+    desc = _rows(x, "x")
+    out = _out(out, "out", (route.source.numel(), x.shape[1]), x.dtype, x.device)
+    _check(_lib.load().ginex_dispatch(C.byref(route._desc), C.byref(desc), C.byref(_rows(out, "out")),
+                                      _stream()))
+    return out
+
+
+def _combine(z, route, weights, out):
+    desc = _rows(z, "z")
+    out = _out(out, "out", (route.rows, z.shape[1]), z.dtype, z.device)
+    _check(_lib.load().ginex_combine(C.byref(route._desc), C.byref(desc),
+                                     None if weights is None else weights.data_ptr(),
+                                     C.byref(_rows(out, "out")), _stream()))
+    return out
+
+
+def combine(z, route: Route, weights, out=None):
+    """ginex_combine: y[r] = sum_j weights[r, j] z[slot[r, j]]; ``weights`` f32 [rows, top]."""
+    _dense(weights, "weights", (route.rows, route.top), torch.float32)
+    return _combine(z, route, weights, out)
+
+
+def dispatch_backward(grad, route: Route, out=None):
+    """The gradient of dispatch: the sum of a row's slots."""
+    return _combine(grad, route, None, out)
+
+
+def combine_backward(grad, z, route: Route, weights):
+    """ginex_combine_backward: the gradients of ``z`` and of ``weights``."""
+    _dense(weights, "weights", (route.rows, route.top), torch.float32)
+    desc, zdesc = _rows(grad, "grad"), _rows(z, "z")
+    dz = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    dweights = torch.empty(weights.shape, dtype=torch.float32, device=z.device)
+    _check(_lib.load().ginex_combine_backward(C.byref(route._desc), C.byref(desc), C.byref(zdesc),
+                                              weights.data_ptr(), C.byref(_rows(dz, "dz")),
+                                              dweights.data_ptr(), _stream()))
+    return dz, dweights
+
+
+@dataclass(frozen=True)
+class Compressed:
+    """Rows in 8 bits: blocks of 32 channels share a power of two, code q of a block with scale byte b
+    stands for q * 2^(b - 133), b = 255 for NaN."""
+    codes: torch.Tensor         # int8 [rows, 32 * blocks]
+    scales: torch.Tensor        # uint8 [rows, blocks]
+    width: int
+    _desc: CodesDesc = field(init=False, repr=False, compare=False)
+
+    def __post_init__(self):
+        _here(self.codes, "codes", torch.int8)
+        if self.codes.dim() != 2:
+            raise ValueError("codes: expected two dimensions")
+        rows, blocks = self.codes.shape[0], -(-self.width // CODE_BLOCK)
+        _dense(self.codes, "codes", (rows, blocks * CODE_BLOCK), torch.int8)
+        _dense(self.scales, "scales", (rows, blocks), torch.uint8)
+        object.__setattr__(self, "_desc", CodesDesc(rows, self.width, self.codes.data_ptr(),
+                                                    self.scales.data_ptr()))
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+
+def _compress(x, activation, y):
+    desc = _rows(x, "x")
+    n, width = x.shape
+    blocks = -(-width // CODE_BLOCK)
+    kept = Compressed(torch.empty((n, blocks * CODE_BLOCK), dtype=torch.int8, device=x.device),
+                      torch.empty((n, blocks), dtype=torch.uint8, device=x.device), width)
+    _check(_lib.load().ginex_compress(C.byref(desc), activation,
+                                      None if y is None else C.byref(_rows(y, "out")),
+                                      C.byref(kept._desc), _stream()))
+    return kept
+
+
+def compress(x) -> Compressed:
+    """ginex_compress: ``x`` kept in 8.25 bits a value."""
+    return _compress(x, 0, None)
+
+
+def activate(x, activation, out=None):
+    """ginex_compress with an activation ("relu", "silu", "gelu"): its values, and ``x`` compressed for the
+    backward pass.  ``out`` may be ``x``."""
+    kind = _activation(activation)
+    _rows(x, "x")
+    out = _out(out, "out", tuple(x.shape), x.dtype, x.device)
+    return out, _compress(x, kind, out)
+
+
+def restore(kept: Compressed, dtype=torch.float32, out=None):
+    """ginex_restore: the values that the codes stand for."""
+    out = _out(out, "out", (kept.rows, kept.width), dtype, kept.codes.device)
+    _check(_lib.load().ginex_restore(C.byref(kept._desc), C.byref(_rows(out, "out")), _stream()))
+    return out
+
+
+def activate_backward(kept: Compressed, grad, activation, out=None):
+    """ginex_activate_backward: ``grad`` times the activation's derivative at the kept values.  ``out`` may
+    be ``grad``."""
+    kind = _activation(activation)
+    desc = _rows(grad, "grad")
+    out = _out(out, "out", tuple(grad.shape), grad.dtype, grad.device)
+    _check(_lib.load().ginex_activate_backward(C.byref(kept._desc), kind, C.byref(desc),
+                                               C.byref(_rows(out, "out")), _stream()))
+    return out
+
+
+def weight_gradient(kept: Compressed, grad, route: Route = None, out=None, workspace=None):
+    """ginex_weight_gradient: per expert the sum over its slots of (kept row)^T (row of ``grad``), f32
+    [experts, width, grad width]; without a route one layer's, [width, grad width]."""
+    lib = _lib.load()
+    desc = _rows(grad, "grad")
+    shape = (kept.width, grad.shape[1])
+    if route is not None:
+        shape = (route.experts, *shape)
+    out = _dense(out, "out", shape, torch.float32) if out is not None \
+        else torch.empty(shape, dtype=torch.float32, device=grad.device)
+    need = lib.ginex_weight_gradient_workspace_bytes(grad.shape[0], shape[0] if route is not None else 1,
+                                                     kept.width, grad.shape[1])
+    if need == 0:
+        raise GinexError(-1, lib.ginex_last_error().decode())
+    ws = workspace if workspace is not None and workspace.numel() >= need \
+        else _workspace(need, grad.device)
+    _check(lib.ginex_weight_gradient(C.byref(kept._desc), None if route is None else C.byref(route._desc),
+                                     C.byref(desc), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
+    return out

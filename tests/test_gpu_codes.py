@@ -1,0 +1,387 @@
+"""Activations kept in 8 bits and their use in the backward pass, against a plain implementation in 64 bits.
+
+Codes and restored values are exact.  Tolerances of the rest, per element, beside half a unit of the
+output's type:
+  exp is good to 2 units, so silu to 8 2^-23; erfc is good to 16 units, and its rounded argument x/sqrt(2)
+  moves it by 2 (x^2/2) 2^-23: gelu to (2^-18 + x^2 2^-22) of its value;
+  slopes are sums with terms up to 1 + |x|: off by 2^-19 (1 + |x|);
+  a sum of n products in f32 is off by at most n 2^-24 sum |terms|, in any order.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+LEAST = {torch.float32: 2.0 ** -126, torch.bfloat16: 2.0 ** -126, torch.float16: 2.0 ** -24}
+SHAPES = [(0, 64), (1, 1), (1, 256), (3, 31), (5, 32), (7, 33), (100, 64), (65, 333), (1000, 100), (33, 1025)]
+
+
+@pytest.fixture(scope="module")
+def g():
+    import paper_2208_09151_amd as lib
+    return lib
+
+
+def plain_codes(x):
+    """Codes, scales and values from the definition, in 64 bits."""
+    n, width = x.shape
+    blocks = -(-width // 32)
+    v = torch.zeros((n, blocks * 32), dtype=torch.float64)
+    v[:, :width] = x.double()
+    v = v.view(n, blocks, 32)
+    bad = ~torch.isfinite(v).all(2)
+    v = torch.where(bad[:, :, None], torch.zeros_like(v), v)
+    e = (torch.frexp(v.abs().amax(2))[1] - 1).double()
+    e[(v == 0).all(2)] = -120
+    e = e.clamp(min=-120)
+    q = torch.round(v * torch.exp2(6 - e)[:, :, None]).clamp(-127, 127)
+    q[bad] = 0
+    values = q * torch.exp2(e - 6)[:, :, None]
+    values[bad] = float("nan")
+    scales = torch.where(bad, torch.full_like(e, 255), e + 127)
+    return q.view(n, blocks * 32).to(torch.int8), scales.to(torch.uint8), values.view(n, blocks * 32)[:, :width]
+
+
+def f(x, activation):
+    if activation == "relu":
+        return torch.where(x < 0, torch.zeros_like(x), x)
+    if activation == "silu":
+        return x * torch.sigmoid(x)
+    return x * 0.5 * torch.special.erfc(-x * math.sqrt(0.5))
+
+
+def slope(x, activation):
+    if activation == "relu":
+        return (x > 0).double()
+    if activation == "silu":
+        return torch.sigmoid(x) * (1 + x * torch.sigmoid(-x))
+    return 0.5 * torch.special.erfc(-x * math.sqrt(0.5)) + x * torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+
+
+def some(shape, dtype, seed=0, by=1.0):
+    t = torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+    return (t * by).to(dtype)
+
+
+def strided(t, pad, shift):
+    rows, width = t.shape
+    base = torch.full((rows * (width + pad) + shift,), float("nan"), dtype=t.dtype, device="cuda")
+    view = base[shift:].view(rows, width + pad)[:, :width]
+    view.copy_(t)
+    return view
+
+
+def same_bits(a, b):
+    return torch.equal(a.cpu().view(torch.uint8), b.cpu().contiguous().view(torch.uint8))
+
+
+def near(got, want, slack, dtype):
+    got = got.cpu().double()
+    allowed = slack + UNIT[dtype] * (want.abs() + slack) + LEAST[dtype]
+    bad = ~((got - want).abs() <= allowed)
+    assert not bad.any(), (int(bad.sum()), float((got - want).abs().max()))
+
+
+def check_codes(kept, x):
+    q, scales, _ = plain_codes(x)
+    assert torch.equal(kept.codes.cpu(), q) and torch.equal(kept.scales.cpu(), scales)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, width", SHAPES)
+@pytest.mark.parametrize("pad, shift", [(0, 0), (3, 1)])
+def test_codes_and_values(g, rows, width, dtype, pad, shift):
+    x = some((rows, width), dtype, rows + width)
+    x[::3] *= 1000
+    x[1::5] = 0
+    kept = g.compress(strided(x, pad, shift))
+    check_codes(kept, x)
+    assert torch.equal(g.restore(kept, dtype).cpu(), plain_codes(x)[2].to(dtype))
+    out = torch.full((rows, width + 9), 7.0, dtype=dtype, device="cuda")
+    g.restore(kept, dtype, out=out[:, 4:4 + width])
+    assert torch.equal(out[:, 4:4 + width].cpu(), plain_codes(x)[2].to(dtype))
+    assert (out[:, :4] == 7).all() and (out[:, 4 + width:] == 7).all()
+
+
+def test_ties_and_ends_of_the_range(g):
+    """Halves go to even, the largest magnitude of a block is cut to 127 steps, blocks below 2^-120 have
+    steps of 2^-126, subnormal numbers count."""
+    rows = []
+    base = torch.zeros(32, dtype=torch.float64)
+    base[0] = 1.0
+    base[1:] = (torch.arange(31) - 15 + 0.5) / 64                       # halves of a step
+    rows.append(base)
+    base = base.clone()
+    base[0] = 1.999                                                     # 127.9 steps
+    base[2] = -1.9999999
+    rows.append(base)
+    for top in (2.0 ** -120, 2.0 ** -121, 2.0 ** -126, 2.0 ** -130, 2.0 ** -149, 3.4e38, 2.0 ** 127):
+        rows.append(top * torch.linspace(-1, 1, 32, dtype=torch.float64))
+    x = torch.stack(rows).float()
+    kept = g.compress(x.cuda())
+    check_codes(kept, x)
+    assert torch.equal(g.restore(kept).cpu(), plain_codes(x)[2].float())
+    assert torch.equal(g.restore(kept, torch.bfloat16).cpu().double(), plain_codes(x)[2])       # exact
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_blocks_with_no_numbers(g, dtype):
+    x = some((6, 100), dtype, 4)
+    x[0, 5] = float("inf")
+    x[1, 40] = float("-inf")
+    x[2, 99] = float("nan")
+    x[3] = float("nan")
+    kept = g.compress(x.cuda())
+    check_codes(kept, x)
+    got, want = g.restore(kept, dtype).cpu(), plain_codes(x)[2].to(dtype)
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num())
+    dy = torch.ones((6, 100), dtype=dtype, device="cuda")
+    for a in ("relu", "silu", "gelu"):
+        assert torch.equal(g.activate_backward(kept, dy, a).cpu().isnan(), want.isnan())
+
+
+@pytest.mark.parametrize("activation", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, width", SHAPES)
+@pytest.mark.parametrize("pad, shift", [(0, 0), (3, 1)])
+def test_activation_and_its_gradient(g, rows, width, dtype, activation, pad, shift):
+    x = some((rows, width), dtype, 7 * rows + width, 3.0)
+    dy = some((rows, width), dtype, 1)
+    xs = strided(x, pad, shift)
+    y, kept = g.activate(xs, activation)
+    check_codes(kept, x)
+    want = f(x.double(), activation)
+    near(y, want, want.abs() * (2.0 ** -18 + x.double() ** 2 * 2.0 ** -22), dtype)
+    restored = plain_codes(x)[2]
+    want = dy.double() * slope(restored, activation)
+    slack = dy.double().abs() * 2.0 ** -19 * (1 + restored.abs())
+    dys = strided(dy, pad, shift)
+    dx = g.activate_backward(kept, dys, activation)
+    near(dx, want, slack, dtype)
+    # in place: the same bits
+    assert same_bits(g.activate_backward(kept, dys, activation, out=dys), dx)
+    y2, kept2 = g.activate(xs, activation, out=xs)
+    assert same_bits(y2, y) and torch.equal(kept2.codes, kept.codes) and torch.equal(kept2.scales, kept.scales)
+
+
+@pytest.mark.parametrize("activation", ["relu", "silu", "gelu"])
+def test_activation_at_the_ends(g, activation):
+    x = torch.tensor([[0.0, -0.0, 1e-30, -1e-30, 20, -20, 88, -88, 100, -100, 1e30, -1e30, 3e38, -3e38,
+                       float("inf"), float("nan")]])
+    y, kept = g.activate(x.cuda(), activation)
+    y = y.cpu().double()[0]
+    xd = x.double()[0]
+    want = f(xd, activation)
+    assert y[15].isnan() and y[14] == math.inf
+    slack = want.abs() * (2.0 ** -18 + xd.clamp(-40, 40) ** 2 * 2.0 ** -22) + 2.0 ** -120
+    assert ((y - want).abs()[:14] <= slack[:14]).all()
+    kept = g.compress(x[:, :14].cuda())
+    dx = g.activate_backward(kept, torch.ones((1, 14), device="cuda"), activation).cpu().double()[0]
+    restored = plain_codes(x[:, :14])[2][0]
+    assert ((dx - slope(restored, activation)).abs() <= 2.0 ** -19 * (1 + restored.abs().clamp(max=100))).all()
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+def test_slope_against_differences(g, activation):
+    """At kept values, steps of 2^-7: the third derivative (below 1) makes h^2/6 = 1.1e-5, and rounding
+    y to f32 2^-24 |y| / h = 7.7e-6 |x|, erfc's error 2^-18 |y| / h = 5e-4 |y|."""
+    kept = g.compress(some((50, 64), torch.float32, 2, 2.0).cuda())
+    x = g.restore(kept)
+    h = 2.0 ** -7
+    up, down = g.activate(x + h, activation)[0], g.activate(x - h, activation)[0]
+    quotient = (up.double() - down.double()) / (2 * h)
+    dx = g.activate_backward(kept, torch.ones_like(x), activation)
+    assert ((quotient - dx.double()).abs() <= 2e-5 + 6e-4 * x.abs().double()).all()
+
+
+def test_refusals(g):
+    x = torch.zeros((4, 64), device="cuda")
+    kept = g.compress(x)
+    with pytest.raises(ValueError):
+        g.compress(x.double())
+    with pytest.raises(ValueError):
+        g.compress(x.int())
+    with pytest.raises(ValueError):
+        g.compress(x.t())
+    with pytest.raises(ValueError):
+        g.activate(x, "tanh")
+    with pytest.raises(ValueError):
+        g.activate(x, "relu", out=torch.zeros((4, 63), device="cuda"))
+    with pytest.raises(g.GinexError):
+        g.compress(torch.zeros((4, 0), device="cuda"))
+    with pytest.raises(g.GinexError):
+        g.activate_backward(kept, torch.zeros((5, 64), device="cuda"), "relu")
+    with pytest.raises(g.GinexError):
+        g.activate_backward(kept, torch.zeros((4, 65), device="cuda"), "relu")
+    with pytest.raises(ValueError):
+        g.restore(kept, torch.float64)
+    with pytest.raises(ValueError):
+        g.Compressed(kept.codes, kept.scales, 65)
+    with pytest.raises(ValueError):
+        g.Compressed(kept.codes, kept.scales[:3], 64)
+    with pytest.raises(g.GinexError):
+        g.weight_gradient(kept, torch.zeros((5, 8), device="cuda"))
+    with pytest.raises(ValueError):
+        g.weight_gradient(kept, torch.zeros((4, 8), device="cuda"), out=torch.zeros((64, 9), device="cuda"))
+    r = g.route(torch.zeros((4, 2), dtype=torch.int64, device="cuda"), 2)
+    with pytest.raises(g.GinexError):
+        g.weight_gradient(kept, torch.zeros((4, 8), device="cuda"), r)
+
+
+# ---- weight gradients --------------------------------------------------------------------------------
+
+def routed(g, rows, top, experts, seed, absent=0.1, capacity=None):
+    gen = torch.Generator().manual_seed(seed)
+    c = torch.randint(0, experts, (rows, top), generator=gen)
+    c = torch.minimum(c, torch.randint(0, experts, (rows, top), generator=gen))
+    c[torch.rand((rows, top), generator=gen) < absent] = -1
+    return g.route(c.cuda(), experts, capacity=capacity)
+
+
+def plain_weights(values, dy, offsets, source):
+    out = []
+    for a, b in zip(offsets[:-1], offsets[1:]):
+        x = values[source[a:b].long()]
+        out.append((x.t() @ dy[a:b].double(), x.abs().t() @ dy[a:b].double().abs(), b - a))
+    return out
+
+
+def check_weights(got, want):
+    for mine, (dw, size, n) in zip(got.cpu().double(), want):
+        bad = ~((mine - dw).abs() <= (n + 1) * 2.0 ** -24 * size + 2.0 ** -126)
+        assert not bad.any(), (int(bad.sum()), float((mine - dw).abs().max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, top, experts, width, out", [
+    (1, 1, 1, 1, 1), (1, 2, 8, 256, 256), (2, 1, 3, 33, 17), (40, 2, 5, 64, 64), (129, 3, 4, 100, 250),
+    (700, 2, 7, 65, 129), (3000, 1, 1, 128, 256), (2500, 4, 40, 257, 31), (1500, 2, 1024, 32, 48),
+    (9000, 2, 3, 96, 160)])
+@pytest.mark.parametrize("pad, shift", [(0, 0), (3, 1)])
+def test_weight_gradient(g, rows, top, experts, width, out, dtype, pad, shift):
+    r = routed(g, rows, top, experts, rows, capacity=max(1, rows * top * 2 // experts))
+    x = some((rows, width), torch.float32, 5)
+    kept = g.compress(x.cuda())
+    dy = some((rows * top, out), dtype, 6)
+    offsets = r.offsets.tolist()
+    dy[offsets[-1]:] = float("nan")             # slots without a row are not read
+    got = g.weight_gradient(kept, strided(dy, pad, shift), r)
+    check_weights(got, plain_weights(plain_codes(x)[2], dy, offsets, r.source.cpu()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [0, 1, 31, 64, 1000, 4097])
+def test_weight_gradient_of_one_layer(g, rows, dtype):
+    x, dy = some((rows, 72), torch.float32, 5), some((rows, 40), dtype, 6)
+    got = g.weight_gradient(g.compress(x.cuda()), dy.cuda())
+    assert got.shape == (72, 40)
+    check_weights(got[None], plain_weights(plain_codes(x)[2], dy, [0, rows], torch.arange(rows)))
+
+
+@pytest.mark.parametrize("absent", [0.0, 1.0])
+def test_weight_gradient_of_experts_without_rows(g, absent):
+    rows = 600
+    c = torch.full((rows, 1), 2)
+    if absent:
+        c[:] = -1
+    r = g.route(c.cuda(), 5)
+    x, dy = some((rows, 40), torch.float32, 5), some((rows, 24), torch.float32, 6)
+    out = torch.full((5, 40, 24), float("nan"), device="cuda")
+    got = g.weight_gradient(g.compress(x.cuda()), dy.cuda(), r, out=out)
+    assert (got[[0, 1, 3, 4]] == 0).all()
+    check_weights(got, plain_weights(plain_codes(x)[2], dy, r.offsets.tolist(), r.source.cpu()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weight_gradient_with_values_that_are_no_numbers(g, dtype):
+    """A NaN block spoils its 32 channels, an infinite gradient its column, of their expert alone; large
+    and small f32 gradients are whole."""
+    rows = 300
+    r = g.route((torch.arange(rows) % 3).view(-1, 1).cuda(), 3)
+    x = some((rows, 64), torch.float32, 5)
+    x[3, 40] = float("nan")                     # row 3: expert 0
+    dy = some((rows, 16), dtype, 6)
+    at = int(r.slot[4, 0])                      # row 4: expert 1
+    dy[at, 2] = float("inf")
+    x[4, 9] = 1.0
+    got = g.weight_gradient(g.compress(x.cuda()), dy.cuda(), r).cpu()
+    assert got[0, 32:].isnan().all() and not got[0, :32].isnan().any()
+    assert not got[1, :, [0, 1] + list(range(3, 16))].isnan().any() and got[1, 9, 2] == math.inf
+    assert not torch.isfinite(got[1, :, 2]).all() and torch.isfinite(got[2]).all()
+
+
+def test_weight_gradient_of_large_and_small_numbers(g):
+    x = torch.ones((64, 32))
+    dy = torch.zeros((64, 8))
+    dy[:, 0] = 3.0e38 / 64
+    dy[:, 1] = 1.2345678e-30
+    dy[:, 2] = 1 + 2.0 ** -23
+    dy[:, 3] = -(1 - 2.0 ** -24)
+    got = g.weight_gradient(g.compress(x.cuda()), dy.cuda()).cpu().double()
+    want = dy.double().sum(0)[None].expand(32, 8)
+    assert ((got - want).abs() <= 64 * 2.0 ** -24 * want.abs()).all()
+
+
+def test_weight_gradient_against_differences(g):
+    """<dy, x W> is linear in W: differences of it over steps of 1 are off by 1e-4 of their terms at most
+    (sums of 500 * 30 products in f32 on one side, f64 on the other)."""
+    rows = 500
+    kept = g.compress(some((rows, 30), torch.float32, 8).cuda())
+    x = g.restore(kept).double()
+    dy = some((rows, 20), torch.float32, 9).cuda()
+    way, W = some((30, 20), torch.float32, 10).cuda().double(), some((30, 20), torch.float32, 11).cuda().double()
+    loss = lambda w: float((dy.double() * (x @ w)).sum())
+    dw = g.weight_gradient(kept, dy).double()
+    terms = float((dy.double().abs() * (x.abs() @ way.abs())).sum())
+    assert abs((loss(W + way) - loss(W - way)) / 2 - float((dw * way).sum())) <= 1e-4 * terms
+
+
+def test_equal_bits_on_other_streams_and_in_a_graph(g):
+    r = routed(g, 9000, 2, 6, 1)
+    x = some((9000, 128), torch.float32, 5).cuda()
+    dy = some((18_000, 96), torch.float32, 6).cuda()
+
+    def step():
+        y, kept = g.activate(x, "silu")
+        return (y, kept.codes, kept.scales, g.restore(kept), g.activate_backward(kept, x, "silu"),
+                g.weight_gradient(kept, dy, r))
+
+    first = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        made = step()
+    for seed in range(3):
+        dy.copy_(some((18_000, 96), torch.float32, 20 + seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(step(), made))
+
+
+def test_codes_beyond_2_to_the_31_chunks(g):
+    """8.4 M rows of 1024 f32 are more chunks of 16 bytes than 31 bits number: the call takes two launches."""
+    n, width = 8_400_000, 1024
+    x = torch.zeros((n, width), dtype=torch.float32, device="cuda")
+    at = torch.tensor([0, 1, 4_000_000, 8_388_606, 8_388_607, 8_388_608, n - 1], device="cuda")
+    x[at] = some((len(at), width), torch.float32, 3).cuda()
+    kept = g.compress(x)
+    check_codes(g.Compressed(kept.codes[at], kept.scales[at], width), x[at].cpu())
+    del x
+    dy = torch.ones((1, width), dtype=torch.float16, device="cuda").expand(n, width)
+    dx = g.activate_backward(kept, dy, "relu")
+    restored = g.restore(g.Compressed(kept.codes[at], kept.scales[at], width))
+    assert torch.equal(dx[at], (restored > 0).half())
+    assert int(dx[-1000:-1].sum()) == 0
+    # one layer's weight gradient from the same codes: all rows but these are zero
+    dw = g.weight_gradient(kept, dy[:, :64])
+    check_weights(dw[None], [(restored.cpu().double().sum(0)[:, None].expand(width, 64),
+                              restored.cpu().double().abs().sum(0)[:, None].expand(width, 64), len(at))])
