@@ -11,9 +11,23 @@
 namespace ginex {
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int TILE = 64;          // channels and outputs of a workgroup
-constexpr int DEPTH = 16;         // slots in LDS at a time
+constexpr int JOIN_THREADS = 256;
+constexpr int WAVE_TILE = 64;     // channels and outputs of a wave: 2 x 2 tiles of a matrix instruction
+constexpr int DEPTH = 32;         // slots in LDS at a time
+constexpr int PAD = 32;           // elements behind a row in LDS, see product()
+
+typedef short half_words __attribute__((ext_vector_type(4)));
+typedef bf16 fragment __attribute__((ext_vector_type(8)));
+typedef float tile __attribute__((ext_vector_type(16)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+
+// A gradient as a sum of bf16 numbers, exactly: the significand's bits eight at a time (bf16 has 8, f16 11, f32 24).
+template <typename T>
+constexpr int TERMS = 1;
+template <>
+constexpr int TERMS<f16> = 2;
+template <>
+constexpr int TERMS<float> = 3;
 
 // The pieces of all experts: ceil(slots of the expert / length) each, numbered in order.
 struct Piece {
@@ -37,6 +51,7 @@ __device__ __forceinline__ void slots_of(const int64_t* __restrict__ offsets, in
   end = end < begin ? begin : (end < slots ? end : slots);
 }
 
+template <int THREADS>
 __device__ __forceinline__ Piece find_piece(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
                                             int64_t length, int64_t wanted, int64_t most_parts, Piece* found,
                                             uint32_t* smem) {
@@ -64,83 +79,267 @@ __device__ __forceinline__ Piece find_piece(const int64_t* __restrict__ offsets,
   return *found;
 }
 
+// Waits for this wave's LDS accesses and for the other waves, not for loads from HBM that are under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The upper halves of two f32: two bf16 in a word.
+__device__ __forceinline__ uint32_t upper_halves(float first, float second) {
+  return __builtin_amdgcn_perm(__float_as_uint(second), __float_as_uint(first), 0x07060302u);
+}
+
+// Eight elements of a gradient on their way from HBM to LDS.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void k_weights(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                     int64_t rows, int32_t blocks, const int32_t* __restrict__ source,
-                                                     const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
-                                                     int64_t length, int64_t most_parts, RowsOf<const T> dy, int32_t width,
-                                                     int32_t out_width, float* __restrict__ dw, float* __restrict__ partial) {
-  __shared__ uint32_t smem[THREADS / WAVE + 1];
-  __shared__ Piece found;
-  __shared__ float xs[DEPTH][TILE], ys[DEPTH][TILE];
-  const Piece piece = find_piece(offsets, experts, slots, length, blockIdx.z, most_parts, &found, smem);
-  if (piece.expert < 0) return;
-  const int32_t c0 = blockIdx.x * TILE, d0 = blockIdx.y * TILE;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float sum[4][4] = {};
-  for (int64_t s0 = piece.begin; s0 < piece.end; s0 += DEPTH) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < DEPTH * TILE; i += THREADS) {
-      const int k = i / TILE, col = i % TILE;
-      const int64_t s = s0 + k;
-      float x = 0.f, y = 0.f;
-      if (s < piece.end) {
-        const int64_t r = source ? source[s] : s;
-        const int32_t c = c0 + col, d = d0 + col;
-        if (r >= 0 && r < rows && c < width)
-          x = (float)codes[r * blocks * GINEX_CODE_BLOCK + c] * code_step(scales[r * blocks + c / GINEX_CODE_BLOCK]);
-        if (r >= 0 && r < rows && d < out_width) y = (float)*dy.at(s, d);
-      }
-      xs[k][col] = x;
-      ys[k][col] = y;
-    }
-    __syncthreads();
+struct Eight {
+  float v[8];
+  __device__ __forceinline__ void load(const T* p, int left) {
+    constexpr int N = Chunk<T>::N;
 #pragma unroll
-    for (int k = 0; k < DEPTH; ++k)
+    for (int i = 0; i < 8; i += N) {
+      float part[N];
+      load_chunk(p + i, left - i, part);
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[i + n] = part[n];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  }
+  // Term t is the upper half of what the terms before it have left; an infinity is its first term alone.
+  __device__ __forceinline__ words4 next_term() {
+    words4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = upper_halves(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float upper = __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+      v[i] = v[i] == upper ? 0.f : v[i] - upper;
+    }
+    return out;
+  }
+};
+template <>
+struct Eight<bf16> {
+  words4 v;
+  __device__ __forceinline__ void load(const bf16* p, int left) {
+    if (left >= 8) {
+      typedef words4 At __attribute__((aligned(2)));
+      v = *reinterpret_cast<const At*>(p);
+    } else {
+      const uint16_t* const q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[i][j] = fmaf(xs[k][ty * 4 + i], ys[k][tx * 4 + j], sum[i][j]);
+        v[i] = (2 * i < left ? q[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+    }
   }
+  __device__ __forceinline__ void clear() { v = words4{0, 0, 0, 0}; }
+  __device__ __forceinline__ words4 next_term() { return v; }
+};
+
+// Eight numbers along the slots for a lane's row of a matrix operand, from an LDS array that has slots as its rows:
+// the 16 lanes of a group bring 4 rows of 16 numbers and get a column each.
+__device__ __forceinline__ fragment column_of(const bf16* at, int pitch) {
+  typedef __attribute__((address_space(3))) half_words* Local;
+  union {
+    half_words half[2];
+    fragment whole;
+  } u;
+  u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Local)at);
+  u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Local)(at + 4 * pitch));
+  return u.whole;
+}
+
+// A workgroup of WM x WN waves has 64 WM channels and 64 WN outputs of one piece.
+template <typename T, int WM, int WN>
+__global__ __launch_bounds__(WM* WN* WAVE, WM == 4 ? 4 : 3) void k_weights(
+    const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int32_t blocks,
+    const int32_t* __restrict__ source, const int64_t* __restrict__ offsets, int32_t experts, int64_t slots, int64_t length,
+    int64_t most_parts, RowsOf<const T> dy, int32_t width, int32_t out_width, int32_t tiles_m, int32_t tiles,
+    float* __restrict__ dw, float* __restrict__ partial) {
+  constexpr int THREADS = WM * WN * WAVE, TM = WM * WAVE_TILE, TN = WN * WAVE_TILE, TERM = TERMS<T>;
+  constexpr int XS = DEPTH * TM / 16, YS = DEPTH * TN / 8;             // chunks of 16 codes and of 8 gradients
+  constexpr int XN = (XS + THREADS - 1) / THREADS, YN = (YS + THREADS - 1) / THREADS;
+  constexpr int XP = TM + PAD, YP = TN + PAD;
+  __shared__ bf16 xs[DEPTH * XP];
+  __shared__ bf16 ys[TERM][DEPTH * YP];
+  __shared__ uint32_t smem[THREADS / WAVE + 1];
+  __shared__ Piece found;
+
+  // Workgroups go to the 8 dies in turn: the tiles of a piece, which read the same rows, to one of them.
+  const uint32_t die = blockIdx.x % 8, local = blockIdx.x / 8;
+  const int32_t tile_of = (int32_t)(local % tiles);
+  const Piece piece = find_piece<THREADS>(offsets, experts, slots, length, (int64_t)(local / tiles) * 8 + die, most_parts,
+                                          &found, smem);
+  if (piece.expert < 0) return;
+  const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
+
+  words4 x[XN];
+  uint32_t scale[XN];
+  Eight<T> y[YN];
+  int64_t row[XN];
+  auto find_rows = [&](int64_t s0) {
+#pragma unroll
+    for (int i = 0; i < XN; ++i) {
+      const int q = threadIdx.x + i * THREADS, k = q / (TM / 16);
+      row[i] = -1;
+      if (q < XS && s0 + k < piece.end) {
+        row[i] = source ? source[s0 + k] : s0 + k;
+        row[i] = row[i] < rows ? row[i] : -1;
+      }
+    }
+  };
+  auto fetch = [&](int64_t s0) {
+#pragma unroll
+    for (int i = 0; i < XN; ++i) {
+      const int q = threadIdx.x + i * THREADS, b = c0 / GINEX_CODE_BLOCK + q % (TM / 16) / 2;
+      x[i] = words4{0, 0, 0, 0};
+      scale[i] = 127;
+      if (row[i] >= 0 && b < blocks) {
+        typedef words4 At __attribute__((aligned(8)));
+        x[i] = *reinterpret_cast<const At*>(codes + (row[i] * blocks + b) * GINEX_CODE_BLOCK + q % 2 * 16);
+        scale[i] = scales[row[i] * blocks + b];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < YN; ++i) {
+      const int q = threadIdx.x + i * THREADS, k = q / (TN / 8), d = d0 + q % (TN / 8) * 8;
+      if (q < YS && s0 + k < piece.end && d < out_width) y[i].load(dy.at(s0 + k, d), out_width - d);
+      else y[i].clear();
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int i = 0; i < XN; ++i) {
+      const int q = threadIdx.x + i * THREADS;
+      if (q >= XS) break;
+      const float step = code_step(scale[i]);
+      words4 out[2];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t word = x[i][w];
+        const float f0 = (float)(int8_t)word * step, f1 = (float)(int8_t)(word >> 8) * step;
+        const float f2 = (float)(int8_t)(word >> 16) * step, f3 = (float)(int8_t)(word >> 24) * step;
+        out[w / 2][w % 2 * 2] = upper_halves(f0, f1);
+        out[w / 2][w % 2 * 2 + 1] = upper_halves(f2, f3);
+      }
+      words4* const to = reinterpret_cast<words4*>(xs + q / (TM / 16) * XP + q % (TM / 16) * 16);
+      to[0] = out[0];
+      to[1] = out[1];
+    }
+#pragma unroll
+    for (int i = 0; i < YN; ++i) {
+      const int q = threadIdx.x + i * THREADS;
+      if (q >= YS) break;
+#pragma unroll
+      for (int t = 0; t < TERM; ++t)
+        *reinterpret_cast<words4*>(ys[t] + q / (TN / 8) * YP + q % (TN / 8) * 8) = y[i].next_term();
+    }
+  };
+
+  // A lane's place in the operands: the group of 16 lanes reads rows k .. k+3 of 16 columns; lanes 32 to 63
+  // have slots 8 to 15.  Rows lie 64 bytes (of 256: all banks) apart, so that a half-wave's 4 rows of 64 bytes
+  // use every bank once.
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  const int wm = wave % WM, wn = wave / WM;
+  const int k_of = 8 * (lane / 32) + lane % 16 / 4, col_of = lane % 32 / 16 * 16 + lane % 4 * 4;
+  const bf16* const xa = xs + k_of * XP + wm * WAVE_TILE + col_of;
+  const int yb = k_of * YP + wn * WAVE_TILE + col_of;
+  tile sum[2][2] = {};
+  auto product = [&]() {
+#pragma unroll
+    for (int k = 0; k < DEPTH; k += 16) {
+      fragment a[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) a[m] = column_of(xa + k * XP + m * 32, XP);
+#pragma unroll
+      for (int t = 0; t < TERM; ++t) {
+        fragment b[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) b[n] = column_of(ys[t] + yb + k * YP + n * 32, YP);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], b[n], sum[m][n], 0, 0, 0);
+      }
+    }
+  };
+
+  find_rows(piece.begin);
+  fetch(piece.begin);
+  find_rows(piece.begin + DEPTH);
+  for (int64_t s0 = piece.begin; s0 < piece.end; s0 += DEPTH) {
+    lds_barrier();
+    put();
+    fetch(s0 + DEPTH);
+    find_rows(s0 + 2 * DEPTH);
+    lds_barrier();
+    product();
+  }
+
   const int64_t size = (int64_t)width * out_width;
   float* const to = piece.part < 0 ? dw + piece.expert * size : partial + piece.part * size;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int32_t c = c0 + ty * 4 + i, d = d0 + tx * 4 + j;
-      if (c < width && d < out_width) to[(int64_t)c * out_width + d] = sum[i][j];
-    }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int32_t c = c0 + wm * WAVE_TILE + m * 32 + i % 4 + i / 4 * 8 + lane / 32 * 4;
+        const int32_t d = d0 + wn * WAVE_TILE + n * 32 + lane % 32;
+        if (c < width && d < out_width) to[(int64_t)c * out_width + d] = sum[m][n][i];
+      }
 }
 
 // Experts of several pieces: added up in order.  Experts without slots: cleared.
-__global__ __launch_bounds__(THREADS) void k_weights_join(const int64_t* __restrict__ offsets, int32_t experts,
+__global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __restrict__ offsets, int32_t experts,
                                                           int64_t slots, int64_t length, int64_t most_parts, int64_t size,
                                                           const float* __restrict__ partial, float* __restrict__ dw) {
-  __shared__ uint32_t smem[THREADS / WAVE + 1];
+  __shared__ uint32_t smem[JOIN_THREADS / WAVE + 1];
   const int32_t mine = blockIdx.y;
   uint32_t before = 0;
-  for (int32_t e0 = 0; e0 < mine; e0 += THREADS) {
+  for (int32_t e0 = 0; e0 < mine; e0 += JOIN_THREADS) {
     const int32_t e = e0 + (int32_t)threadIdx.x;
     int64_t begin = 0, end = 0;
     if (e < mine) slots_of(offsets, e, slots, begin, end);
     const uint32_t pieces = (uint32_t)((end - begin + length - 1) / length);
     uint32_t total;
-    block_exclusive_scan<uint32_t, THREADS>(pieces > 1 ? pieces : 0, smem, total);
+    block_exclusive_scan<uint32_t, JOIN_THREADS>(pieces > 1 ? pieces : 0, smem, total);
     before += total;
   }
   int64_t begin, end;
   slots_of(offsets, mine, slots, begin, end);
   const int64_t pieces = (end - begin + length - 1) / length;
   if (pieces == 1) return;
-  for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < size; i += (int64_t)gridDim.x * THREADS) {
+  for (int64_t i = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x; i < size; i += (int64_t)gridDim.x * JOIN_THREADS) {
     float sum = 0.f;
     for (int64_t p = 0; p < pieces && before + p < most_parts; ++p) sum += partial[(before + p) * size + i];
     dw[mine * size + i] = sum;
   }
 }
 
+// Waves of a workgroup along the channels and the outputs.
+struct Tiling {
+  int32_t wm, wn;
+  int64_t tiles_m, tiles_n;
+  int64_t tiles() const { return tiles_m * tiles_n; }
+};
+
+Tiling tiling_of(int64_t width, int64_t out_width) {
+  Tiling t;
+  t.wm = width > 2 * WAVE_TILE ? 4 : width > WAVE_TILE ? 2 : 1;
+  t.wn = t.wm == 1 ? 4 : 2;
+  t.tiles_m = ceil_div(width, t.wm * WAVE_TILE);
+  t.tiles_n = ceil_div(out_width, t.wn * WAVE_TILE);
+  return t;
+}
+
 Shares shares_of(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
-  const int64_t tiles = ceil_div(width, TILE) * ceil_div(out_width, TILE);
-  int64_t cuts = ceil_div(1024, tiles);
+  const Tiling t = tiling_of(width, out_width);
+  int64_t cuts = ceil_div(512, t.tiles());
   const int64_t most = ceil_div(slots, 512);
   cuts = cuts < most ? cuts : most;
   cuts = cuts < 1 ? 1 : cuts;
@@ -199,14 +398,19 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
   const int64_t size = kept->width * dy->width;
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const dim3 grid((unsigned)ceil_div(kept->width, TILE), (unsigned)ceil_div(dy->width, TILE), (unsigned)share.pieces);
-    hipLaunchKernelGGL(k_weights<T>, grid, dim3(THREADS), 0, st, kept->codes, kept->scales, kept->rows,
-                       (int32_t)code_blocks(kept->width), source, offsets, experts, slots, share.length,
-                       share.parts, RowsOf<const T>{static_cast<const T*>(dy->data), dy->stride}, (int32_t)kept->width,
-                       (int32_t)dy->width, dw, partial);
+    const Tiling by = tiling_of(kept->width, dy->width);
+    const auto kernel = by.wm == 4 ? k_weights<T, 4, 2> : by.wm == 2 ? k_weights<T, 2, 2> : k_weights<T, 1, 4>;
+    const int64_t groups = ceil_div(share.pieces, 8) * 8 * by.tiles();
+    if (groups >= ((int64_t)1 << 31)) return fail(GINEX_ERR_ARG, "weight gradient: %d x %lld x %lld weights are too many",
+                                                  experts, (long long)kept->width, (long long)dy->width);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups),
+                       dim3((unsigned)(by.wm * by.wn * WAVE)), 0, st, kept->codes, kept->scales, kept->rows,
+                       (int32_t)code_blocks(kept->width), source, offsets, experts, slots, share.length, share.parts,
+                       RowsOf<const T>{static_cast<const T*>(dy->data), dy->stride}, (int32_t)kept->width,
+                       (int32_t)dy->width, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
     GINEX_LAUNCH_CHECK();
-    const int64_t blocks = ceil_div(size, THREADS);
-    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)experts), dim3(THREADS), 0,
+    const int64_t blocks = ceil_div(size, JOIN_THREADS);
+    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)experts), dim3(JOIN_THREADS), 0,
                        st, offsets, experts, slots, share.length, share.parts, size, partial, dw);
     GINEX_LAUNCH_CHECK();
     return GINEX_OK;
