@@ -91,53 +91,57 @@ __device__ __forceinline__ uint32_t upper_halves(float first, float second) {
   return __builtin_amdgcn_perm(__float_as_uint(second), __float_as_uint(first), 0x07060302u);
 }
 
-// Eight elements of a gradient on their way from HBM to LDS.
+// Eight elements of a gradient on their way from HBM to LDS: as they came, until they are cut into terms.
 template <typename T>
 struct Eight {
-  float v[8];
+  static constexpr int N = Chunk<T>::N;
+  typename Chunk<T>::Wide v[8 / N];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) v[i] = *reinterpret_cast<const typename Chunk<T>::At*>(p + i * N);
+  }
   __device__ __forceinline__ void load(const T* p, int left) {
-    constexpr int N = Chunk<T>::N;
 #pragma unroll
-    for (int i = 0; i < 8; i += N) {
-      float part[N];
-      load_chunk(p + i, left - i, part);
-#pragma unroll
-      for (int n = 0; n < N; ++n) v[i + n] = part[n];
-    }
+    for (int i = 0; i < 8; ++i) v[i / N][i % N] = i < left ? p[i] : (T)0.f;
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    for (int i = 0; i < 8; ++i) v[i / N][i % N] = (T)0.f;
   }
-  // Term t is the upper half of what the terms before it have left; an infinity is its first term alone.
-  __device__ __forceinline__ words4 next_term() {
+};
+
+// Term t is the upper half (sign, exponent, 8 bits of significand) of what the terms before it have left.  An infinity
+// is its first term alone: taken from itself it would leave a NaN.  One is looked for in all eight numbers at once.
+template <typename T>
+struct Terms {
+  float v[8];
+  bool infinite;
+  __device__ __forceinline__ explicit Terms(const Eight<T>& from) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = (float)from.v[i / Eight<T>::N][i % Eight<T>::N];
+      top = fmaxf(top, fabsf(v[i]));
+    }
+    infinite = __any(top == INFINITY);
+  }
+  __device__ __forceinline__ words4 next() {
     words4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = upper_halves(v[2 * i], v[2 * i + 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float upper = __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
-      v[i] = v[i] == upper ? 0.f : v[i] - upper;
+      const float left = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+      v[i] = infinite && fabsf(v[i]) == INFINITY ? 0.f : left;
     }
     return out;
   }
 };
 template <>
-struct Eight<bf16> {
+struct Terms<bf16> {
   words4 v;
-  __device__ __forceinline__ void load(const bf16* p, int left) {
-    if (left >= 8) {
-      typedef words4 At __attribute__((aligned(2)));
-      v = *reinterpret_cast<const At*>(p);
-    } else {
-      const uint16_t* const q = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        v[i] = (2 * i < left ? q[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)q[2 * i + 1] << 16 : 0u);
-    }
-  }
-  __device__ __forceinline__ void clear() { v = words4{0, 0, 0, 0}; }
-  __device__ __forceinline__ words4 next_term() { return v; }
+  __device__ __forceinline__ explicit Terms(const Eight<bf16>& from) : v(__builtin_bit_cast(words4, from.v[0])) {}
+  __device__ __forceinline__ words4 next() { return v; }
 };
 
 // Eight numbers along the slots for a lane's row of a matrix operand, from an LDS array that has slots as its rows:
@@ -158,11 +162,12 @@ template <typename T, int WM, int WN>
 __global__ __launch_bounds__(WM* WN* WAVE, WM == 4 ? 4 : 3) void k_weights(
     const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int32_t blocks,
     const int32_t* __restrict__ source, const int64_t* __restrict__ offsets, int32_t experts, int64_t slots, int64_t length,
-    int64_t most_parts, RowsOf<const T> dy, int32_t width, int32_t out_width, int32_t tiles_m, int32_t tiles,
+    int64_t most_parts, RowsOf<const T> dy, int32_t width, int32_t out_width, int64_t whole_slots, int32_t tiles_m, int32_t tiles,
     float* __restrict__ dw, float* __restrict__ partial) {
   constexpr int THREADS = WM * WN * WAVE, TM = WM * WAVE_TILE, TN = WN * WAVE_TILE, TERM = TERMS<T>;
   constexpr int XS = DEPTH * TM / 16, YS = DEPTH * TN / 8;             // chunks of 16 codes and of 8 gradients
-  constexpr int XN = (XS + THREADS - 1) / THREADS, YN = (YS + THREADS - 1) / THREADS;
+  constexpr int XN = (XS + THREADS - 1) / THREADS, YN = YS / THREADS;
+  static_assert(YS % THREADS == 0, "every thread has as many chunks");
   constexpr int XP = TM + PAD, YP = TN + PAD;
   __shared__ bf16 xs[DEPTH * XP];
   __shared__ bf16 ys[TERM][DEPTH * YP];
@@ -177,55 +182,85 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM == 4 ? 4 : 3) void k_weights(
   if (piece.expert < 0) return;
   const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
 
+  // Loads are issued a step ahead and not looked at before put(): no branch and no use stands between them.  What
+  // lies behind the piece's last slot is read from that slot and cleared in put(); what lies behind the last channel or
+  // output goes to sums that are not written.
   words4 x[XN];
   uint32_t scale[XN];
   Eight<T> y[YN];
-  int64_t row[XN];
+  int32_t row[XN], row_of[XN];       // rows of the slots of the next step, and of the one in x
+  const int64_t last = piece.end - 1;
+  // Steps that end here or before read whole chunks: a row of dy that ends inside a chunk is read beyond its end, which
+  // is inside dy except for the rows at its end.
+  const int64_t whole_end = piece.end < whole_slots ? piece.end : whole_slots;
+  const uint32_t pitch = (uint32_t)blocks * GINEX_CODE_BLOCK;
+  const int8_t* x_at[XN];
+  const uint8_t* scale_at[XN];
+  const T* y_at[YN];
+#pragma unroll
+  for (int i = 0; i < XN; ++i) {
+    const int q = threadIdx.x + i * THREADS, b = c0 / GINEX_CODE_BLOCK + q % (TM / 16) / 2;
+    const int block = b < blocks ? b : blocks - 1;
+    x_at[i] = codes + block * GINEX_CODE_BLOCK + q % 2 * 16;
+    scale_at[i] = scales + block;
+  }
+#pragma unroll
+  for (int i = 0; i < YN; ++i) {
+    const int q = threadIdx.x + i * THREADS, d = d0 + q % (TN / 8) * 8;
+    y_at[i] = dy.at(piece.begin + q / (TN / 8), d < out_width ? d : 0);
+  }
   auto find_rows = [&](int64_t s0) {
 #pragma unroll
     for (int i = 0; i < XN; ++i) {
-      const int q = threadIdx.x + i * THREADS, k = q / (TM / 16);
-      row[i] = -1;
-      if (q < XS && s0 + k < piece.end) {
-        row[i] = source ? source[s0 + k] : s0 + k;
-        row[i] = row[i] < rows ? row[i] : -1;
-      }
+      const int k = (threadIdx.x + i * THREADS) / (TM / 16);
+      const int64_t s = s0 + k < last ? s0 + k : last;
+      row[i] = (int32_t)s;
+      if (source) row[i] = source[s];
     }
   };
   auto fetch = [&](int64_t s0) {
 #pragma unroll
     for (int i = 0; i < XN; ++i) {
-      const int q = threadIdx.x + i * THREADS, b = c0 / GINEX_CODE_BLOCK + q % (TM / 16) / 2;
-      x[i] = words4{0, 0, 0, 0};
-      scale[i] = 127;
-      if (row[i] >= 0 && b < blocks) {
-        typedef words4 At __attribute__((aligned(8)));
-        x[i] = *reinterpret_cast<const At*>(codes + (row[i] * blocks + b) * GINEX_CODE_BLOCK + q % 2 * 16);
-        scale[i] = scales[row[i] * blocks + b];
+      row_of[i] = row[i];
+      // (a row that is not there, of a routing made elsewhere, is cleared in put() as well)
+      const uint32_t r = (uint32_t)row[i] < (uint32_t)rows ? (uint32_t)row[i] : 0;
+      typedef words4 At __attribute__((aligned(8)));
+      x[i] = *reinterpret_cast<const At*>(x_at[i] + (uint64_t)r * pitch);
+      scale[i] = scale_at[i][(uint64_t)r * (uint32_t)blocks];
+    }
+    if (s0 + DEPTH <= whole_end) {
+#pragma unroll
+      for (int i = 0; i < YN; ++i) {
+        y[i].load(y_at[i]);
+        y_at[i] += DEPTH * dy.stride;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < YN; ++i) {
+        const int q = threadIdx.x + i * THREADS, k = q / (TN / 8), d = d0 + q % (TN / 8) * 8;
+        const int64_t s = s0 + k < last ? s0 + k : last;
+        y[i].load(dy.at(s, d < out_width ? d : 0), out_width - (d < out_width ? d : 0));
       }
     }
-#pragma unroll
-    for (int i = 0; i < YN; ++i) {
-      const int q = threadIdx.x + i * THREADS, k = q / (TN / 8), d = d0 + q % (TN / 8) * 8;
-      if (q < YS && s0 + k < piece.end && d < out_width) y[i].load(dy.at(s0 + k, d), out_width - d);
-      else y[i].clear();
-    }
   };
-  auto put = [&]() {
+  auto put = [&](int64_t s0) {
+    const bool ends = s0 + DEPTH > piece.end;
 #pragma unroll
     for (int i = 0; i < XN; ++i) {
       const int q = threadIdx.x + i * THREADS;
-      if (q >= XS) break;
-      const float step = code_step(scale[i]);
+      if (XS % THREADS && q >= XS) break;
+      const float step = code_step(scale[i]), below = -128.f * step;
       words4 out[2];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const uint32_t word = x[i][w];
-        const float f0 = (float)(int8_t)word * step, f1 = (float)(int8_t)(word >> 8) * step;
-        const float f2 = (float)(int8_t)(word >> 16) * step, f3 = (float)(int8_t)(word >> 24) * step;
+        // q step = (q + 128) step - 128 step, exactly: a byte becomes a float in one instruction if it has no sign
+        const uint32_t word = x[i][w] ^ 0x80808080u;
+        const float f0 = fmaf((float)(word & 255), step, below), f1 = fmaf((float)(word >> 8 & 255), step, below);
+        const float f2 = fmaf((float)(word >> 16 & 255), step, below), f3 = fmaf((float)(word >> 24), step, below);
         out[w / 2][w % 2 * 2] = upper_halves(f0, f1);
         out[w / 2][w % 2 * 2 + 1] = upper_halves(f2, f3);
       }
+      if ((ends && s0 + q / (TM / 16) > last) || (uint32_t)row_of[i] >= (uint32_t)rows) out[0] = out[1] = words4{0, 0, 0, 0};
       words4* const to = reinterpret_cast<words4*>(xs + q / (TM / 16) * XP + q % (TM / 16) * 16);
       to[0] = out[0];
       to[1] = out[1];
@@ -233,10 +268,11 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM == 4 ? 4 : 3) void k_weights(
 #pragma unroll
     for (int i = 0; i < YN; ++i) {
       const int q = threadIdx.x + i * THREADS;
-      if (q >= YS) break;
+      if (ends && s0 + q / (TN / 8) > last) y[i].clear();
+      Terms<T> terms(y[i]);
 #pragma unroll
       for (int t = 0; t < TERM; ++t)
-        *reinterpret_cast<words4*>(ys[t] + q / (TN / 8) * YP + q % (TN / 8) * 8) = y[i].next_term();
+        *reinterpret_cast<words4*>(ys[t] + q / (TN / 8) * YP + q % (TN / 8) * 8) = terms.next();
     }
   };
 
@@ -273,7 +309,7 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM == 4 ? 4 : 3) void k_weights(
   find_rows(piece.begin + DEPTH);
   for (int64_t s0 = piece.begin; s0 < piece.end; s0 += DEPTH) {
     lds_barrier();
-    put();
+    put(s0);
     fetch(s0 + DEPTH);
     find_rows(s0 + 2 * DEPTH);
     lds_barrier();
@@ -339,7 +375,10 @@ Tiling tiling_of(int64_t width, int64_t out_width) {
 
 Shares shares_of(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
   const Tiling t = tiling_of(width, out_width);
-  int64_t cuts = ceil_div(512, t.tiles());
+  // Two workgroups to a CU.  Every expert's last piece may be a short one, so there are up to `experts` more pieces than
+  // cuts: they are to fit in as well, unless there are so many that the GPU goes through its pieces several times anyway.
+  int64_t cuts = 512 / t.tiles() - experts;
+  if (cuts < 256 / t.tiles()) cuts = ceil_div(1024, t.tiles());
   const int64_t most = ceil_div(slots, 512);
   cuts = cuts < most ? cuts : most;
   cuts = cuts < 1 ? 1 : cuts;
@@ -398,6 +437,9 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
   const int64_t size = kept->width * dy->width;
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
+    // rows at the end of dy from which no 8 elements can be read at the last chunk
+    const int64_t over = (8 - dy->width % 8) % 8;
+    const int64_t cut_off = over == 0 ? 0 : dy->stride == 0 ? slots : ceil_div(over, dy->stride);
     const Tiling by = tiling_of(kept->width, dy->width);
     const auto kernel = by.wm == 4 ? k_weights<T, 4, 2> : by.wm == 2 ? k_weights<T, 2, 2> : k_weights<T, 1, 4>;
     const int64_t groups = ceil_div(share.pieces, 8) * 8 * by.tiles();
@@ -407,7 +449,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
                        dim3((unsigned)(by.wm * by.wn * WAVE)), 0, st, kept->codes, kept->scales, kept->rows,
                        (int32_t)code_blocks(kept->width), source, offsets, experts, slots, share.length, share.parts,
                        RowsOf<const T>{static_cast<const T*>(dy->data), dy->stride}, (int32_t)kept->width,
-                       (int32_t)dy->width, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
+                       (int32_t)dy->width, slots - cut_off, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
     GINEX_LAUNCH_CHECK();
     const int64_t blocks = ceil_div(size, JOIN_THREADS);
     hipLaunchKernelGGL(k_weights_join, dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)experts), dim3(JOIN_THREADS), 0,
