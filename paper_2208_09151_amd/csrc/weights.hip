@@ -50,14 +50,24 @@ __device__ __forceinline__ int64_t range_length(const int64_t* __restrict__ offs
   int64_t taken = offsets ? offsets[experts] : slots;
   taken = taken < 0 ? 0 : (taken < slots ? taken : slots);
   const int64_t length = ((taken + ranges - 1) / ranges + STEP - 1) / STEP * STEP;
-  return length > STEP ? length : STEP;
+  return uniform(length > STEP ? length : STEP);
+}
+
+// Ranges begin at multiples of their length, but not near to where an expert begins: there they begin with it, which
+// spares its part in the workspace and the start of another sum.  Both cost about as much as NEAR slots do.
+constexpr int64_t NEAR = 256;
+
+__device__ __forceinline__ int64_t near_of(int64_t length) { return length / 2 < NEAR ? length / 2 : NEAR; }
+
+// Where a range that would begin at `at`, a slot of the expert that has begin .. end - 1, does begin.
+__device__ __forceinline__ int64_t range_begin_of(int64_t at, int64_t length, int64_t begin, int64_t end) {
+  const int64_t near = near_of(length);
+  return at - begin <= near ? begin : end - at <= near ? end : at;
 }
 
 // Where a range leaves its part of an expert that it shares: only the first of its experts can have begun in front of
 // it, and only the last can go on behind it.
-__device__ __forceinline__ int64_t part_of(int64_t range, int64_t length, int64_t begin) {
-  return 2 * range + (begin >= range * length ? 1 : 0);
-}
+__device__ __forceinline__ int64_t part_of(int64_t range, bool first) { return 2 * range + (first ? 1 : 0); }
 
 // Waits for this wave's LDS accesses and for the other waves, not for loads from HBM that are under way.
 __device__ __forceinline__ void lds_barrier() {
@@ -135,10 +145,10 @@ __device__ __forceinline__ fragment column_of(const bf16* at, int pitch) {
   return u.whole;
 }
 
-// A workgroup of WM x WN waves of 64 x 32 NT has 64 WM channels and 32 NT WN outputs of a range.
-template <typename T, int WM, int WN, int NT>
+// A workgroup of WM x WN waves of 32 MT x 32 NT has 32 MT WM channels and 32 NT WN outputs of a range.
+template <typename T, int WM, int MT, int WN, int NT>
 struct Shape {
-  static constexpr int THREADS = WM * WN * WAVE, TM = WM * 64, TN = WN * NT * 32, TERM = TERMS<T>;
+  static constexpr int THREADS = WM * WN * WAVE, TM = WM * MT * 32, TN = WN * NT * 32, TERM = TERMS<T>;
   static constexpr int BUFFERS = WM * WN == 8 ? 2 : 1;
   static constexpr int DEPTH = TERM == 1 && BUFFERS == 2 ? 64 : 32;       // slots in LDS at a time
   static constexpr int XP = TM + PAD, YP = TN + PAD;
@@ -147,34 +157,47 @@ struct Shape {
 };
 
 // NARROW: dy has fewer than 8 columns.
-template <typename T, int WM, int WN, int NT, bool NARROW>
+template <typename T, int WM, int MT, int WN, int NT, bool NARROW>
 __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
     const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int32_t blocks,
     const int32_t* __restrict__ source, const int64_t* __restrict__ offsets, int32_t experts, int64_t slots, int32_t ranges,
     RowsOf<const T> dy, int32_t width, int32_t out_width, int32_t tiles_m, int32_t tiles, float* __restrict__ dw,
     float* __restrict__ partial) {
-  using S = Shape<T, WM, WN, NT>;
+  using S = Shape<T, WM, MT, WN, NT>;
   constexpr int THREADS = S::THREADS, TM = S::TM, TN = S::TN, TERM = S::TERM, DEPTH = S::DEPTH, XP = S::XP, YP = S::YP;
   constexpr int XS = DEPTH * TM / 16, YS = DEPTH * TN / 8;             // chunks of 16 codes and of 8 gradients
   constexpr int XN = (XS + THREADS - 1) / THREADS, YN = YS / THREADS;
   static_assert(YS % THREADS == 0 && STEP % DEPTH == 0 && (XS % THREADS == 0 || XS < THREADS), "chunks of a thread");
   __shared__ __attribute__((aligned(16))) bf16 lds[S::BUFFERS * S::SIZE];
+  __shared__ int64_t ends[2];
   __shared__ int32_t first_last[2];
 
   // Workgroups go to the 8 dies in turn: the tiles of a range, which read the same rows, to one of them.
   const uint32_t die = blockIdx.x % 8, local = blockIdx.x / 8;
   const int32_t tile_of = (int32_t)(local % tiles);
   const int64_t range = (int64_t)(local / tiles) * 8 + die;
-  const int64_t length = uniform(range_length(offsets, experts, slots, ranges));
-  const int64_t range_begin = range * length, range_end = range_begin + length;
+  if (range >= ranges) return;
+  const int64_t length = range_length(offsets, experts, slots, ranges);
   const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
 
-  // the experts that have slots in the range
+  // its ends, and the experts that have slots in it
   if (threadIdx.x == 0) {
     first_last[0] = experts;
     first_last[1] = -1;
+    ends[0] = ends[1] = slots;
   }
   __syncthreads();
+  for (int32_t e = threadIdx.x; e < experts; e += THREADS) {
+    int64_t begin, end;
+    slots_of(offsets, e, slots, begin, end);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = (range + i) * length;
+      if (begin <= at && at < end) ends[i] = range_begin_of(at, length, begin, end);
+    }
+  }
+  __syncthreads();
+  const int64_t range_begin = uniform(ends[0]), range_end = uniform(ends[1]);
   for (int32_t e = threadIdx.x; e < experts; e += THREADS) {
     int64_t begin, end;
     slots_of(offsets, e, slots, begin, end);
@@ -211,7 +234,7 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wm = wave % WM, wn = wave / WM;
   const int k_of = 8 * (lane / 32) + lane % 16 / 4, col_of = lane % 32 / 16 * 16 + lane % 4 * 4;
-  const int xb = k_of * XP + wm * 64 + col_of, yb = S::XSIZE + k_of * YP + wn * NT * 32 + col_of;
+  const int xb = k_of * XP + wm * MT * 32 + col_of, yb = S::XSIZE + k_of * YP + wn * NT * 32 + col_of;
 
   for (int32_t expert = first_expert; expert <= last_expert; ++expert) {
     int64_t expert_begin, expert_end;
@@ -222,15 +245,16 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
     const int64_t end = expert_end < range_end ? expert_end : range_end;
     if (begin >= end) continue;
 
-    // Loads are issued a step ahead and not looked at before put(): no branch and no use stands between them.  What
-    // lies behind the last slot is read from that slot and cleared in put().
-    words4 x[XN];
-    uint32_t scale[XN];
-    Eight<T> y[YN];
-    int32_t row[XN];                   // of the slots of the next step
-    bool there[XN];                    // whether the row of the one in x is: it may not be in a routing made elsewhere
+    // Loads are issued two steps ahead and not looked at before put(): no branch and no use stands between them.  With
+    // one step ahead the requests of all workgroups come at once, and then HBM waits for the next ones.  What lies
+    // behind the last slot is read from that slot and cleared in put().
+    words4 x[2][XN];
+    uint32_t scale[2][XN];
+    Eight<T> y[2][YN];
+    bool there[2][XN];                 // whether the row in x exists: it may not, in a routing made elsewhere
+    int32_t row[XN];                   // of the slots of the step that is fetched next
     const int64_t last = end - 1;
-    auto find_rows = [&](int64_t s0) {
+    auto find_rows = [&](int32_t (&row)[XN], int64_t s0) {
       const int64_t from = s0 < last ? s0 : last;
       const uint32_t left = (uint32_t)(last - from < DEPTH ? last - from : DEPTH);
       const int32_t* const at = source_or_any + (source ? from : 0);
@@ -240,40 +264,42 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
         row[i] = at[source ? (k < left ? k : left) : 0];
       }
     };
-    auto fetch = [&](int64_t s0) {
+    auto fetch = [&](auto set, const int32_t (&row)[XN], int64_t s0) {
+      constexpr int P = decltype(set)::value;
       const int64_t from = s0 < last ? s0 : last;
       const uint32_t left = (uint32_t)(last - from < DEPTH ? last - from : DEPTH);
 #pragma unroll
       for (int i = 0; i < XN; ++i) {
         const uint32_t k = (threadIdx.x + i * THREADS) / (TM / 16);
         uint32_t r = source ? (uint32_t)row[i] : (uint32_t)from + (k < left ? k : left);
-        there[i] = r < (uint32_t)rows;
-        r = there[i] ? r : 0;
+        there[P][i] = r < (uint32_t)rows;
+        r = there[P][i] ? r : 0;
         typedef words4 At __attribute__((aligned(8)));
-        x[i] = *reinterpret_cast<const At*>(codes + ((uint64_t)r * pitch + x_at[i]));
-        scale[i] = scales[(uint64_t)r * (uint32_t)blocks + scale_at[i]];
+        x[P][i] = *reinterpret_cast<const At*>(codes + ((uint64_t)r * pitch + x_at[i]));
+        scale[P][i] = scales[(uint64_t)r * (uint32_t)blocks + scale_at[i]];
       }
       const T* const at = dy.data + from * dy.stride;
 #pragma unroll
       for (int i = 0; i < YN; ++i) {
         const uint32_t k = (threadIdx.x + i * THREADS) / (TN / 8);
         const T* const p = at + ((uint64_t)(k < left ? k : left) * stride + y_at[i]);
-        if (NARROW) y[i].load(p, out_width);
-        else y[i].load(p);
+        if (NARROW) y[P][i].load(p, out_width);
+        else y[P][i].load(p);
       }
     };
-    auto put = [&](bf16* to, int64_t s0) {
+    auto put = [&](auto set, bf16* to, int64_t s0) {
+      constexpr int P = decltype(set)::value;
       const int left = (int)(last - s0 < DEPTH ? last - s0 : DEPTH);      // the last row that is a slot's
 #pragma unroll
       for (int i = 0; i < XN; ++i) {
         const int q = threadIdx.x + i * THREADS;
         if (XS < THREADS && q >= XS) break;
-        const float step = there[i] && q / (TM / 16) <= left ? code_step(scale[i]) : 0.f, below = -128.f * step;
+        const float step = there[P][i] && q / (TM / 16) <= left ? code_step(scale[P][i]) : 0.f, below = -128.f * step;
         words4 out[2];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           // q step = (q + 128) step - 128 step, exactly: a byte becomes a float in one instruction if it has no sign
-          const uint32_t word = x[i][w] ^ 0x80808080u;
+          const uint32_t word = x[P][i][w] ^ 0x80808080u;
           const float f0 = fmaf((float)(word & 255), step, below), f1 = fmaf((float)(word >> 8 & 255), step, below);
           const float f2 = fmaf((float)(word >> 16 & 255), step, below), f3 = fmaf((float)(word >> 24), step, below);
           out[w / 2][w % 2 * 2] = upper_halves(f0, f1);
@@ -286,105 +312,128 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
       if (__builtin_expect(left < DEPTH - 1, false)) {
 #pragma unroll
         for (int i = 0; i < YN; ++i)
-          if ((int)(threadIdx.x + i * THREADS) / (TN / 8) > left) y[i].clear();
+          if ((int)(threadIdx.x + i * THREADS) / (TN / 8) > left) y[P][i].clear();
       }
 #pragma unroll
       for (int i = 0; i < YN; ++i) {
         const int q = threadIdx.x + i * THREADS;
         words4* const at = reinterpret_cast<words4*>(to + S::XSIZE + q / (TN / 8) * YP + q % (TN / 8) * 8);
-        Terms<T> terms(y[i]);
+        Terms<T> terms(y[P][i]);
         at[0] = terms.template next<true>();
 #pragma unroll
         for (int t = 1; t < TERM; ++t) at[t * S::YSIZE / 8] = terms.template next<false>();
       }
     };
-    tile sum[2][NT] = {};
+    tile sum[MT][NT] = {};
     auto product = [&](const bf16* from) {
       constexpr int FRAGMENTS = TERM * NT, STEPS = DEPTH / 16;
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
-        fragment a[2];
+        fragment a[MT];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) a[m] = column_of(from + xb + k * 16 * XP + m * 32, XP);
+        for (int m = 0; m < MT; ++m) a[m] = column_of(from + xb + k * 16 * XP + m * 32, XP);
 #pragma unroll
         for (int j = 0; j < FRAGMENTS; ++j) {
           const int t = j / NT, n = j % NT;
           const fragment b = column_of(from + yb + t * S::YSIZE + k * 16 * YP + n * 32, YP);
 #pragma unroll
-          for (int m = 0; m < 2; ++m) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], b, sum[m][n], 0, 0, 0);
+          for (int m = 0; m < MT; ++m) sum[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[m], b, sum[m][n], 0, 0, 0);
         }
       }
-      // The order of issue: a fragment is read AHEAD pairs of matrix instructions (64 cycles each) before its own pair.
-      constexpr int AHEAD = 3, LDS_READ = 0x100, MATRIX = 0x008;
-      __builtin_amdgcn_sched_group_barrier(LDS_READ, 4 + 2 * AHEAD, 0);
+      // The order of issue: a fragment is read AHEAD groups of matrix instructions (32 MT cycles each) before its own.
+      constexpr int AHEAD = MT == 2 ? 3 : 2, LDS_READ = 0x100, MATRIX = 0x008;
+      __builtin_amdgcn_sched_group_barrier(LDS_READ, 2 * MT + 2 * AHEAD, 0);
 #pragma unroll
       for (int j = 0; j < FRAGMENTS * STEPS; ++j) {
-        __builtin_amdgcn_sched_group_barrier(MATRIX, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(MATRIX, MT, 0);
         if (j + AHEAD < FRAGMENTS * STEPS) {
-          if ((j + AHEAD) % FRAGMENTS == 0) __builtin_amdgcn_sched_group_barrier(LDS_READ, 6, 0);
+          if ((j + AHEAD) % FRAGMENTS == 0) __builtin_amdgcn_sched_group_barrier(LDS_READ, 2 * MT + 2, 0);
           else __builtin_amdgcn_sched_group_barrier(LDS_READ, 2, 0);
         }
       }
     };
 
-    find_rows(begin);
-    fetch(begin);
-    find_rows(begin + DEPTH);
+    const std::integral_constant<int, 0> even;
+    const std::integral_constant<int, 1> odd;
+    {
+      int32_t row0[XN], row1[XN];
+      find_rows(row0, begin);
+      find_rows(row1, begin + DEPTH);
+      find_rows(row, begin + 2 * DEPTH);
+      fetch(even, row0, begin);
+      fetch(odd, row1, begin + DEPTH);
+    }
     if (S::BUFFERS == 1) {
-      for (int64_t s0 = begin; s0 < end; s0 += DEPTH) {
+      auto step = [&](auto set, int64_t s0) {
         lds_barrier();
-        put(lds, s0);
-        fetch(s0 + DEPTH);
-        find_rows(s0 + 2 * DEPTH);
+        put(set, lds, s0);
+        fetch(set, row, s0 + 2 * DEPTH);
+        find_rows(row, s0 + 3 * DEPTH);
         lds_barrier();
         product(lds);
+      };
+      for (int64_t s0 = begin; s0 < end; s0 += 2 * DEPTH) {
+        step(even, s0);
+        if (s0 + DEPTH < end) step(odd, s0 + DEPTH);
       }
     } else {
       // The next step is put into one half of LDS while the matrix cores work from the other.  The two waves of a SIMD
       // do the two things in opposite order, so that one has the matrix core while the other has the vector unit: the
       // late one is half a turn of the loop ahead with its product.  What is put behind the last step is not read.
       const bool late = wave >= WM * WN / 2;
-      put(lds, begin);
-      fetch(begin + DEPTH);
-      find_rows(begin + 2 * DEPTH);
+      put(even, lds, begin);
+      fetch(even, row, begin + 2 * DEPTH);
+      find_rows(row, begin + 3 * DEPTH);
       lds_barrier();
       if (late) product(lds);
-      int half = 1;
-      for (int64_t s0 = begin; s0 < end; s0 += DEPTH) {
-        put(lds + half * S::SIZE, s0 + DEPTH);
-        fetch(s0 + 2 * DEPTH);
-        find_rows(s0 + 3 * DEPTH);
+      auto step = [&](auto set, int64_t s0) {
+        constexpr int P = decltype(set)::value;
+        put(set, lds + P * S::SIZE, s0 + DEPTH);
+        fetch(set, row, s0 + 3 * DEPTH);
+        find_rows(row, s0 + 4 * DEPTH);
         if (late) lds_barrier();
-        if (!late || s0 + DEPTH < end) product(lds + (late ? half : half ^ 1) * S::SIZE);
+        if (s0 + (late ? DEPTH : 0) < end) product(lds + (late ? P : 1 - P) * S::SIZE);
         if (!late) lds_barrier();
-        half ^= 1;
+      };
+      for (int64_t s0 = begin; s0 < end; s0 += 2 * DEPTH) {
+        step(odd, s0);
+        step(even, s0 + DEPTH);
       }
     }
 
     const int64_t size = (int64_t)width * out_width;
     const bool whole = expert_begin >= range_begin && expert_end <= range_end;
-    float* const to = whole ? dw + expert * size : partial + part_of(range, length, expert_begin) * size;
+    float* const to = whole ? dw + expert * size : partial + part_of(range, expert_begin >= range_begin) * size;
     // (the lane's number is made anew: addresses that do not depend on the expert would be kept through the loop above)
     int here = lane;
     asm volatile("" : "+v"(here));
-    const int32_t c1 = c0 + wm * 64 + here / 32 * 4, d1 = d0 + wn * NT * 32 + here % 32;
-    int32_t d[NT];
+    const int32_t c1 = c0 + wm * MT * 32 + here / 32 * 4, d1 = d0 + wn * NT * 32 + here % 32;
+    if (c0 + TM <= width && d0 + TN <= out_width) {
+      float* at = to + (int64_t)c1 * out_width + d1;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      d[n] = d1 + n * 32;
-      // (a chunk that ends with the row, see y_at)
-      if (!NARROW && d[n] / 8 * 8 > out_width - 8 && d[n] / 8 * 8 < out_width) d[n] = out_width - 8 + d[n] % 8;
-    }
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+        for (int i = 0; i < 16; ++i) {
+          float* const line = at + (int64_t)(m * 32 + i % 4 + i / 4 * 8) * out_width;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int32_t c = c1 + m * 32 + i % 4 + i / 4 * 8;
-        float* const at = to + (int64_t)c * out_width;
+          for (int n = 0; n < NT; ++n) line[n * 32] = sum[m][n][i];
+        }
+    } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-          if (c < width && d[n] < out_width) at[d[n]] = sum[m][n][i];
+      for (int n = 0; n < NT; ++n) {
+        int32_t d = d1 + n * 32;
+        // (a chunk that ends with the row, see y_at)
+        if (!NARROW && d / 8 * 8 > out_width - 8 && d / 8 * 8 < out_width) d = out_width - 8 + d % 8;
+        float* const at = to + d;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int32_t c = c1 + m * 32 + i % 4 + i / 4 * 8;
+            if (c < width && d < out_width) at[(int64_t)c * out_width] = sum[m][n][i];
+          }
       }
+    }
   }
 }
 
@@ -396,19 +445,39 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __
   const int64_t length = range_length(offsets, experts, slots, ranges);
   int64_t begin, end;
   slots_of(offsets, mine, slots, begin, end);
-  const int64_t first = begin / length, last = end > begin ? (end - 1) / length : first - 1;
-  if (first == last) return;
-  for (int64_t i = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x; i < size; i += (int64_t)gridDim.x * JOIN_THREADS) {
-    float sum = 0.f;
-    for (int64_t r = first; r <= last && r < ranges; ++r) sum += partial[part_of(r, length, begin) * size + i];
-    dw[mine * size + i] = sum;
+  // the ranges that begin inside the expert; the one in front of them has its first part
+  const int64_t near = near_of(length);
+  const int64_t first = (begin + near) / length + 1;
+  int64_t last = (end - near - 1) / length;
+  if (end > begin && last < first) return;
+  last = end > begin && last >= ranges ? ranges - 1 : last;
+  const int64_t i = ((int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
+  if (i >= size) return;
+  typedef float four __attribute__((ext_vector_type(4)));
+  typedef four At __attribute__((aligned(4)));
+  four sum = {};
+  if (i + 4 <= size) {
+    if (end > begin) {
+      sum = *reinterpret_cast<const At*>(partial + part_of(first - 1, true) * size + i);
+#pragma unroll 4
+      for (int64_t r = first; r <= last; ++r) sum += *reinterpret_cast<const At*>(partial + part_of(r, false) * size + i);
+    }
+    *reinterpret_cast<At*>(dw + mine * size + i) = sum;
+  } else {
+    for (int64_t n = i; n < size; ++n) {
+      float one = 0.f;
+      if (end > begin) {
+        one = partial[part_of(first - 1, true) * size + n];
+        for (int64_t r = first; r <= last; ++r) one += partial[part_of(r, false) * size + n];
+      }
+      dw[mine * size + n] = one;
+    }
   }
 }
 
-// The workgroup's shape by the sizes: one tile for all channels up to 256, so that a gradient is cut into its terms
-// once, and tiles no wider than the outputs ask for.
+// The workgroup's shape and the number of ranges by the sizes.
 struct Tiling {
-  int32_t wm, wn, nt;
+  int32_t wm, mt, wn, nt;
   int64_t tiles_m, tiles_n;
   int32_t ranges;
   int64_t tiles() const { return tiles_m * tiles_n; }
@@ -417,14 +486,25 @@ struct Tiling {
 
 Tiling tiling_of(int64_t slots, int64_t width, int64_t out_width) {
   Tiling t;
-  t.wm = out_width < 8 ? 2 : width > 128 ? 4 : width > 64 ? 2 : 1;
-  t.wn = t.wm == 4 || (t.wm == 2 && out_width <= 128) ? 2 : 4;
-  t.nt = t.wm == 4 && out_width > 128 ? 4 : 2;
-  t.tiles_m = ceil_div(width, t.wm * 64);
-  t.tiles_n = ceil_div(out_width, t.wn * t.nt * 32);
-  const int64_t groups = t.wm * t.wn == 8 ? 256 : 512;
-  int64_t ranges = groups / t.tiles();
-  const int64_t most = ceil_div(slots, 256);
+  const auto shape = [&](int wm, int mt, int wn, int nt) {
+    t.wm = wm;
+    t.mt = mt;
+    t.wn = wn;
+    t.nt = nt;
+    t.tiles_m = ceil_div(width, wm * mt * 32);
+    t.tiles_n = ceil_div(out_width, wn * nt * 32);
+  };
+  // One tile for all of up to 256 outputs where every CU has a thousand slots to go through: gradients and codes are
+  // then taken apart once (and not once per tile of 128), but a CU has room for one such workgroup.  256 x 256 weights of
+  // 128 experts from 40 000 slots: 60 us in these, 43 in small ones; 512 x 512 of 32 from 200 000: 151 and 190; 100 x 250
+  // of 64 from 708 000: 99 and 113.  With 128 outputs and fewer there is nothing in it (54 and 54, 65 and 67 us).
+  if (width > 128) shape(4, 2, 2, 4);
+  else shape(2, 2, 4, 2);
+  const bool large = out_width > 128 && slots * t.tiles() >= 256 * 1024;
+  if (!large) shape(2, 2, 2, 2);
+  // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us)
+  int64_t ranges = (large ? 256 : 512) / t.tiles();
+  const int64_t most = ceil_div(slots, 128);
   ranges = ranges < most ? ranges : most;
   t.ranges = (int32_t)(ranges < 1 ? 1 : ranges);
   return t;
@@ -432,10 +512,9 @@ Tiling tiling_of(int64_t slots, int64_t width, int64_t out_width) {
 
 template <typename T>
 auto kernel_of(const Tiling& t, int64_t out_width) {
-  if (out_width < 8) return k_weights<T, 2, 2, 2, true>;
-  if (t.wm == 4) return t.nt == 4 ? k_weights<T, 4, 2, 4, false> : k_weights<T, 4, 2, 2, false>;
-  if (t.wm == 2) return t.wn == 4 ? k_weights<T, 2, 4, 2, false> : k_weights<T, 2, 2, 2, false>;
-  return k_weights<T, 1, 4, 2, false>;
+  if (t.nt == 4) return k_weights<T, 4, 2, 2, 4, false>;
+  if (t.wn == 4) return k_weights<T, 2, 2, 4, 2, false>;
+  return out_width < 8 ? k_weights<T, 2, 2, 2, 2, true> : k_weights<T, 2, 2, 2, 2, false>;
 }
 
 }  // namespace
@@ -492,8 +571,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
                        slots, by.ranges, RowsOf<const T>{static_cast<const T*>(dy->data), dy->stride}, (int32_t)kept->width,
                        (int32_t)dy->width, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
     GINEX_LAUNCH_CHECK();
-    const int64_t blocks = ceil_div(size, JOIN_THREADS);
-    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)experts), dim3(JOIN_THREADS), 0,
+    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(size, 4 * JOIN_THREADS), (unsigned)experts), dim3(JOIN_THREADS), 0,
                        st, offsets, experts, slots, by.ranges, size, partial, dw);
     GINEX_LAUNCH_CHECK();
     return GINEX_OK;
