@@ -13,7 +13,7 @@ namespace ginex {
 namespace {
 
 constexpr int JOIN_THREADS = 256;
-constexpr int STEP = 64;          // the length of a range is a multiple of it
+constexpr int STEP = 16;          // the length of a range is a multiple of it
 constexpr int PAD = 32;           // elements behind a row in LDS, see k_weights
 
 typedef short half_words __attribute__((ext_vector_type(4)));
@@ -44,7 +44,7 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32)) << 32 | lo);
 }
 
-// Slots of a range: the slots that are taken, over `ranges` ranges, in whole steps.
+// Slots of a range: the slots that are taken, over `ranges` ranges, rounded up.
 __device__ __forceinline__ int64_t range_length(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
                                                 int32_t ranges) {
   int64_t taken = offsets ? offsets[experts] : slots;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
   constexpr int THREADS = S::THREADS, TM = S::TM, TN = S::TN, TERM = S::TERM, DEPTH = S::DEPTH, XP = S::XP, YP = S::YP;
   constexpr int XS = DEPTH * TM / 16, YS = DEPTH * TN / 8;             // chunks of 16 codes and of 8 gradients
   constexpr int XN = (XS + THREADS - 1) / THREADS, YN = YS / THREADS;
-  static_assert(YS % THREADS == 0 && STEP % DEPTH == 0 && (XS % THREADS == 0 || XS < THREADS), "chunks of a thread");
+  static_assert(YS % THREADS == 0 && (XS % THREADS == 0 || XS < THREADS), "chunks of a thread");
   __shared__ __attribute__((aligned(16))) bf16 lds[S::BUFFERS * S::SIZE];
   __shared__ int64_t ends[2];
   __shared__ int32_t first_last[2];
@@ -484,7 +484,7 @@ struct Tiling {
   int64_t parts() const { return 2 * (int64_t)ranges; }
 };
 
-Tiling tiling_of(int64_t slots, int64_t width, int64_t out_width) {
+Tiling tiling_of(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
   Tiling t;
   const auto shape = [&](int wm, int mt, int wn, int nt) {
     t.wm = wm;
@@ -504,7 +504,9 @@ Tiling tiling_of(int64_t slots, int64_t width, int64_t out_width) {
   if (!large) shape(2, 2, 2, 2);
   // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us)
   int64_t ranges = (large ? 256 : 512) / t.tiles();
-  const int64_t most = ceil_div(slots, 128);
+  // 128 slots at least, but a range for every expert of few slots (64 rows of 8 experts: 27 -> 14 us)
+  const int64_t each = ceil_div(slots, STEP) < experts ? ceil_div(slots, STEP) : experts;
+  const int64_t most = ceil_div(slots, 128) > each ? ceil_div(slots, 128) : each;
   ranges = ranges < most ? ranges : most;
   t.ranges = (int32_t)(ranges < 1 ? 1 : ranges);
   return t;
@@ -533,7 +535,7 @@ static int32_t check_sizes(int64_t slots, int32_t experts, int64_t width, int64_
 extern "C" size_t ginex_weight_gradient_workspace_bytes(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
   if (check_sizes(slots, experts, width, out_width) != GINEX_OK) return 0;
   Arena a(nullptr);
-  a.take<float>(tiling_of(slots, width, out_width).parts() * width * out_width);
+  a.take<float>(tiling_of(slots, experts, width, out_width).parts() * width * out_width);
   a.take<char>(256);
   return a.used;
 }
@@ -556,7 +558,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
     return fail(GINEX_ERR_ARG, "weight gradient: null or misaligned workspace (256 bytes)");
   if (ws_bytes < need) return fail(GINEX_ERR_WORKSPACE, "weight gradient: workspace %zu bytes, need %zu", ws_bytes, need);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const Tiling by = tiling_of(slots, kept->width, dy->width);
+  const Tiling by = tiling_of(slots, experts, kept->width, dy->width);
   const int32_t* const source = route ? route->source : nullptr;
   const int64_t* const offsets = route ? route->offsets : nullptr;
   float* const partial = static_cast<float*>(ws);
