@@ -47,7 +47,7 @@ struct Word<8> {
 template <typename T, int ACT>
 __global__ __launch_bounds__(THREADS) void k_compress(RowsOf<const T> x, RowsOf<T> y, int8_t* __restrict__ codes,
                                                       uint8_t* __restrict__ scales, int64_t first, uint32_t chunks,
-                                                      Divisor cpr, int32_t width) {
+                                                      Divisor cpr, Width width) {
   constexpr int N = Chunk<T>::N, LANES = GINEX_CODE_BLOCK / N;
   const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
   if (t >= chunks) return;            // (whole blocks: chunks is a multiple of LANES)
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(THREADS) void k_compress(RowsOf<const T> x, RowsOf<
   const int32_t c = (int32_t)at * N;
   const int64_t r = first + row;
   float v[N];
-  load_chunk(x.at(r, c), width - c, v);
+  load_chunk(x.at(r), c, width, v);
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -80,10 +80,10 @@ __global__ __launch_bounds__(THREADS) void k_compress(RowsOf<const T> x, RowsOf<
   const int64_t chunk = r * cpr.d + at;
   reinterpret_cast<typename Word<N>::type*>(codes)[chunk] = word;
   if (at % LANES == 0) scales[chunk / LANES] = (uint8_t)scale;
-  if (ACT != GINEX_ACT_NONE && c < width) {
+  if (ACT != GINEX_ACT_NONE && c < width.width) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = activated<ACT>(v[i]);
-    store_chunk(y.at(r, c), width - c, v);
+    store_chunk(y.at(r), c, width, v);
   }
 }
 
@@ -100,24 +100,24 @@ __device__ __forceinline__ void restored(const int8_t* __restrict__ codes, const
 template <typename T, int ACT>
 __global__ __launch_bounds__(THREADS) void k_restore(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                      RowsOf<const T> dy, RowsOf<T> out, int64_t first, uint32_t chunks,
-                                                     Divisor cpr, int32_t width) {
+                                                     Divisor cpr, Width width) {
   constexpr int N = Chunk<T>::N;
   const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
   if (t >= chunks) return;
   const uint32_t row = cpr.of(t);
   const uint32_t at = t - row * cpr.d;
   const int32_t c = (int32_t)at * N;
-  if (c >= width) return;
+  if (c >= width.width) return;
   const int64_t r = first + row;
   float v[N];
   restored<N>(codes, scales, r * cpr.d + at, v);
   if (ACT >= 0) {
     float g[N];
-    load_chunk(dy.at(r, c), width - c, g);
+    load_chunk(dy.at(r), c, width, g);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = sloped<ACT>(v[i], g[i]);
   }
-  store_chunk(out.at(r, c), width - c, v);
+  store_chunk(out.at(r), c, width, v);
 }
 
 // Calls go(first row, chunks, chunks of a row) for the launches that cover `rows` rows, chunks numbered in 31 bits.
@@ -142,11 +142,6 @@ int32_t check_kept(const char* what, const ginex_rows_t* r, const ginex_codes_t*
     return fail(GINEX_ERR_ARG, "%s is %lld x %lld, the codes %lld x %lld", what, (long long)r->rows, (long long)r->width,
                 (long long)kept->rows, (long long)kept->width);
   return GINEX_OK;
-}
-
-template <typename T>
-RowsOf<const T> read_rows(const ginex_rows_t* r) {
-  return {static_cast<const T*>(r->data), r->stride};
 }
 
 }  // namespace
@@ -176,7 +171,7 @@ extern "C" int32_t ginex_compress(const ginex_rows_t* x, int32_t activation, con
                                                        : k_compress<T, GINEX_ACT_GELU>;
     return by_launches<T>(x->rows, x->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, read_rows<T>(x), to,
-                         kept->codes, kept->scales, r, chunks, cpr, (int32_t)x->width);
+                         kept->codes, kept->scales, r, chunks, cpr, Width::of<T>(x->width));
     });
   });
 }
@@ -190,7 +185,7 @@ extern "C" int32_t ginex_restore(const ginex_codes_t* kept, const ginex_rows_t* 
     using T = decltype(t);
     return by_launches<T>(out->rows, out->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
       hipLaunchKernelGGL((k_restore<T, -1>), dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes,
-                         kept->scales, RowsOf<const T>{nullptr, 0}, rows_of<T>(out), r, chunks, cpr, (int32_t)out->width);
+                         kept->scales, RowsOf<const T>{nullptr, 0}, rows_of<T>(out), r, chunks, cpr, Width::of<T>(out->width));
     });
   });
 }
@@ -212,7 +207,7 @@ extern "C" int32_t ginex_activate_backward(const ginex_codes_t* kept, int32_t ac
                                                        : k_restore<T, GINEX_ACT_GELU>;
     return by_launches<T>(dy->rows, dy->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes, kept->scales,
-                         read_rows<T>(dy), rows_of<T>(dx), r, chunks, cpr, (int32_t)dx->width);
+                         read_rows<T>(dy), rows_of<T>(dx), r, chunks, cpr, Width::of<T>(dx->width));
     });
   });
 }

@@ -14,11 +14,9 @@ namespace ginex {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int CHOICES = 4;       // of a row, in flight together
-
 // Rows from offsets[experts] on are cleared, chunk by chunk, by all threads of the launch.
 template <typename T>
-__device__ __forceinline__ void clear_rest(RowsOf<T> out, int32_t width, Divisor cpr, const int64_t* __restrict__ end,
+__device__ __forceinline__ void clear_rest(RowsOf<T> out, Width width, Divisor cpr, const int64_t* __restrict__ end,
                                            int64_t slots, int64_t thread, int64_t threads) {
   constexpr int N = Chunk<T>::N;
   const float zero[N] = {};
@@ -26,16 +24,25 @@ __device__ __forceinline__ void clear_rest(RowsOf<T> out, int32_t width, Divisor
   kept = kept < 0 ? 0 : kept;
   for (int64_t s = kept * cpr.d + thread; s < slots * cpr.d; s += threads) {
     const int64_t row = s / cpr.d;
-    const int32_t c = (int32_t)(s - row * cpr.d) * N;
-    store_chunk(out.at(row, c), width - c, zero);
+    store_chunk(out.at(row), (int32_t)(s - row * cpr.d) * N, width, zero);
   }
 }
 
-// A thread moves one chunk of row `first + t / cpr` to the row's slots.
-template <typename T>
-__global__ __launch_bounds__(THREADS) void k_dispatch(RowsOf<T> x, RowsOf<T> out, const int32_t* __restrict__ slot,
+// The slots of K of a row's choices from j0 on, -1 where there is none.
+template <int K>
+__device__ __forceinline__ void slots_of_row(const int32_t* __restrict__ slot, int64_t r, int32_t j0, int32_t top,
+                                             int64_t slots, int32_t (&s)[K]) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) s[i] = slot[r * top + (j0 + i < top ? j0 + i : j0)];
+#pragma unroll
+  for (int i = 0; i < K; ++i) s[i] = j0 + i < top && s[i] < slots ? s[i] : -1;
+}
+
+// A thread moves one chunk of row `first + t / cpr` to the row's slots, K of them at a time.
+template <typename T, int K, bool KEEP>
+__global__ __launch_bounds__(THREADS) void k_dispatch(RowsOf<const T> x, RowsOf<T> out, const int32_t* __restrict__ slot,
                                                       const int64_t* __restrict__ end, int32_t top, int64_t first,
-                                                      uint32_t chunks, Divisor cpr, int32_t width, int64_t slots,
+                                                      uint32_t chunks, Divisor cpr, Width width, int64_t slots,
                                                       bool clear) {
   constexpr int N = Chunk<T>::N;
   const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
@@ -44,19 +51,23 @@ __global__ __launch_bounds__(THREADS) void k_dispatch(RowsOf<T> x, RowsOf<T> out
     const int32_t c = (int32_t)(t - row * cpr.d) * N;
     const int64_t r = first + row;
     float v[N];
-    load_chunk(x.at(r, c), width - c, v);
-    for (int j = 0; j < top; ++j) {
-      const int32_t s = slot[r * top + j];
-      if (s >= 0 && s < slots) store_chunk(out.at(s, c), width - c, v);
+    load_chunk(x.at(r), c, width, v);
+    for (int32_t j = 0; j < top; j += K) {
+      int32_t s[K];
+      slots_of_row<K>(slot, r, j, top, slots, s);
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (s[i] >= 0) store_chunk<KEEP>(out.at(s[i]), c, width, v);
     }
   }
   if (clear) clear_rest(out, width, cpr, end, slots, t, (int64_t)gridDim.x * THREADS);
 }
 
-template <typename T, bool WEIGHTED>
-__global__ __launch_bounds__(THREADS) void k_combine(RowsOf<T> z, RowsOf<T> y, const int32_t* __restrict__ slot,
+// K slots of a row are read together; a choice without a slot reads slot 0 and counts for nothing.
+template <typename T, bool WEIGHTED, int K>
+__global__ __launch_bounds__(THREADS) void k_combine(RowsOf<const T> z, RowsOf<T> y, const int32_t* __restrict__ slot,
                                                      const float* __restrict__ weights, int32_t top, int64_t first,
-                                                     uint32_t chunks, Divisor cpr, int32_t width, int64_t slots) {
+                                                     uint32_t chunks, Divisor cpr, Width width, int64_t slots) {
   constexpr int N = Chunk<T>::N;
   const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
   if (t >= chunks) return;
@@ -64,77 +75,101 @@ __global__ __launch_bounds__(THREADS) void k_combine(RowsOf<T> z, RowsOf<T> y, c
   const int32_t c = (int32_t)(t - row * cpr.d) * N;
   const int64_t r = first + row;
   float sum[N] = {};
-  for (int j0 = 0; j0 < top; j0 += CHOICES) {
-    float v[CHOICES][N], w[CHOICES];
+  for (int32_t j = 0; j < top; j += K) {
+    int32_t s[K];
+    float v[K][N], w[K];
+    slots_of_row<K>(slot, r, j, top, slots, s);
 #pragma unroll
-    for (int i = 0; i < CHOICES; ++i) {
-      const bool in = j0 + i < top;
-      const int32_t s = in ? slot[r * top + j0 + i] : -1;
-      const bool has = s >= 0 && s < slots;
-      w[i] = has ? (WEIGHTED ? weights[r * top + j0 + i] : 1.f) : 0.f;
-      if (has) {
-        load_chunk(z.at(s, c), width - c, v[i]);
-      } else {
-#pragma unroll
-        for (int n = 0; n < N; ++n) v[i][n] = 0.f;
-      }
+    for (int i = 0; i < K; ++i) {
+      w[i] = WEIGHTED ? weights[r * top + (j + i < top ? j + i : j)] : 1.f;
+      load_chunk(z.at(s[i] >= 0 ? s[i] : 0), c, width, v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < CHOICES; ++i)
+    for (int i = 0; i < K; ++i)
 #pragma unroll
-      for (int n = 0; n < N; ++n) sum[n] = WEIGHTED ? fmaf(w[i], v[i][n], sum[n]) : sum[n] + v[i][n];
+      for (int n = 0; n < N; ++n) {
+        const float next = WEIGHTED ? fmaf(w[i], v[i][n], sum[n]) : sum[n] + v[i][n];
+        sum[n] = s[i] >= 0 ? next : sum[n];
+      }
   }
-  store_chunk(y.at(r, c), width - c, sum);
+  store_chunk(y.at(r), c, width, sum);
 }
 
-// GROUP lanes share a row: they walk its chunks and add up their products at the end.
-template <typename T>
-__global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<T> dy, RowsOf<T> z, RowsOf<T> dz,
+// The sum of a group's lanes, in the last of them: lane by lane inside rows of 16 (DPP), then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float from_lane(float v) {
+  return __uint_as_float(dpp_or_zero<CTRL, ROWS>(__float_as_uint(v)));
+}
+__device__ __forceinline__ float sum_to_last(float v, int32_t group) {
+  if (group > 1) v += from_lane<0x111, 0xF>(v);     // row_shr:1
+  if (group > 2) v += from_lane<0x112, 0xF>(v);
+  if (group > 4) v += from_lane<0x114, 0xF>(v);
+  if (group > 8) v += from_lane<0x118, 0xF>(v);
+  if (group > 16) v += from_lane<0x142, 0xA>(v);    // row_bcast:15
+  if (group > 32) v += from_lane<0x143, 0xC>(v);    // row_bcast:31
+  return v;
+}
+
+// `group` lanes share a row: they walk its chunks and add up their products at the end.
+template <typename T, int K>
+__global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy, RowsOf<const T> z, RowsOf<T> dz,
                                                               const int32_t* __restrict__ slot,
                                                               const float* __restrict__ weights,
                                                               const int64_t* __restrict__ end,
                                                               float* __restrict__ dweights, int64_t rows, int32_t top,
-                                                              int32_t group, Divisor cpr, int32_t width, int64_t slots) {
+                                                              int32_t shift, Divisor cpr, Width width, int64_t slots) {
   constexpr int N = Chunk<T>::N;
   const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int64_t r = t / group;
+  const int32_t group = 1 << shift;
+  const bool has_row = t >> shift < rows;
+  const int64_t r = has_row ? t >> shift : rows - 1;       // (all lanes take part in the sums)
   const int lane = (int)(t & (group - 1));
-  if (r < rows) {
-    for (int j0 = 0; j0 < top; j0 += CHOICES) {
-      int32_t s[CHOICES];
-      float w[CHOICES], dot[CHOICES] = {};
+  for (int32_t j = 0; j < top; j += K) {
+    int32_t s[K];
+    float w[K], dot[K] = {};
+    slots_of_row<K>(slot, r, j, top, slots, s);
 #pragma unroll
-      for (int i = 0; i < CHOICES; ++i) {
-        s[i] = j0 + i < top ? slot[r * top + j0 + i] : -1;
-        s[i] = s[i] < slots ? s[i] : -1;
-        w[i] = s[i] >= 0 ? weights[r * top + j0 + i] : 0.f;
-      }
-      for (int32_t c = lane * N; c < width; c += group * N) {
-        float g[N];
-        load_chunk(dy.at(r, c), width - c, g);
+    for (int i = 0; i < K; ++i) w[i] = weights[r * top + (j + i < top ? j + i : j)];
+    for (int32_t c = lane * N; c < width.width; c += group * N) {
+      float g[N], v[K][N];
+      load_chunk(dy.at(r), c, width, g);
 #pragma unroll
-        for (int i = 0; i < CHOICES; ++i) {
-          if (s[i] < 0) continue;
-          float v[N];
-          load_chunk(z.at(s[i], c), width - c, v);
-          float scaled[N];
+      for (int i = 0; i < K; ++i) load_chunk(z.at(s[i] >= 0 ? s[i] : 0), c, width, v[i]);
 #pragma unroll
-          for (int n = 0; n < N; ++n) {
-            dot[i] = fmaf(g[n], v[n], dot[i]);
-            scaled[n] = w[i] * g[n];
-          }
-          store_chunk(dz.at(s[i], c), width - c, scaled);
+      for (int i = 0; i < K; ++i) {
+        if (s[i] < 0 || !has_row) continue;
+        float scaled[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          dot[i] = fmaf(g[n], v[i][n], dot[i]);
+          scaled[n] = w[i] * g[n];
         }
+        store_chunk(dz.at(s[i]), c, width, scaled);
       }
-      // (the lanes of a group are neighbours, and all of them are here: a group has one row)
+    }
 #pragma unroll
-      for (int i = 0; i < CHOICES; ++i) {
-        for (int step = group / 2; step > 0; step /= 2) dot[i] += __shfl_xor(dot[i], step, WAVE);
-        if (lane == 0 && j0 + i < top) dweights[r * top + j0 + i] = s[i] >= 0 ? dot[i] : 0.f;
-      }
+    for (int i = 0; i < K; ++i) {
+      const float sum = sum_to_last(dot[i], group);
+      if (has_row && lane == group - 1 && j + i < top) dweights[r * top + j + i] = s[i] >= 0 ? sum : 0.f;
     }
   }
   clear_rest(dz, width, cpr, end, slots, t, (int64_t)gridDim.x * THREADS);
+}
+
+// How many of a row's choices are in flight together.
+template <typename Go>
+int32_t with_choices(int32_t top, Go go) {
+  if (top == 1) return go(std::integral_constant<int, 1>{});
+  if (top == 2) return go(std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 4>{});
+}
+
+// Whether every row begins and ends with a line of 128 bytes.  Where lines are shared by the slots of different rows,
+// a dispatch stores through the caches, which put them together (41 017 x 8 slots of 1000 bytes: 123 -> 96 us); whole
+// lines go past them (177 000 x 2 slots of 512 bytes: 45 -> 41).
+bool whole_lines(const ginex_rows_t* r) {
+  const int64_t bytes = element_bytes(r->type);
+  return r->width * bytes % 128 == 0 && r->stride * bytes % 128 == 0 && reinterpret_cast<uintptr_t>(r->data) % 128 == 0;
 }
 
 // Rows of a launch: chunks are numbered in 31 bits.
@@ -167,16 +202,20 @@ extern "C" int32_t ginex_dispatch(const ginex_routing_t* route, const ginex_rows
   if (int32_t rc = check_slots("out", out, route)) return rc;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return with_type(x->type, [&](auto t) -> int32_t {
-    using T = decltype(t);
-    const int64_t cpr = ceil_div(x->width, Chunk<T>::N), step = rows_a_launch(cpr);
-    for (int64_t r = 0; r < x->rows; r += step) {
-      const int64_t chunks = (x->rows - r < step ? x->rows - r : step) * cpr;
-      hipLaunchKernelGGL(k_dispatch<T>, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, rows_of<T>(x),
-                         rows_of<T>(out), route->slot, route->offsets + route->experts, route->top, r, (uint32_t)chunks,
-                         Divisor((uint32_t)cpr), (int32_t)x->width, out->rows, r == 0);
-      GINEX_LAUNCH_CHECK();
-    }
-    return GINEX_OK;
+    return with_choices(route->top, [&](auto k) -> int32_t {
+      using T = decltype(t);
+      constexpr int K = decltype(k)::value;
+      const int64_t cpr = ceil_div(x->width, Chunk<T>::N), step = rows_a_launch(cpr);
+      for (int64_t r = 0; r < x->rows; r += step) {
+        const int64_t chunks = (x->rows - r < step ? x->rows - r : step) * cpr;
+        const auto kernel = whole_lines(out) ? k_dispatch<T, K, false> : k_dispatch<T, K, true>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st,
+                           read_rows<T>(x), rows_of<T>(out), route->slot, route->offsets + route->experts, route->top, r,
+                           (uint32_t)chunks, Divisor((uint32_t)cpr), Width::of<T>(x->width), out->rows, r == 0);
+        GINEX_LAUNCH_CHECK();
+      }
+      return GINEX_OK;
+    });
   });
 }
 
@@ -191,17 +230,20 @@ extern "C" int32_t ginex_combine(const ginex_routing_t* route, const ginex_rows_
   if (reinterpret_cast<uintptr_t>(weights) % 4) return fail(GINEX_ERR_ARG, "weights: misaligned");
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return with_type(y->type, [&](auto t) -> int32_t {
-    using T = decltype(t);
-    const int64_t cpr = ceil_div(y->width, Chunk<T>::N), step = rows_a_launch(cpr);
-    const auto kernel = weights ? k_combine<T, true> : k_combine<T, false>;
-    for (int64_t r = 0; r < y->rows; r += step) {
-      const int64_t chunks = (y->rows - r < step ? y->rows - r : step) * cpr;
-      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, rows_of<T>(z),
-                         rows_of<T>(y), route->slot, weights, route->top, r, (uint32_t)chunks, Divisor((uint32_t)cpr),
-                         (int32_t)y->width, z->rows);
-      GINEX_LAUNCH_CHECK();
-    }
-    return GINEX_OK;
+    return with_choices(route->top, [&](auto k) -> int32_t {
+      using T = decltype(t);
+      constexpr int K = decltype(k)::value;
+      const int64_t cpr = ceil_div(y->width, Chunk<T>::N), step = rows_a_launch(cpr);
+      const auto kernel = weights ? k_combine<T, true, K> : k_combine<T, false, K>;
+      for (int64_t r = 0; r < y->rows; r += step) {
+        const int64_t chunks = (y->rows - r < step ? y->rows - r : step) * cpr;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, read_rows<T>(z),
+                           rows_of<T>(y), route->slot, weights, route->top, r, (uint32_t)chunks, Divisor((uint32_t)cpr),
+                           Width::of<T>(y->width), z->rows);
+        GINEX_LAUNCH_CHECK();
+      }
+      return GINEX_OK;
+    });
   });
 }
 
@@ -222,15 +264,18 @@ extern "C" int32_t ginex_combine_backward(const ginex_routing_t* route, const gi
   if (route->rows == 0) return GINEX_OK;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return with_type(dy->type, [&](auto t) -> int32_t {
-    using T = decltype(t);
-    const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);
-    int32_t group = 1;
-    while (group < WAVE && group < cpr) group *= 2;
-    const int64_t blocks = ceil_div(dy->rows * group, THREADS);
-    hipLaunchKernelGGL(k_combine_backward<T>, dim3((unsigned)blocks), dim3(THREADS), 0, st, rows_of<T>(dy), rows_of<T>(z),
-                       rows_of<T>(dz), route->slot, weights, route->offsets + route->experts, dweights, dy->rows,
-                       route->top, group, Divisor((uint32_t)cpr), (int32_t)dy->width, dz->rows);
-    GINEX_LAUNCH_CHECK();
-    return GINEX_OK;
+    return with_choices(route->top, [&](auto k) -> int32_t {
+      using T = decltype(t);
+      constexpr int K = decltype(k)::value;
+      const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);
+      int32_t shift = 0;
+      while (1 << shift < WAVE && 1 << shift < cpr) ++shift;
+      const int64_t blocks = ceil_div(dy->rows << shift, THREADS);
+      hipLaunchKernelGGL((k_combine_backward<T, K>), dim3((unsigned)blocks), dim3(THREADS), 0, st, read_rows<T>(dy),
+                         read_rows<T>(z), rows_of<T>(dz), route->slot, weights, route->offsets + route->experts, dweights,
+                         dy->rows, route->top, shift, Divisor((uint32_t)cpr), Width::of<T>(dy->width), dz->rows);
+      GINEX_LAUNCH_CHECK();
+      return GINEX_OK;
+    });
   });
 }

@@ -11,7 +11,7 @@ using bf16 = __bf16;
 using f16 = _Float16;
 
 // Elements of 16 bytes.  The hardware reads and writes such a vector at any address of an element, so rows
-// of odd widths and strides take the same path as aligned ones and only a row's last elements go one by one.
+// of odd widths and strides take the same path as aligned ones.
 template <typename T>
 struct Chunk {
   static constexpr int N = 16 / sizeof(T);
@@ -19,34 +19,86 @@ struct Chunk {
   typedef Wide At __attribute__((aligned(sizeof(T))));
 };
 
-// The `left` (at most N) elements from p on, as f32; the others are 0.
-template <typename T>
-__device__ __forceinline__ void load_chunk(const T* p, int left, float (&v)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-  if (left >= N) {
-    const typename Chunk<T>::Wide w = *reinterpret_cast<const typename Chunk<T>::At*>(p);
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (float)w[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < left ? (float)p[i] : 0.f;
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+typedef words2 words2_at __attribute__((aligned(2)));
+typedef uint32_t word_at __attribute__((aligned(2)));
+
+// What a kernel knows about the rows' ends: the width, and how many elements the last chunk of a row has too few.
+struct Width {
+  int32_t width;
+  int32_t missing;
+  template <typename T>
+  static Width of(int64_t width) {
+    constexpr int N = Chunk<T>::N;
+    return {(int32_t)width, (int32_t)(ceil_div(width, N) * N - width)};
   }
+};
+
+// The chunk of the row that begins at `row` from column c on, a multiple of N, as f32; columns behind the width are 0.
+// The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
+// others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
+template <typename T>
+__device__ __forceinline__ void load_chunk(const T* row, int32_t c, Width w, float (&v)[Chunk<T>::N]) {
+  constexpr int N = Chunk<T>::N;
+  if (w.width < N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = c + i < w.width ? (float)row[c + i] : 0.f;
+    return;
+  }
+  const bool ends = c + N > w.width;
+  union {
+    typename Chunk<T>::Wide wide;
+    words4 words;
+  } u;
+  u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (ends ? w.width - N : c));
+  if (w.missing) {
+    words4 m = u.words;
+    const int bytes = w.missing * (int)sizeof(T);
+    if (bytes & 8) m = words4{m[2], m[3], 0, 0};
+    if (bytes & 4) m = words4{m[1], m[2], m[3], 0};
+    if (bytes & 2)
+      m = words4{__builtin_amdgcn_alignbit(m[1], m[0], 16), __builtin_amdgcn_alignbit(m[2], m[1], 16),
+                 __builtin_amdgcn_alignbit(m[3], m[2], 16), m[3] >> 16};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.words[i] = ends ? m[i] : u.words[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = c < w.width ? (float)u.wide[i] : 0.f;
 }
 
-// Rounded to nearest, halves to even; written past the caches that a later kernel would not find it in.
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* p, int left, const float (&v)[Chunk<T>::N]) {
+// Rounded to nearest, halves to even.  KEEP: through the caches, which put together lines that several rows share;
+// else past them.
+template <bool KEEP = false, typename T>
+__device__ __forceinline__ void store_chunk(T* row, int32_t c, Width w, const float (&v)[Chunk<T>::N]) {
   constexpr int N = Chunk<T>::N;
-  if (left >= N) {
-    typename Chunk<T>::Wide w;
+  union {
+    typename Chunk<T>::Wide wide;
+    words4 words;
+  } u;
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = (T)v[i];
-    __builtin_nontemporal_store(w, reinterpret_cast<typename Chunk<T>::At*>(p));
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < left) p[i] = (T)v[i];
+  for (int i = 0; i < N; ++i) u.wide[i] = (T)v[i];
+  T* p = row + c;
+  if (c + N <= w.width) {
+    if (KEEP) *reinterpret_cast<typename Chunk<T>::At*>(p) = u.wide;
+    else __builtin_nontemporal_store(u.wide, reinterpret_cast<typename Chunk<T>::At*>(p));
+    return;
   }
+  // 8, 4 and 2 bytes of what is left, the same for all rows
+  const int bytes = (w.width - c) * (int)sizeof(T);
+  words4 m = u.words;
+  if (bytes & 8) {
+    *reinterpret_cast<words2_at*>(p) = words2{m[0], m[1]};
+    p += 8 / sizeof(T);
+    m[0] = m[2];
+    m[1] = m[3];
+  }
+  if (bytes & 4) {
+    *reinterpret_cast<word_at*>(p) = m[0];
+    p += 4 / sizeof(T);
+    m[0] = m[1];
+  }
+  if (bytes & 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)m[0];
 }
 
 // n / d for n below 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers
@@ -64,12 +116,17 @@ template <typename T>
 struct RowsOf {
   T* data;
   int64_t stride;
-  __device__ __forceinline__ T* at(int64_t r, int64_t c) const { return data + r * stride + c; }
+  __device__ __forceinline__ T* at(int64_t r) const { return data + r * stride; }
 };
 
 template <typename T>
-inline RowsOf<T> rows_of(const ginex_rows_t* r, int64_t first = 0) {
-  return {static_cast<T*>(r->data) + first * r->stride, r->stride};
+inline RowsOf<T> rows_of(const ginex_rows_t* r) {
+  return {static_cast<T*>(r->data), r->stride};
+}
+
+template <typename T>
+inline RowsOf<const T> read_rows(const ginex_rows_t* r) {
+  return {static_cast<const T*>(r->data), r->stride};
 }
 
 inline int element_bytes(int32_t type) { return type == GINEX_F32 ? 4 : 2; }

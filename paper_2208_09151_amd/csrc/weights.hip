@@ -19,7 +19,6 @@ constexpr int PAD = 32;           // elements behind a row in LDS, see k_weights
 typedef short half_words __attribute__((ext_vector_type(4)));
 typedef bf16 fragment __attribute__((ext_vector_type(8)));
 typedef float tile __attribute__((ext_vector_type(16)));
-typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 
 // A gradient as a sum of bf16 numbers, exactly: the significand's bits eight at a time (bf16 has 8, f16 11, f32 24).
 template <typename T>
@@ -570,7 +569,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
                                                   (long long)kept->width, (long long)dy->width);
     hipLaunchKernelGGL(kernel_of<T>(by, dy->width), dim3((unsigned)groups), dim3((unsigned)(by.wm * by.wn * WAVE)), 0, st,
                        kept->codes, kept->scales, kept->rows, (int32_t)code_blocks(kept->width), source, offsets, experts,
-                       slots, by.ranges, RowsOf<const T>{static_cast<const T*>(dy->data), dy->stride}, (int32_t)kept->width,
+                       slots, by.ranges, read_rows<T>(dy), (int32_t)kept->width,
                        (int32_t)dy->width, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
     GINEX_LAUNCH_CHECK();
     hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(size, 4 * JOIN_THREADS), (unsigned)experts), dim3(JOIN_THREADS), 0,
