@@ -293,14 +293,13 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
       for (int i = 0; i < XN; ++i) {
         const int q = threadIdx.x + i * THREADS;
         if (XS < THREADS && q >= XS) break;
-        const float step = there[P][i] && q / (TM / 16) <= left ? code_step(scale[P][i]) : 0.f, below = -128.f * step;
+        const float step = there[P][i] && q / (TM / 16) <= left ? code_step(scale[P][i]) : 0.f;
         words4 out[2];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          // q step = (q + 128) step - 128 step, exactly: a byte becomes a float in one instruction if it has no sign
-          const uint32_t word = x[P][i][w] ^ 0x80808080u;
-          const float f0 = fmaf((float)(word & 255), step, below), f1 = fmaf((float)(word >> 8 & 255), step, below);
-          const float f2 = fmaf((float)(word >> 16 & 255), step, below), f3 = fmaf((float)(word >> 24), step, below);
+          const uint32_t word = x[P][i][w];
+          const float f0 = (float)(int8_t)word * step, f1 = (float)(int8_t)(word >> 8) * step;
+          const float f2 = (float)(int8_t)(word >> 16) * step, f3 = (float)((int32_t)word >> 24) * step;
           out[w / 2][w % 2 * 2] = upper_halves(f0, f1);
           out[w / 2][w % 2 * 2 + 1] = upper_halves(f2, f3);
         }

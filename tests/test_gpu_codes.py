@@ -326,6 +326,18 @@ def test_weight_gradient_of_large_and_small_numbers(g):
     assert ((got - want).abs() <= 64 * 2.0 ** -24 * want.abs()).all()
 
 
+def test_weight_gradient_of_the_largest_and_smallest_blocks(g):
+    """Blocks whose largest magnitude is 2^127 and more, or below 2^-120."""
+    x = torch.zeros((40, 64))
+    x[3, :32] = torch.linspace(-1, 1, 32) * 3.3e38
+    x[5, 32:] = torch.linspace(-1, 1, 32) * 2.0 ** -121
+    dy = torch.zeros((40, 9))
+    dy[3, 0], dy[5, 1], dy[5, 2] = 1.0, 1.0, 2.0 ** 30
+    got = g.weight_gradient(g.compress(x.cuda()), dy.cuda()).cpu().double()
+    want = plain_codes(x)[2].t() @ dy.double()
+    assert torch.equal(got, want)               # one product each: exact
+
+
 def test_weight_gradient_against_differences(g):
     """<dy, x W> is linear in W: differences of it over steps of 1 are off by 1e-4 of their terms at most
     (sums of 500 * 30 products in f32 on one side, f64 on the other)."""
