@@ -11,6 +11,9 @@ namespace ginex {
 namespace {
 
 constexpr int THREADS = 256;
+// Chunks of a thread, their loads issued together (compress, 820 000 x 256 f32: 179 us with one, 175 with two, 174 with four;
+// silu 313, 309 and 322; 300 000 x 333 f16: 57, 49 and 49, silu's gradient 90, 83 and 87).
+constexpr int UNROLL = 2;
 
 // exp and 1/x: the library's and the division for f32; for results of 8 or 11 bits the instructions (1 unit each, and
 // exp's argument is rounded once more: off by |x| 2^-24), without which 16-bit rows are bound by the vector unit.
@@ -98,47 +101,67 @@ __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d
   return ab | cd;
 }
 
+// The largest of the 4 or 8 neighbouring lanes that share a block, in all of them.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+  const uint32_t other = dpp_or_zero<CTRL, 0xF>(v);
+  return v > other ? v : other;
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t max_of_block(uint32_t v) {
+  v = max_with<0xB1>(v);                        // quad_perm [1, 0, 3, 2]
+  v = max_with<0x4E>(v);                        // quad_perm [2, 3, 0, 1]
+  return LANES == 8 ? max_with<0x141>(v) : v;   // row_half_mirror: the other four of eight
+}
+
 template <typename T, int ACT>
 __global__ __launch_bounds__(THREADS) void k_compress(RowsOf<const T> x, RowsOf<T> y, int8_t* __restrict__ codes,
                                                       uint8_t* __restrict__ scales, int64_t first, uint32_t chunks,
                                                       Divisor cpr, Width width) {
-  constexpr int N = Chunk<T>::N, LANES = GINEX_CODE_BLOCK / N;
-  const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
-  if (t >= chunks) return;            // (whole blocks: chunks is a multiple of LANES)
-  const uint32_t row = cpr.of(t);
-  const uint32_t at = t - row * cpr.d;
-  const int32_t c = (int32_t)at * N;
-  const int64_t r = first + row;
-  float v[N];
-  load_chunk(x.at(r), c, width, v);
-  uint32_t top = 0;
+  constexpr int N = Chunk<T>::N, LANES = GINEX_CODE_BLOCK / N, U = UNROLL;
+  uint32_t at[U];
+  int64_t r[U];
+  float v[U][N];
+  // (a chunk behind the last one repeats it and is not written: all lanes of a block do the same, as chunks is a multiple of
+  // LANES)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t magnitude = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-    top = top > magnitude ? top : magnitude;
+  for (int u = 0; u < U; ++u) {
+    uint32_t t = (blockIdx.x * U + u) * THREADS + threadIdx.x;
+    t = t < chunks ? t : chunks - LANES + t % LANES;
+    const uint32_t row = cpr.of(t);
+    at[u] = t - row * cpr.d;
+    r[u] = first + row;
   }
 #pragma unroll
-  for (int step = 1; step < LANES; step *= 2) {
-    const uint32_t other = __shfl_xor(top, step, WAVE);
-    top = top > other ? top : other;
-  }
-  const uint32_t scale = scale_byte(top);
-  const float by = to_codes(scale);
-  // v by + 1.5 2^23 is rounded to a whole number, halves to even, and has it in its lowest bits
-  constexpr float whole = 12582912.f;
-  float q[N];
+  for (int u = 0; u < U; ++u) load_chunk(x.at(r[u]), (int32_t)at[u] * N, width, v[u]);
 #pragma unroll
-  for (int i = 0; i < N; ++i) q[i] = __builtin_amdgcn_fmed3f(fmaf(v[i], by, whole), whole - 127.f, whole + 127.f);
-  typename Word<N>::type word = low_bytes(q[0], q[1], q[2], q[3]);
-  if constexpr (N == 8) word |= (uint64_t)low_bytes(q[4], q[5], q[6], q[7]) << 32;
-  word = scale == NO_NUMBER ? 0 : word;
-  const int64_t chunk = r * cpr.d + at;
-  reinterpret_cast<typename Word<N>::type*>(codes)[chunk] = word;
-  if (at % LANES == 0) scales[chunk / LANES] = (uint8_t)scale;
-  if (ACT != GINEX_ACT_NONE && c < width.width) {
+  for (int u = 0; u < U; ++u) {
+    if ((blockIdx.x * U + u) * THREADS + threadIdx.x >= chunks) return;
+    const int32_t c = (int32_t)at[u] * N;
+    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = activated<ACT, sizeof(T) == 4>(v[i]);
-    store_chunk(y.at(r), c, width, v);
+    for (int i = 0; i < N; ++i) {
+      const uint32_t magnitude = __float_as_uint(v[u][i]) & 0x7FFFFFFFu;
+      top = top > magnitude ? top : magnitude;
+    }
+    const uint32_t scale = scale_byte(max_of_block<LANES>(top));
+    const float by = to_codes(scale);
+    // v by + 1.5 2^23 is rounded to a whole number, halves to even, and has it in its lowest bits
+    constexpr float whole = 12582912.f;
+    float q[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i] = __builtin_amdgcn_fmed3f(fmaf(v[u][i], by, whole), whole - 127.f, whole + 127.f);
+    typename Word<N>::type word = low_bytes(q[0], q[1], q[2], q[3]);
+    if constexpr (N == 8) word |= (uint64_t)low_bytes(q[4], q[5], q[6], q[7]) << 32;
+    word = scale == NO_NUMBER ? 0 : word;
+    const int64_t chunk = r[u] * cpr.d + at[u];
+    __builtin_nontemporal_store(word, reinterpret_cast<typename Word<N>::type*>(codes) + chunk);
+    if (at[u] % LANES == 0) scales[chunk / LANES] = (uint8_t)scale;
+    if (ACT != GINEX_ACT_NONE && c < width.width) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[u][i] = activated<ACT, sizeof(T) == 4>(v[u][i]);
+      store_chunk(y.at(r[u]), c, width, v[u]);
+    }
   }
 }
 
@@ -156,30 +179,40 @@ template <typename T, int ACT>
 __global__ __launch_bounds__(THREADS) void k_restore(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                      RowsOf<const T> dy, RowsOf<T> out, int64_t first, uint32_t chunks,
                                                      Divisor cpr, Width width) {
-  constexpr int N = Chunk<T>::N;
-  const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
-  if (t >= chunks) return;
-  const uint32_t row = cpr.of(t);
-  const uint32_t at = t - row * cpr.d;
-  const int32_t c = (int32_t)at * N;
-  if (c >= width.width) return;
-  const int64_t r = first + row;
-  float v[N];
-  restored<N>(codes, scales, r * cpr.d + at, v);
-  if (ACT >= 0) {
-    float g[N];
-    load_chunk(dy.at(r), c, width, g);
+  constexpr int N = Chunk<T>::N, U = UNROLL;
+  int32_t c[U];
+  int64_t r[U];
+  float v[U][N], g[U][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = sloped<ACT, sizeof(T) == 4>(v[i], g[i]);
+  for (int u = 0; u < U; ++u) {
+    uint32_t t = (blockIdx.x * U + u) * THREADS + threadIdx.x;
+    t = t < chunks ? t : chunks - 1;
+    const uint32_t row = cpr.of(t);
+    c[u] = (int32_t)(t - row * cpr.d) * N;
+    r[u] = first + row;
   }
-  store_chunk(out.at(r), c, width, v);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    restored<N>(codes, scales, r[u] * cpr.d + c[u] / N, v[u]);
+    if (ACT >= 0) load_chunk(dy.at(r[u]), c[u], width, g[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if ((blockIdx.x * U + u) * THREADS + threadIdx.x >= chunks) return;
+    if (c[u] >= width.width) continue;
+    if (ACT >= 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[u][i] = sloped<ACT, sizeof(T) == 4>(v[u][i], g[u][i]);
+    }
+    store_chunk(out.at(r[u]), c[u], width, v[u]);
+  }
 }
 
 // Calls go(first row, chunks, chunks of a row) for the launches that cover `rows` rows, chunks numbered in 31 bits.
 template <typename T, typename Go>
 int32_t by_launches(int64_t rows, int64_t width, Go go) {
   const int64_t cpr = code_blocks(width) * (GINEX_CODE_BLOCK / Chunk<T>::N);
-  const int64_t step = (((int64_t)1 << 31) - THREADS) / cpr;
+  const int64_t step = (((int64_t)1 << 31) - THREADS * UNROLL) / cpr;
   for (int64_t r = 0; r < rows; r += step) {
     go(r, (uint32_t)((rows - r < step ? rows - r : step) * cpr), Divisor((uint32_t)cpr));
     GINEX_LAUNCH_CHECK();
@@ -225,7 +258,7 @@ extern "C" int32_t ginex_compress(const ginex_rows_t* x, int32_t activation, con
                         : activation == GINEX_ACT_SILU ? k_compress<T, GINEX_ACT_SILU>
                                                        : k_compress<T, GINEX_ACT_GELU>;
     return by_launches<T>(x->rows, x->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, read_rows<T>(x), to,
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS * UNROLL)), dim3(THREADS), 0, st, read_rows<T>(x), to,
                          kept->codes, kept->scales, r, chunks, cpr, Width::of<T>(x->width));
     });
   });
@@ -239,7 +272,7 @@ extern "C" int32_t ginex_restore(const ginex_codes_t* kept, const ginex_rows_t* 
   return with_type(out->type, [&](auto t) -> int32_t {
     using T = decltype(t);
     return by_launches<T>(out->rows, out->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
-      hipLaunchKernelGGL((k_restore<T, -1>), dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes,
+      hipLaunchKernelGGL((k_restore<T, -1>), dim3((unsigned)ceil_div(chunks, THREADS * UNROLL)), dim3(THREADS), 0, st, kept->codes,
                          kept->scales, RowsOf<const T>{nullptr, 0}, rows_of<T>(out), r, chunks, cpr, Width::of<T>(out->width));
     });
   });
@@ -261,7 +294,7 @@ extern "C" int32_t ginex_activate_backward(const ginex_codes_t* kept, int32_t ac
                         : activation == GINEX_ACT_SILU ? k_restore<T, GINEX_ACT_SILU>
                                                        : k_restore<T, GINEX_ACT_GELU>;
     return by_launches<T>(dy->rows, dy->width, [&](int64_t r, uint32_t chunks, Divisor cpr) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st, kept->codes, kept->scales,
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS * UNROLL)), dim3(THREADS), 0, st, kept->codes, kept->scales,
                          read_rows<T>(dy), rows_of<T>(dx), r, chunks, cpr, Width::of<T>(dx->width));
     });
   });
