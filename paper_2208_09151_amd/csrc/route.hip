@@ -2,91 +2,120 @@
 //
 //   slot(p) = offset(e(p)) + #{q < p : e(q) = e(p)},  offset(e) = sum over e' < e of min(count(e'), capacity)
 //
-// A wave owns a run of consecutive pairs, 64 at a time.  Lanes of the same expert find each other by
-// ballots over the bits of the expert's number, so a pair's rank among them is a popcount, and the run's
-// count of the expert so far (in LDS, a row of counters per wave) gives the rest: no atomic decides a
-// place, and equal inputs give equal slots.
+// A wave owns a run of consecutive pairs, 64 at a time, all of them in registers.  Lanes of the same expert
+// find each other by ballots over the bits of the expert's number, so a pair's rank among them is a
+// popcount, and the run's count of the expert so far (in LDS, a row of counters per wave) gives the rest:
+// no atomic decides a place, and equal inputs give equal slots.
+//
+// Bound by launches: up to 8192 pairs one workgroup in one launch (128 pairs 2.3 us), else the tiles'
+// counts and the places, in which every workgroup adds up the counts of the tiles itself; with a scan
+// between them, five launches, 1.64 M pairs took 35 us and 152 000 20.
 #include "primitives.hpp"
 #include "train.hpp"
 
 namespace ginex {
 namespace {
 
-constexpr int TILE_THREADS = 256;
-constexpr int TILE_WAVES = TILE_THREADS / WAVE;
-constexpr int RUN = 1024;                       // pairs of a wave
-constexpr int TILE = TILE_WAVES * RUN;
-constexpr int ONE_THREADS = 512;
-constexpr int ONE_WAVES = ONE_THREADS / WAVE;
-// Up to here one workgroup does it all in one launch.
-constexpr int64_t ONE_PAIRS = 8192;
+constexpr int WAVES = 8;
+constexpr int THREADS = WAVES * WAVE;
+constexpr int TILE_KEYS = 8;                    // pairs of a lane
+constexpr int ONE = THREADS * 16;               // up to here one workgroup does it all in one launch
+constexpr int TILE = THREADS * TILE_KEYS;
+// Up to here the tiles' counts are added up by every workgroup (reads that grow with the square of the
+// tiles: with 512 of them and 256 experts 270 MB of L2), beyond it they are scanned.
+constexpr int64_t MOST_TILES = 1024;
 
-// The expert of pair p, or `experts` for none.
-template <typename Key>
-__device__ __forceinline__ uint32_t expert_of(const Key* __restrict__ chosen, int64_t p, int64_t end, uint32_t experts) {
-  if (p >= end) return experts;
-  const Key e = chosen[p];
-  return e >= 0 && e < (Key)experts ? (uint32_t)e : experts;
-}
-
-// The lanes whose value is this lane's.
-__device__ __forceinline__ uint64_t same_lanes(uint32_t value, int bits) {
-  uint64_t same = ~(uint64_t)0;
-  for (int b = 0; b < bits; ++b) {
-    const bool set = (value >> b) & 1;
-    const uint64_t lanes = __ballot(set);
-    same &= set ? lanes : ~lanes;
+// A lane's pair: its expert (`experts` for none), its rank among the lanes with the same one, and how many they are.
+struct Place {
+  uint32_t packed;
+  __device__ __forceinline__ Place(uint32_t expert, uint64_t same) {
+    const uint64_t below = ((uint64_t)1 << lane_id()) - 1;
+    packed = expert | (uint32_t)__popcll(same & below) << 16 | (uint32_t)__popcll(same) << 24;
   }
-  return same;
-}
+  Place() = default;
+  __device__ __forceinline__ uint32_t expert() const { return packed & 0xFFFF; }
+  __device__ __forceinline__ uint32_t rank() const { return packed >> 16 & 0xFF; }
+  __device__ __forceinline__ uint32_t lanes() const { return packed >> 24; }
+};
 
-template <typename Key>
-__device__ __forceinline__ void count_run(const Key* __restrict__ chosen, int64_t first, int64_t last, int64_t end,
-                                          uint32_t experts, uint32_t* counts) {
-  for (int64_t p = first + lane_id(); p < last; p += WAVE) atomicAdd(&counts[expert_of(chosen, p, end, experts)], 1u);
-}
-
-// Places the pairs of a run.  ranks[e]: pairs of expert e in front of the run; starts[e]: its first slot.
-template <typename Key>
-__device__ __forceinline__ void place_run(const Key* __restrict__ chosen, int64_t first, int64_t last, int64_t end,
-                                          uint32_t experts, int bits, uint32_t capacity, Divisor top,
-                                          uint32_t* ranks, const uint32_t* starts, int32_t* __restrict__ slot,
-                                          int32_t* __restrict__ source) {
-  const uint64_t below = ((uint64_t)1 << lane_id()) - 1;
-  for (int64_t at = first; at < last; at += WAVE) {
-    const int64_t p = at + lane_id();
-    const uint32_t e = expert_of(chosen, p, end, experts);
-    const uint64_t same = same_lanes(e, bits);
-    const uint32_t before = ranks[e];
-    __builtin_amdgcn_wave_barrier();
-    if ((same & below) == 0) ranks[e] = before + (uint32_t)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
-    if (p < end) {
-      const uint32_t rank = before + (uint32_t)__popcll(same & below);
-      const bool kept = e < experts && rank < capacity;
-      const int32_t s = kept ? (int32_t)(starts[e] + rank) : -1;
-      slot[p] = s;
-      if (kept) source[s] = (int32_t)top.of((uint32_t)p);
+// Reads a wave's run and counts it: counts [experts + 1] of this wave, zero before.  The rounds of 64 go through the bits
+// together, and nothing waits for LDS: one round after the other took three times as long.
+template <typename Key, int KEYS>
+__device__ __forceinline__ void count_run(const Key* __restrict__ chosen, int64_t first, int64_t pairs, uint32_t experts,
+                                          int bits, uint32_t* counts, Place (&places)[KEYS]) {
+  Key e[KEYS];
+  uint64_t same[KEYS];
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    const int64_t p = first + i * WAVE + lane_id();
+    e[i] = p < pairs ? chosen[p] : (Key)-1;
+  }
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    e[i] = e[i] >= 0 && e[i] < (Key)experts ? e[i] : (Key)experts;
+    same[i] = ~(uint64_t)0;
+  }
+  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+      const bool set = ((uint32_t)e[i] >> b) & 1;
+      const uint64_t lanes = __ballot(set);
+      same[i] &= set ? lanes : ~lanes;
     }
   }
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    places[i] = Place((uint32_t)e[i], same[i]);
+    if (places[i].rank() == 0) atomicAdd(&counts[(uint32_t)e[i]], places[i].lanes());
+  }
 }
 
-// From counts[w][e] of W runs: counts[w][e] becomes the pairs of e in front of run w, starts[e] its first slot;
-// returns the number of slots.
-template <int THREADS, int W>
-__device__ __forceinline__ uint32_t runs_to_ranks(uint32_t* counts, uint32_t* starts, uint32_t experts,
-                                                  uint32_t capacity, uint32_t* smem) {
+// ranks[e]: pairs of expert e in front of the run; starts[e]: its first slot.  A wave's LDS accesses are carried out in
+// their order, so a round reads what the rounds before it have added without waiting for them.
+template <int KEYS>
+__device__ __forceinline__ void place_run(const Place (&places)[KEYS], int64_t first, int64_t pairs, uint32_t experts,
+                                          uint32_t capacity, Divisor top, uint32_t* ranks, const uint32_t* starts,
+                                          int32_t* __restrict__ slot, int32_t* __restrict__ source) {
+  uint32_t before[KEYS], start[KEYS];
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    before[i] = ranks[places[i].expert()];
+    __builtin_amdgcn_wave_barrier();
+    if (places[i].rank() == 0) atomicAdd(&ranks[places[i].expert()], places[i].lanes());
+    __builtin_amdgcn_wave_barrier();
+  }
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) start[i] = starts[places[i].expert() < experts ? places[i].expert() : 0];
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    const int64_t p = first + i * WAVE + lane_id();
+    if (p >= pairs) break;
+    const uint32_t rank = before[i] + places[i].rank();
+    const bool kept = places[i].expert() < experts && rank < capacity;
+    const int32_t s = kept ? (int32_t)(start[i] + rank) : -1;
+    slot[p] = s;
+    if (kept) source[s] = (int32_t)top.of((uint32_t)p);
+  }
+}
+
+// From counts[w][e] of the waves' runs, the pairs of e in front of them and those of e in all: counts[w][e] becomes the
+// pairs of e in front of run w, starts[e] its first slot; returns the number of slots.
+template <typename InFront, typename All>
+__device__ __forceinline__ uint32_t runs_to_ranks(uint32_t* counts, uint32_t* starts, uint32_t experts, uint32_t capacity,
+                                                  uint32_t* smem, InFront in_front, All all) {
   uint32_t done = 0;
   for (uint32_t e0 = 0; e0 < experts; e0 += THREADS) {
     const uint32_t e = e0 + threadIdx.x;
     uint32_t sum = 0;
     if (e < experts) {
+      uint32_t rank = in_front(e);
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         const uint32_t n = counts[w * (experts + 1) + e];
-        counts[w * (experts + 1) + e] = sum;
-        sum += n;
+        counts[w * (experts + 1) + e] = rank;
+        rank += n;
       }
+      sum = all(e, rank);
     }
     uint32_t total;
     const uint32_t first = block_exclusive_scan<uint32_t, THREADS>(sum < capacity ? sum : capacity, smem, total);
@@ -96,93 +125,105 @@ __device__ __forceinline__ uint32_t runs_to_ranks(uint32_t* counts, uint32_t* st
   return done;
 }
 
-template <typename Key>
-__global__ __launch_bounds__(ONE_THREADS) void k_route_one(const Key* __restrict__ chosen, int64_t pairs, uint32_t experts,
-                                                           int bits, uint32_t capacity, Divisor top,
-                                                           int64_t* __restrict__ offsets, int32_t* __restrict__ slot,
-                                                           int32_t* __restrict__ source) {
+template <typename Key, int KEYS>
+__global__ __launch_bounds__(THREADS) void k_route_one(const Key* __restrict__ chosen, int64_t pairs, uint32_t experts,
+                                                       int bits, uint32_t capacity, Divisor top,
+                                                       int64_t* __restrict__ offsets, int32_t* __restrict__ slot,
+                                                       int32_t* __restrict__ source) {
   extern __shared__ uint32_t dynamic[];
-  __shared__ uint32_t smem[ONE_WAVES + 1];
-  uint32_t* const counts = dynamic;                                  // [ONE_WAVES][experts + 1]
-  uint32_t* const starts = dynamic + ONE_WAVES * (experts + 1);      // [experts]
-  for (uint32_t i = threadIdx.x; i < ONE_WAVES * (experts + 1); i += ONE_THREADS) counts[i] = 0;
+  __shared__ uint32_t smem[WAVES + 1];
+  uint32_t* const counts = dynamic;                              // [WAVES][experts + 1]
+  uint32_t* const starts = dynamic + WAVES * (experts + 1);      // [experts]
+  for (uint32_t i = threadIdx.x; i < WAVES * (experts + 1); i += THREADS) counts[i] = 0;
   __syncthreads();
   const int w = threadIdx.x / WAVE;
-  const int64_t run = (pairs + ONE_THREADS - 1) / ONE_THREADS * WAVE;
+  // (as even runs as whole rounds of 64 allow)
+  const int64_t run = (pairs + THREADS - 1) / THREADS * WAVE;
   const int64_t first = w * run, last = first + run < pairs ? first + run : pairs;
   uint32_t* const mine = counts + w * (experts + 1);
-  count_run(chosen, first, last, pairs, experts, mine);
+  Place places[KEYS];
+  count_run(chosen, first, last, experts, bits, mine, places);
   __syncthreads();
-  const uint32_t kept = runs_to_ranks<ONE_THREADS, ONE_WAVES>(counts, starts, experts, capacity, smem);
+  const uint32_t kept = runs_to_ranks(counts, starts, experts, capacity, smem, [](uint32_t) { return 0u; },
+                                      [](uint32_t, uint32_t sum) { return sum; });
   __syncthreads();
-  place_run(chosen, first, last, pairs, experts, bits, capacity, top, mine, starts, slot, source);
-  for (uint32_t e = threadIdx.x; e < experts; e += ONE_THREADS) offsets[e] = starts[e];
+  place_run(places, first, last, experts, capacity, top, mine, starts, slot, source);
+  for (uint32_t e = threadIdx.x; e < experts; e += THREADS) offsets[e] = starts[e];
   if (threadIdx.x == 0) offsets[experts] = kept;
-  for (int64_t s = kept + threadIdx.x; s < pairs; s += ONE_THREADS) source[s] = -1;
+  for (int64_t s = kept + threadIdx.x; s < pairs; s += THREADS) source[s] = -1;
 }
 
-template <typename Key>
-__global__ __launch_bounds__(TILE_THREADS) void k_route_count(const Key* __restrict__ chosen, int64_t pairs,
-                                                              uint32_t experts, uint32_t* __restrict__ hist) {
+// hist: [tiles][experts + 1], or (SCANNED) [experts + 1][tiles].
+template <typename Key, bool SCANNED>
+__global__ __launch_bounds__(THREADS) void k_route_count(const Key* __restrict__ chosen, int64_t pairs, uint32_t experts,
+                                                         uint32_t* __restrict__ hist) {
   extern __shared__ uint32_t counts[];     // [experts + 1]
-  for (uint32_t e = threadIdx.x; e <= experts; e += TILE_THREADS) counts[e] = 0;
+  for (uint32_t e = threadIdx.x; e <= experts; e += THREADS) counts[e] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * TILE;
-  const int64_t last = first + TILE < pairs ? first + TILE : pairs;
-  for (int64_t p = first + threadIdx.x; p < last; p += TILE_THREADS)
-    atomicAdd(&counts[expert_of(chosen, p, pairs, experts)], 1u);
+  Key e[TILE_KEYS];
+#pragma unroll
+  for (int i = 0; i < TILE_KEYS; ++i) {
+    const int64_t p = (int64_t)blockIdx.x * TILE + i * THREADS + threadIdx.x;
+    e[i] = p < pairs ? chosen[p] : (Key)-1;
+  }
+#pragma unroll
+  for (int i = 0; i < TILE_KEYS; ++i) atomicAdd(&counts[e[i] >= 0 && e[i] < (Key)experts ? (uint32_t)e[i] : experts], 1u);
   __syncthreads();
-  for (uint32_t e = threadIdx.x; e <= experts; e += TILE_THREADS) hist[(int64_t)e * gridDim.x + blockIdx.x] = counts[e];
+  for (uint32_t e = threadIdx.x; e <= experts; e += THREADS)
+    hist[SCANNED ? (int64_t)e * gridDim.x + blockIdx.x : (int64_t)blockIdx.x * (experts + 1) + e] = counts[e];
 }
 
-// hist: scanned, expert after expert, tile after tile.
-template <typename Key>
-__global__ __launch_bounds__(TILE_THREADS) void k_route_place(const Key* __restrict__ chosen, int64_t pairs,
-                                                              uint32_t experts, int bits, uint32_t capacity, Divisor top,
-                                                              const uint32_t* __restrict__ hist,
-                                                              int64_t* __restrict__ offsets, int32_t* __restrict__ slot,
-                                                              int32_t* __restrict__ source) {
+template <typename Key, bool SCANNED>
+__global__ __launch_bounds__(THREADS) void k_route_place(const Key* __restrict__ chosen, int64_t pairs, uint32_t experts,
+                                                         int bits, uint32_t capacity, Divisor top,
+                                                         const uint32_t* __restrict__ hist, int64_t* __restrict__ offsets,
+                                                         int32_t* __restrict__ slot, int32_t* __restrict__ source) {
   extern __shared__ uint32_t dynamic[];
-  __shared__ uint32_t smem[TILE_WAVES + 1];
-  uint32_t* const counts = dynamic;                                   // [TILE_WAVES][experts + 1]
-  uint32_t* const starts = dynamic + TILE_WAVES * (experts + 1);      // [experts]
-  for (uint32_t i = threadIdx.x; i < TILE_WAVES * (experts + 1); i += TILE_THREADS) counts[i] = 0;
+  __shared__ uint32_t smem[WAVES + 1];
+  uint32_t* const counts = dynamic;                              // [WAVES][experts + 1]
+  uint32_t* const starts = counts + WAVES * (experts + 1);       // [experts]
+  uint32_t* const in_front = starts + experts;                   // [experts], of the tiles in front of this one
+  uint32_t* const all = in_front + experts;                      // [experts]
+  for (uint32_t i = threadIdx.x; i < (WAVES + 3) * (experts + 1) - 3; i += THREADS) counts[i] = 0;
   __syncthreads();
   const int w = threadIdx.x / WAVE;
-  const int64_t tiles = gridDim.x;
-  const int64_t first = (int64_t)blockIdx.x * TILE + w * RUN;
-  const int64_t last = first + RUN < pairs ? first + RUN : pairs;
+  const int64_t tiles = gridDim.x, first = (int64_t)blockIdx.x * TILE + w * (TILE / WAVES);
   uint32_t* const mine = counts + w * (experts + 1);
-  count_run(chosen, first, last, pairs, experts, mine);
-  __syncthreads();
-  uint32_t kept = 0;
-  for (uint32_t e0 = 0; e0 < experts; e0 += TILE_THREADS) {
-    const uint32_t e = e0 + threadIdx.x;
-    uint32_t all = 0;
-    if (e < experts) {
-      const uint32_t begin = hist[e * tiles];
-      all = hist[(e + 1) * tiles] - begin;
-      uint32_t rank = hist[e * tiles + blockIdx.x] - begin;
-#pragma unroll
-      for (int v = 0; v < TILE_WAVES; ++v) {
-        const uint32_t n = counts[v * (experts + 1) + e];
-        counts[v * (experts + 1) + e] = rank;
-        rank += n;
+  Place places[TILE_KEYS];
+  count_run(chosen, first, pairs, experts, bits, mine, places);
+  if (!SCANNED) {
+    // `lanes` threads beside each other have an expert each, the groups of them every so many tiles
+    uint32_t lanes = 1;
+    while (lanes < experts && lanes < THREADS) lanes *= 2;
+    const uint32_t groups = THREADS / lanes;
+    for (uint32_t e = threadIdx.x % lanes; e < experts; e += lanes) {
+      uint32_t mine_in_front = 0, mine_all = 0;
+#pragma unroll 8
+      for (uint32_t q = threadIdx.x / lanes; q < tiles; q += groups) {
+        const uint32_t n = hist[q * (experts + 1) + e];
+        mine_all += n;
+        mine_in_front += q < blockIdx.x ? n : 0;
       }
+      atomicAdd(&in_front[e], mine_in_front);
+      atomicAdd(&all[e], mine_all);
     }
-    uint32_t total;
-    const uint32_t start = block_exclusive_scan<uint32_t, TILE_THREADS>(all < capacity ? all : capacity, smem, total);
-    if (e < experts) {
-      starts[e] = kept + start;
-      if (blockIdx.x == 0) offsets[e] = kept + start;
+  } else {
+    for (uint32_t e = threadIdx.x; e < experts; e += THREADS) {
+      const uint32_t begin = hist[e * tiles];
+      in_front[e] = hist[e * tiles + blockIdx.x] - begin;
+      all[e] = hist[(e + 1) * tiles] - begin;
     }
-    kept += total;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) offsets[experts] = kept;
   __syncthreads();
-  place_run(chosen, first, last, pairs, experts, bits, capacity, top, mine, starts, slot, source);
-  for (int64_t s = (int64_t)kept + (int64_t)blockIdx.x * TILE_THREADS + threadIdx.x; s < pairs; s += tiles * TILE_THREADS)
-    source[s] = -1;
+  const uint32_t kept = runs_to_ranks(counts, starts, experts, capacity, smem, [&](uint32_t e) { return in_front[e]; },
+                                      [&](uint32_t e, uint32_t) { return all[e]; });
+  __syncthreads();
+  place_run(places, first, pairs, experts, capacity, top, mine, starts, slot, source);
+  if (blockIdx.x == 0) {
+    for (uint32_t e = threadIdx.x; e < experts; e += THREADS) offsets[e] = starts[e];
+    if (threadIdx.x == 0) offsets[experts] = kept;
+  }
+  for (int64_t s = (int64_t)kept + (int64_t)blockIdx.x * THREADS + threadIdx.x; s < pairs; s += tiles * THREADS) source[s] = -1;
 }
 
 struct RouteSpace {
@@ -191,7 +232,7 @@ struct RouteSpace {
 };
 
 RouteSpace route_space(Arena& a, int64_t pairs, int32_t experts) {
-  const int64_t counters = pairs > ONE_PAIRS ? ((int64_t)experts + 1) * ceil_div(pairs, TILE) : 0;
+  const int64_t counters = pairs > ONE ? ((int64_t)experts + 1) * ceil_div(pairs, TILE) : 0;
   RouteSpace s;
   s.hist = a.take<uint32_t>(counters);
   s.scratch = a.take<uint32_t>(scan_scratch_elems(counters));
@@ -199,33 +240,41 @@ RouteSpace route_space(Arena& a, int64_t pairs, int32_t experts) {
   return s;
 }
 
+template <typename Key, bool SCANNED>
+int32_t route_tiles(const Key* chosen, uint32_t experts, int bits, uint32_t most, const ginex_routing_t* out,
+                    const RouteSpace& s, hipStream_t st) {
+  const int64_t pairs = out->rows * out->top, tiles = ceil_div(pairs, TILE);
+  const size_t counters = ((size_t)experts + 1) * sizeof(uint32_t);
+  hipLaunchKernelGGL((k_route_count<Key, SCANNED>), dim3((unsigned)tiles), dim3(THREADS), counters, st, chosen, pairs, experts,
+                     s.hist);
+  GINEX_LAUNCH_CHECK();
+  if (SCANNED) GINEX_HIP(exclusive_scan_inplace(s.hist, (experts + 1) * tiles, s.scratch, st));
+  hipLaunchKernelGGL((k_route_place<Key, SCANNED>), dim3((unsigned)tiles), dim3(THREADS), (WAVES + 3) * counters, st, chosen,
+                     pairs, experts, bits, most, Divisor((uint32_t)out->top), s.hist, out->offsets, out->slot, out->source);
+  GINEX_LAUNCH_CHECK();
+  return GINEX_OK;
+}
+
 template <typename Key>
 int32_t route_pairs(const Key* chosen, int64_t capacity, const ginex_routing_t* out, void* ws, hipStream_t st) {
   const int64_t pairs = out->rows * out->top;
   const uint32_t experts = (uint32_t)out->experts;
   const uint32_t most = capacity < 0 || capacity > INT32_MAX ? (uint32_t)INT32_MAX : (uint32_t)capacity;
-  const Divisor top((uint32_t)out->top);
   int bits = 0;
   while ((experts >> bits) != 0) ++bits;       // the numbers 0 .. experts
-  if (pairs <= ONE_PAIRS) {
-    const size_t lds = (ONE_WAVES * ((size_t)experts + 1) + experts) * sizeof(uint32_t);
-    hipLaunchKernelGGL(k_route_one<Key>, dim3(1), dim3(ONE_THREADS), lds, st, chosen, pairs, experts, bits, most, top,
-                       out->offsets, out->slot, out->source);
+  if (pairs <= ONE) {
+    const size_t lds = (WAVES * ((size_t)experts + 1) + experts) * sizeof(uint32_t);
+    // (lanes go through all the rounds they have registers for: 2.6 us for up to 512 pairs, 5.6 with 16 rounds)
+    const auto kernel = pairs <= THREADS ? k_route_one<Key, 1> : pairs <= 4 * THREADS ? k_route_one<Key, 4> : k_route_one<Key, 16>;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(THREADS), lds, st, chosen, pairs, experts, bits, most,
+                       Divisor((uint32_t)out->top), out->offsets, out->slot, out->source);
     GINEX_LAUNCH_CHECK();
     return GINEX_OK;
   }
   Arena a(ws);
   const RouteSpace s = route_space(a, pairs, out->experts);
-  const int64_t tiles = ceil_div(pairs, TILE);
-  hipLaunchKernelGGL(k_route_count<Key>, dim3((unsigned)tiles), dim3(TILE_THREADS), ((size_t)experts + 1) * sizeof(uint32_t),
-                     st, chosen, pairs, experts, s.hist);
-  GINEX_LAUNCH_CHECK();
-  GINEX_HIP(exclusive_scan_inplace(s.hist, (experts + 1) * tiles, s.scratch, st));
-  const size_t lds = (TILE_WAVES * ((size_t)experts + 1) + experts) * sizeof(uint32_t);
-  hipLaunchKernelGGL(k_route_place<Key>, dim3((unsigned)tiles), dim3(TILE_THREADS), lds, st, chosen, pairs, experts, bits,
-                     most, top, s.hist, out->offsets, out->slot, out->source);
-  GINEX_LAUNCH_CHECK();
-  return GINEX_OK;
+  return ceil_div(pairs, TILE) <= MOST_TILES ? route_tiles<Key, false>(chosen, experts, bits, most, out, s, st)
+                                             : route_tiles<Key, true>(chosen, experts, bits, most, out, s, st);
 }
 
 }  // namespace

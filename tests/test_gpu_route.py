@@ -83,6 +83,12 @@ def test_route_all_to_one_value(g, rows, value):
     same_route(routed(g, chosen, 7), plain_route(chosen, 7))
 
 
+@pytest.mark.parametrize("rows, top, experts", [(524_288, 8, 300), (524_289, 8, 300), (2_100_001, 2, 5)])
+def test_route_of_many_tiles(g, rows, top, experts):
+    chosen = choices(rows, top, experts, seed=rows)
+    same_route(routed(g, chosen, experts, 1_000_000, False), plain_route(chosen, experts, 1_000_000))
+
+
 def test_route_refusals(g):
     good = torch.zeros((4, 2), dtype=torch.int64, device="cuda")
     with pytest.raises(ValueError):
