@@ -64,6 +64,33 @@ __device__ __forceinline__ int64_t range_begin_of(int64_t at, int64_t length, in
   return at - begin <= near ? begin : end - at <= near ? end : at;
 }
 
+// The ends of a range, and the expert that its first slot is of (`experts` for a range behind all slots).  Every wave finds
+// them by itself, its lanes look at 64 experts at a time: one trip to memory and no barrier.
+__device__ __forceinline__ int32_t find_range(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
+                                              int64_t range, int64_t length, int64_t& range_begin, int64_t& range_end) {
+  int32_t first = experts;
+  for (int32_t e0 = 0; e0 < experts; e0 += WAVE) {
+    const int32_t e = e0 + lane_id();
+    int64_t begin = 0, end = 0;
+    if (e < experts) slots_of(offsets, e, slots, begin, end);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = (range + i) * length;
+      const uint64_t has = __ballot(begin <= at && at < end);
+      if (has == 0) continue;
+      const int lane = __ffsll((unsigned long long)has) - 1;
+      const int64_t snapped = range_begin_of(at, length, (int64_t)of_lane((uint64_t)begin, lane), (int64_t)of_lane((uint64_t)end, lane));
+      if (i == 0) {
+        range_begin = snapped;
+        first = e0 + lane;
+      } else {
+        range_end = snapped;
+      }
+    }
+  }
+  return first;
+}
+
 // Where a range leaves its part of an expert that it shares: only the first of its experts can have begun in front of
 // it, and only the last can go on behind it.
 __device__ __forceinline__ int64_t part_of(int64_t range, bool first) { return 2 * range + (first ? 1 : 0); }
@@ -168,8 +195,6 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
   constexpr int XN = (XS + THREADS - 1) / THREADS, YN = YS / THREADS;
   static_assert(YS % THREADS == 0 && (XS % THREADS == 0 || XS < THREADS), "chunks of a thread");
   __shared__ __attribute__((aligned(16))) bf16 lds[S::BUFFERS * S::SIZE];
-  __shared__ int64_t ends[2];
-  __shared__ int32_t first_last[2];
 
   // Workgroups go to the 8 dies in turn: the tiles of a range, which read the same rows, to one of them.
   const uint32_t die = blockIdx.x % 8, local = blockIdx.x / 8;
@@ -179,35 +204,9 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
   const int64_t length = range_length(offsets, experts, slots, ranges);
   const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
 
-  // its ends, and the experts that have slots in it
-  if (threadIdx.x == 0) {
-    first_last[0] = experts;
-    first_last[1] = -1;
-    ends[0] = ends[1] = slots;
-  }
-  __syncthreads();
-  for (int32_t e = threadIdx.x; e < experts; e += THREADS) {
-    int64_t begin, end;
-    slots_of(offsets, e, slots, begin, end);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t at = (range + i) * length;
-      if (begin <= at && at < end) ends[i] = range_begin_of(at, length, begin, end);
-    }
-  }
-  __syncthreads();
-  const int64_t range_begin = uniform(ends[0]), range_end = uniform(ends[1]);
-  for (int32_t e = threadIdx.x; e < experts; e += THREADS) {
-    int64_t begin, end;
-    slots_of(offsets, e, slots, begin, end);
-    if (begin < end && begin < range_end && end > range_begin) {
-      atomicMin(&first_last[0], e);
-      atomicMax(&first_last[1], e);
-    }
-  }
-  __syncthreads();
-  const int32_t first_expert = __builtin_amdgcn_readfirstlane(first_last[0]);
-  const int32_t last_expert = __builtin_amdgcn_readfirstlane(first_last[1]);
+  // its ends, and the first expert that has slots in it
+  int64_t range_begin = slots, range_end = slots;
+  const int32_t first_expert = find_range(offsets, experts, slots, range, length, range_begin, range_end);
 
   // Where a thread's chunks are in a row of codes and of dy.  Chunks behind the end repeat one that is there, and their
   // sums are not written; the last chunk of dy ends with the row, so it may share columns with the one in front of it.
@@ -235,11 +234,12 @@ __global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
   const int k_of = 8 * (lane / 32) + lane % 16 / 4, col_of = lane % 32 / 16 * 16 + lane % 4 * 4;
   const int xb = k_of * XP + wm * MT * 32 + col_of, yb = S::XSIZE + k_of * YP + wn * NT * 32 + col_of;
 
-  for (int32_t expert = first_expert; expert <= last_expert; ++expert) {
+  for (int32_t expert = first_expert; expert < experts; ++expert) {
     int64_t expert_begin, expert_end;
     slots_of(offsets, expert, slots, expert_begin, expert_end);
     expert_begin = uniform(expert_begin);
     expert_end = uniform(expert_end);
+    if (expert_begin >= range_end) break;
     const int64_t begin = expert_begin > range_begin ? expert_begin : range_begin;
     const int64_t end = expert_end < range_end ? expert_end : range_end;
     if (begin >= end) continue;
