@@ -176,7 +176,7 @@ template <typename T, int WM, int MT, int WN, int NT>
 struct Shape {
   static constexpr int THREADS = WM * WN * WAVE, TM = WM * MT * 32, TN = WN * NT * 32, TERM = TERMS<T>;
   static constexpr int BUFFERS = WM * WN == 8 ? 2 : 1;
-  static constexpr int DEPTH = TERM == 1 && BUFFERS == 2 ? 64 : 32;       // slots in LDS at a time
+  static constexpr int DEPTH = TERM == 1 ? 64 : 32;       // slots in LDS at a time
   static constexpr int XP = TM + PAD, YP = TN + PAD;
   static constexpr int XSIZE = DEPTH * XP, YSIZE = DEPTH * YP;            // of an array in LDS
   static constexpr int SIZE = XSIZE + TERM * YSIZE;
@@ -184,7 +184,7 @@ struct Shape {
 
 // NARROW: dy has fewer than 8 columns.
 template <typename T, int WM, int MT, int WN, int NT, bool NARROW>
-__global__ __launch_bounds__(WM* WN* WAVE, WM* WN == 8 ? 2 : 3) void k_weights(
+__global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
     const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int32_t blocks,
     const int32_t* __restrict__ source, const int64_t* __restrict__ offsets, int32_t experts, int64_t slots, int32_t ranges,
     RowsOf<const T> dy, int32_t width, int32_t out_width, int32_t tiles_m, int32_t tiles, float* __restrict__ dw,
