@@ -43,13 +43,12 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32)) << 32 | lo);
 }
 
-// Slots of a range: the slots that are taken, over `ranges` ranges, rounded up.
-__device__ __forceinline__ int64_t range_length(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
-                                                int32_t ranges) {
-  int64_t taken = offsets ? offsets[experts] : slots;
+// Slots of a range: the slots that are taken, over `ranges` ranges, rounded up.  (There are fewer than 2^31 slots: divisions
+// are in 32 bits, a quarter of the instructions of 64.)
+__device__ __forceinline__ int64_t range_length(int64_t taken, int64_t slots, int32_t ranges) {
   taken = taken < 0 ? 0 : (taken < slots ? taken : slots);
-  const int64_t length = ((taken + ranges - 1) / ranges + STEP - 1) / STEP * STEP;
-  return uniform(length > STEP ? length : STEP);
+  const uint32_t length = ((uint32_t)(taken + ranges - 1) / (uint32_t)ranges + STEP - 1) / STEP * STEP;
+  return uniform((int64_t)(length > STEP ? length : STEP));
 }
 
 // Ranges begin at multiples of their length, but not near to where an expert begins: there they begin with it, which
@@ -64,25 +63,39 @@ __device__ __forceinline__ int64_t range_begin_of(int64_t at, int64_t length, in
   return at - begin <= near ? begin : end - at <= near ? end : at;
 }
 
-// The ends of a range, and the expert that its first slot is of (`experts` for a range behind all slots).  Every wave finds
-// them by itself, its lanes look at 64 experts at a time: one trip to memory and no barrier.
+// The slots of 64 experts, one to a lane: what a wave knows of the experts, read in one trip to memory.
+struct Experts {
+  int32_t first;
+  int64_t begin, end;
+  __device__ __forceinline__ void read(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots, int32_t from) {
+    first = from;
+    begin = end = 0;
+    if (from + lane_id() < experts) slots_of(offsets, from + lane_id(), slots, begin, end);
+  }
+  __device__ __forceinline__ int64_t begin_of(int lane) const { return (int64_t)of_lane((uint64_t)begin, lane); }
+  __device__ __forceinline__ int64_t end_of(int lane) const { return (int64_t)of_lane((uint64_t)end, lane); }
+};
+
+// The ends of a range and the expert that its first slot is of (`experts` for a range behind all slots), which is among those
+// in `some` afterwards, as some[0] is before.  Every wave finds them by itself, without a barrier.
 __device__ __forceinline__ int32_t find_range(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
-                                              int64_t range, int64_t length, int64_t& range_begin, int64_t& range_end) {
+                                              int64_t range, int64_t length, Experts& some, int64_t& range_begin,
+                                              int64_t& range_end) {
   int32_t first = experts;
+  Experts now = some;
   for (int32_t e0 = 0; e0 < experts; e0 += WAVE) {
-    const int32_t e = e0 + lane_id();
-    int64_t begin = 0, end = 0;
-    if (e < experts) slots_of(offsets, e, slots, begin, end);
+    if (e0 > 0) now.read(offsets, experts, slots, e0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t at = (range + i) * length;
-      const uint64_t has = __ballot(begin <= at && at < end);
+      const uint64_t has = __ballot(now.begin <= at && at < now.end);
       if (has == 0) continue;
       const int lane = __ffsll((unsigned long long)has) - 1;
-      const int64_t snapped = range_begin_of(at, length, (int64_t)of_lane((uint64_t)begin, lane), (int64_t)of_lane((uint64_t)end, lane));
+      const int64_t snapped = range_begin_of(at, length, now.begin_of(lane), now.end_of(lane));
       if (i == 0) {
         range_begin = snapped;
         first = e0 + lane;
+        some = now;
       } else {
         range_end = snapped;
       }
@@ -201,12 +214,14 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
   const int32_t tile_of = (int32_t)(local % tiles);
   const int64_t range = (int64_t)(local / tiles) * 8 + die;
   if (range >= ranges) return;
-  const int64_t length = range_length(offsets, experts, slots, ranges);
+  Experts some;
+  some.read(offsets, experts, slots, 0);
+  const int64_t length = range_length(offsets ? offsets[experts] : slots, slots, ranges);
   const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
 
   // its ends, and the first expert that has slots in it
   int64_t range_begin = slots, range_end = slots;
-  const int32_t first_expert = find_range(offsets, experts, slots, range, length, range_begin, range_end);
+  const int32_t first_expert = find_range(offsets, experts, slots, range, length, some, range_begin, range_end);
 
   // Where a thread's chunks are in a row of codes and of dy.  Chunks behind the end repeat one that is there, and their
   // sums are not written; the last chunk of dy ends with the row, so it may share columns with the one in front of it.
@@ -235,10 +250,8 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
   const int xb = k_of * XP + wm * MT * 32 + col_of, yb = S::XSIZE + k_of * YP + wn * NT * 32 + col_of;
 
   for (int32_t expert = first_expert; expert < experts; ++expert) {
-    int64_t expert_begin, expert_end;
-    slots_of(offsets, expert, slots, expert_begin, expert_end);
-    expert_begin = uniform(expert_begin);
-    expert_end = uniform(expert_end);
+    if (expert >= some.first + WAVE) some.read(offsets, experts, slots, expert);
+    const int64_t expert_begin = some.begin_of(expert - some.first), expert_end = some.end_of(expert - some.first);
     if (expert_begin >= range_end) break;
     const int64_t begin = expert_begin > range_begin ? expert_begin : range_begin;
     const int64_t end = expert_end < range_end ? expert_end : range_end;
@@ -267,6 +280,15 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
       constexpr int P = decltype(set)::value;
       const int64_t from = s0 < last ? s0 : last;
       const uint32_t left = (uint32_t)(last - from < DEPTH ? last - from : DEPTH);
+      // (the gradients first: they need not wait for the rows)
+      const T* const at = dy.data + from * dy.stride;
+#pragma unroll
+      for (int i = 0; i < YN; ++i) {
+        const uint32_t k = (threadIdx.x + i * THREADS) / (TN / 8);
+        const T* const p = at + ((uint64_t)(k < left ? k : left) * stride + y_at[i]);
+        if (NARROW) y[P][i].load(p, out_width);
+        else y[P][i].load(p);
+      }
 #pragma unroll
       for (int i = 0; i < XN; ++i) {
         const uint32_t k = (threadIdx.x + i * THREADS) / (TM / 16);
@@ -276,14 +298,6 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
         typedef words4 At __attribute__((aligned(8)));
         x[P][i] = *reinterpret_cast<const At*>(codes + ((uint64_t)r * pitch + x_at[i]));
         scale[P][i] = scales[(uint64_t)r * (uint32_t)blocks + scale_at[i]];
-      }
-      const T* const at = dy.data + from * dy.stride;
-#pragma unroll
-      for (int i = 0; i < YN; ++i) {
-        const uint32_t k = (threadIdx.x + i * THREADS) / (TN / 8);
-        const T* const p = at + ((uint64_t)(k < left ? k : left) * stride + y_at[i]);
-        if (NARROW) y[P][i].load(p, out_width);
-        else y[P][i].load(p);
       }
     };
     auto put = [&](auto set, bf16* to, int64_t s0) {
@@ -440,15 +454,15 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __
                                                                int64_t slots, int32_t ranges, int64_t size,
                                                                const float* __restrict__ partial, float* __restrict__ dw) {
   const int32_t mine = blockIdx.y;
-  const int64_t length = range_length(offsets, experts, slots, ranges);
   int64_t begin, end;
   slots_of(offsets, mine, slots, begin, end);
+  const int64_t length = range_length(offsets ? offsets[experts] : slots, slots, ranges);
   // the ranges that begin inside the expert; the one in front of them has its first part
   const int64_t near = near_of(length);
-  const int64_t first = (begin + near) / length + 1;
-  int64_t last = (end - near - 1) / length;
+  const int64_t first = (uint32_t)(begin + near) / (uint32_t)length + 1;
+  int64_t last = end > near ? (uint32_t)(end - near - 1) / (uint32_t)length : 0;
   if (end > begin && last < first) return;
-  last = end > begin && last >= ranges ? ranges - 1 : last;
+  last = last < ranges ? last : ranges - 1;
   const int64_t i = ((int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
   if (i >= size) return;
   typedef float four __attribute__((ext_vector_type(4)));
