@@ -7,9 +7,10 @@
 // popcount, and the run's count of the expert so far (in LDS, a row of counters per wave) gives the rest:
 // no atomic decides a place, and equal inputs give equal slots.
 //
-// Bound by launches: up to 8192 pairs one workgroup in one launch (128 pairs 2.3 us), else the tiles'
-// counts and the places, in which every workgroup adds up the counts of the tiles itself; with a scan
-// between them, five launches, 1.64 M pairs took 35 us and 152 000 20.
+// Bound by launches and their latencies: up to 8192 pairs one workgroup in one launch (up to 512 pairs 2.3 us,
+// 7000 7.8), else the tiles' counts and the places, in which every workgroup adds up the counts of the tiles
+// itself (354 000 pairs 4.7 + 7.6 us, 1.64 M 4.6 + 18); with a scan between them, five launches, 1.64 M pairs
+// took 35 us in all and 152 000 20 instead of 15.
 #include "primitives.hpp"
 #include "train.hpp"
 

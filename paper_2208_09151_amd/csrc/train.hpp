@@ -35,22 +35,25 @@ struct Width {
   }
 };
 
-// The chunk of the row that begins at `row` from column c on, a multiple of N, as f32; columns behind the width are 0.
+template <typename T>
+union ChunkWords {
+  typename Chunk<T>::Wide wide;
+  words4 words;
+};
+
+// The chunk of the row that begins at `row` from column c on, a multiple of N, as it is; columns behind the width are 0.
 // The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
 // others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
 template <typename T>
-__device__ __forceinline__ void load_chunk(const T* row, int32_t c, Width w, float (&v)[Chunk<T>::N]) {
+__device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Width w) {
   constexpr int N = Chunk<T>::N;
+  ChunkWords<T> u;
   if (w.width < N) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = c + i < w.width ? (float)row[c + i] : 0.f;
-    return;
+    for (int i = 0; i < N; ++i) u.wide[i] = c + i < w.width ? row[c + i] : (T)0.f;
+    return u;
   }
   const bool ends = c + N > w.width;
-  union {
-    typename Chunk<T>::Wide wide;
-    words4 words;
-  } u;
   u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (ends ? w.width - N : c));
   if (w.missing) {
     words4 m = u.words;
@@ -64,22 +67,23 @@ __device__ __forceinline__ void load_chunk(const T* row, int32_t c, Width w, flo
     for (int i = 0; i < 4; ++i) u.words[i] = ends ? m[i] : u.words[i];
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = c < w.width ? (float)u.wide[i] : 0.f;
+  for (int i = 0; i < 4; ++i) u.words[i] = c < w.width ? u.words[i] : 0;
+  return u;
 }
 
-// Rounded to nearest, halves to even.  KEEP: through the caches, which put together lines that several rows share;
-// else past them.
-template <bool KEEP = false, typename T>
-__device__ __forceinline__ void store_chunk(T* row, int32_t c, Width w, const float (&v)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-  union {
-    typename Chunk<T>::Wide wide;
-    words4 words;
-  } u;
+// The same as f32.
+template <typename T>
+__device__ __forceinline__ void load_chunk(const T* row, int32_t c, Width w, float (&v)[Chunk<T>::N]) {
+  const ChunkWords<T> u = load_words(row, c, w);
 #pragma unroll
-  for (int i = 0; i < N; ++i) u.wide[i] = (T)v[i];
+  for (int i = 0; i < Chunk<T>::N; ++i) v[i] = (float)u.wide[i];
+}
+
+// KEEP: through the caches, which put together lines that several rows share; else past them.
+template <bool KEEP = false, typename T>
+__device__ __forceinline__ void store_words(T* row, int32_t c, Width w, const ChunkWords<T>& u) {
   T* p = row + c;
-  if (c + N <= w.width) {
+  if (c + Chunk<T>::N <= w.width) {
     if (KEEP) *reinterpret_cast<typename Chunk<T>::At*>(p) = u.wide;
     else __builtin_nontemporal_store(u.wide, reinterpret_cast<typename Chunk<T>::At*>(p));
     return;
@@ -99,6 +103,15 @@ __device__ __forceinline__ void store_chunk(T* row, int32_t c, Width w, const fl
     m[0] = m[1];
   }
   if (bytes & 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)m[0];
+}
+
+// Rounded to nearest, halves to even.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* row, int32_t c, Width w, const float (&v)[Chunk<T>::N]) {
+  ChunkWords<T> u;
+#pragma unroll
+  for (int i = 0; i < Chunk<T>::N; ++i) u.wide[i] = (T)v[i];
+  store_words(row, c, w, u);
 }
 
 // n / d for n below 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers

@@ -7,6 +7,16 @@
 // range expert by expert.  An expert that lies in one range is written where it belongs; one that several
 // ranges share leaves its parts in the workspace, and a second launch adds them up in their order, so that
 // equal inputs give equal bits.
+//
+// Codes are exact in bf16, and so are the terms that a gradient is cut into: all products are exact, and the
+// sums are the matrix cores' f32.  Codes and gradients come from HBM into registers two steps ahead, are
+// taken apart on the vector unit and put into LDS with the slots as rows, where transposing reads turn them
+// into operands.
+//
+// Measured, kernel and join, 820 000 x 2 slots in 32 experts, 256 x 256: f32 616-680 us (1040 TFLOP/s of bf16
+// products; the clock falls to 1.6-1.9 GHz: bound by power), f16 422, bf16 290 (codes are read once per expert of a
+// row: 1.34 GB, 5.1 TB/s without the join).  76 000 x 2 in 8 experts, 128 x 256, bf16: 30 + 7.5 us, of which the
+// parts of 512 workgroups are 6.5 + 7, the slots 13, launch and first loads 7.
 #include "codes.hpp"
 
 namespace ginex {
@@ -146,7 +156,11 @@ struct Terms {
   float v[8];
   __device__ __forceinline__ explicit Terms(const Eight<T>& from) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)from.v[i / Eight<T>::N][i % Eight<T>::N];
+    for (int i = 0; i < 8; ++i) {
+      v[i] = (float)from.v[i / Eight<T>::N][i % Eight<T>::N];
+      // (a signalling NaN may have its bits in the lower half alone, a quiet one has not)
+      if (sizeof(T) == 4) v[i] = __builtin_canonicalizef(v[i]);
+    }
   }
   template <bool FIRST>
   __device__ __forceinline__ words4 next() {

@@ -314,6 +314,17 @@ def test_weight_gradient_with_values_that_are_no_numbers(g, dtype):
     assert not torch.isfinite(got[1, :, 2]).all() and torch.isfinite(got[2]).all()
 
 
+@pytest.mark.parametrize("bits", [0x7F800001, 0x7FC00000, 0x7FFFFFFF])
+def test_weight_gradient_with_any_nan(g, bits):
+    """A NaN's bits may all be in the lower half of an f32."""
+    dy = torch.ones((40, 9))
+    dy.view(torch.int32)[7, 3] = bits
+    got = g.weight_gradient(g.compress(torch.ones((40, 32)).cuda()), dy.cuda()).cpu()
+    assert got[:, 3].isnan().all()
+    got[:, 3] = 40
+    assert (got == 40).all()
+
+
 def test_weight_gradient_of_large_and_small_numbers(g):
     x = torch.ones((64, 32))
     dy = torch.zeros((64, 8))

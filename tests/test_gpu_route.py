@@ -222,6 +222,18 @@ def test_written_rows_stay_inside_their_width(g, dtype):
     assert torch.equal(y[:, 3:40], (x.double() * count[:, None]).to(dtype))     # 0, 1 or 2 times the row
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [5, 32, 37])
+def test_dispatch_copies_bits(g, dtype, width):
+    """Whatever a row holds, NaNs of any bits and subnormal numbers among it."""
+    words = torch.int32 if dtype == torch.float32 else torch.int16
+    low, high = torch.iinfo(words).min, torch.iinfo(words).max
+    x = torch.randint(low, high, (200, width), dtype=words, generator=torch.Generator().manual_seed(width))
+    r = routed(g, choices(200, 2, 5, absent=0), 5)
+    out = g.dispatch(x.cuda().view(dtype), r).view(words).cpu()
+    assert torch.equal(out, x[r.source.cpu().long()])
+
+
 def test_one_row_for_all(g):
     chosen = choices(300, 2, 5, absent=0)
     r = routed(g, chosen, 5)
