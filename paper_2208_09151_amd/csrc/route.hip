@@ -22,8 +22,11 @@ constexpr int THREADS = WAVES * WAVE;
 constexpr int TILE_KEYS = 8;                    // pairs of a lane
 constexpr int ONE = THREADS * 16;               // up to here one workgroup does it all in one launch
 constexpr int TILE = THREADS * TILE_KEYS;
-// Up to here the tiles' counts are added up by every workgroup (reads that grow with the square of the
-// tiles: with 512 of them and 256 experts 270 MB of L2), beyond it they are scanned.
+// Up to here the tiles' counts are added up by every workgroup, which reads tiles x experts of them, beyond it they are
+// scanned, three launches more.  Adding and scanning, us of a call, by tiles and experts: 2048 x 8 50 and 45, 512 x 32
+// 24 and 27, 1024 x 32 42 and 36, 128 x 128 21 and 23, 256 x 128 31 and 26, 16 x 1024 21 and 25, 64 x 1024 45 and 26,
+// 1024 x 1024 1063 and 82.
+constexpr int64_t MOST_COUNTS = 1 << 14;
 constexpr int64_t MOST_TILES = 1024;
 
 // A lane's pair: its expert (`experts` for none), its rank among the lanes with the same one, and how many they are.
@@ -274,8 +277,10 @@ int32_t route_pairs(const Key* chosen, int64_t capacity, const ginex_routing_t* 
   }
   Arena a(ws);
   const RouteSpace s = route_space(a, pairs, out->experts);
-  return ceil_div(pairs, TILE) <= MOST_TILES ? route_tiles<Key, false>(chosen, experts, bits, most, out, s, st)
-                                             : route_tiles<Key, true>(chosen, experts, bits, most, out, s, st);
+  const int64_t tiles = ceil_div(pairs, TILE);
+  return tiles <= MOST_TILES && tiles * experts <= MOST_COUNTS
+             ? route_tiles<Key, false>(chosen, experts, bits, most, out, s, st)
+             : route_tiles<Key, true>(chosen, experts, bits, most, out, s, st);
 }
 
 }  // namespace

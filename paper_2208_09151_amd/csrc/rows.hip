@@ -126,13 +126,14 @@ __global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy
                                                               const int32_t* __restrict__ slot,
                                                               const float* __restrict__ weights,
                                                               const int64_t* __restrict__ end,
-                                                              float* __restrict__ dweights, int64_t rows, int32_t top,
-                                                              int32_t shift, Divisor cpr, Width width, int64_t slots) {
+                                                              float* __restrict__ dweights, int64_t first, int64_t rows,
+                                                              int32_t top, int32_t shift, Divisor cpr, Width width,
+                                                              int64_t slots) {
   constexpr int N = Chunk<T>::N;
   const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
   const int32_t group = 1 << shift;
   const bool has_row = t >> shift < rows;
-  const int64_t r = has_row ? t >> shift : rows - 1;       // (all lanes take part in the sums)
+  const int64_t r = first + (has_row ? t >> shift : rows - 1);       // (all lanes take part in the sums)
   const int lane = (int)(t & (group - 1));
   for (int32_t j = 0; j < top; j += K) {
     int32_t s[K];
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy
       if (has_row && lane == group - 1 && j + i < top) dweights[r * top + j + i] = s[i] >= 0 ? sum : 0.f;
     }
   }
-  clear_rest(dz, width, cpr, end, slots, t, (int64_t)gridDim.x * THREADS);
+  if (first == 0) clear_rest(dz, width, cpr, end, slots, t, (int64_t)gridDim.x * THREADS);
 }
 
 // How many of a row's choices are in flight together.
@@ -271,7 +272,6 @@ extern "C" int32_t ginex_combine_backward(const ginex_routing_t* route, const gi
   if (route->rows > 0 && (!weights || !dweights)) return fail(GINEX_ERR_ARG, "null weights or their gradient");
   if ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(dweights)) % 4)
     return fail(GINEX_ERR_ARG, "weights: misaligned");
-  if (route->rows == 0) return GINEX_OK;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   return with_type(dy->type, [&](auto t) -> int32_t {
     return with_choices(route->top, [&](auto k) -> int32_t {
@@ -280,11 +280,16 @@ extern "C" int32_t ginex_combine_backward(const ginex_routing_t* route, const gi
       const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);
       int32_t shift = 0;
       while (1 << shift < WAVE && 1 << shift < cpr) ++shift;
-      const int64_t blocks = ceil_div(dy->rows << shift, THREADS);
-      hipLaunchKernelGGL((k_combine_backward<T, K>), dim3((unsigned)blocks), dim3(THREADS), 0, st, read_rows<T>(dy),
-                         read_rows<T>(z), rows_of<T>(dz), route->slot, weights, route->offsets + route->experts, dweights,
-                         dy->rows, route->top, shift, Divisor((uint32_t)cpr), Width::of<T>(dy->width), dz->rows);
-      GINEX_LAUNCH_CHECK();
+      // (a launch has fewer than 2^32 threads)
+      const int64_t step = ((int64_t)1 << 31) >> shift;
+      for (int64_t r = 0; r < dy->rows; r += step) {
+        const int64_t rows = dy->rows - r < step ? dy->rows - r : step;
+        hipLaunchKernelGGL((k_combine_backward<T, K>), dim3((unsigned)ceil_div(rows << shift, THREADS)), dim3(THREADS), 0, st,
+                           read_rows<T>(dy), read_rows<T>(z), rows_of<T>(dz), route->slot, weights,
+                           route->offsets + route->experts, dweights, r, rows, route->top, shift, Divisor((uint32_t)cpr),
+                           Width::of<T>(dy->width), dz->rows);
+        GINEX_LAUNCH_CHECK();
+      }
       return GINEX_OK;
     });
   });

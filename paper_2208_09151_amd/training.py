@@ -51,6 +51,23 @@ def _dense(t, what, shape, dtype):
     return t
 
 
+def _space(workspace, need, like):
+    """The caller's workspace, or one for this call where there is none or it is too small."""
+    if workspace is None or workspace.numel() < need:
+        return _workspace(need, like.device)
+    _here(workspace, "workspace", torch.uint8)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return workspace
+
+
+def _with(made, what, t):
+    """A route or compressed rows in the memory that ``t`` is in, too."""
+    if made._device != t.get_device():
+        raise ValueError(f"{what}: on GPU {made._device}, the rows on {t.device}")
+    return made
+
+
 def _rows(t, what):
     """The descriptor of a matrix of rows."""
     _here(t, what)
@@ -93,6 +110,7 @@ class Route:
     slot: torch.Tensor          # int32 [rows, top]
     source: torch.Tensor        # int32 [rows * top]
     _desc: RoutingDesc = field(init=False, repr=False, compare=False)
+    _device: int = field(init=False, repr=False, compare=False)
 
     def __post_init__(self):
         _here(self.slot, "slot", torch.int32)
@@ -104,13 +122,14 @@ class Route:
         _dense(self.source, "source", (rows * top,), torch.int32)
         self.__dict__["_desc"] = RoutingDesc(rows, top, self.experts, self.offsets.data_ptr(),
                                              self.slot.data_ptr(), self.source.data_ptr())
+        self.__dict__["_device"] = self.slot.get_device()
 
     @classmethod
     def _made(cls, offsets, slot, source):
         """Of tensors that are known to be right."""
         made = object.__new__(cls)
         rows, top = slot.shape
-        made.__dict__.update(offsets=offsets, slot=slot, source=source, _desc=RoutingDesc(
+        made.__dict__.update(offsets=offsets, slot=slot, source=source, _device=slot.get_device(), _desc=RoutingDesc(
             rows, top, offsets.numel() - 1, offsets.data_ptr(), slot.data_ptr(), source.data_ptr()))
         return made
 
@@ -142,8 +161,7 @@ def route(chosen, experts, capacity=None, workspace=None) -> Route:
     need = lib.ginex_route_workspace_bytes(rows, top, experts)
     if need == 0:
         raise GinexError(-1, lib.ginex_last_error().decode())
-    ws = workspace if workspace is not None and workspace.numel() >= need \
-        else _workspace(need, chosen.device)
+    ws = _space(workspace, need, chosen)
     made = Route._made(chosen.new_empty(experts + 1, dtype=torch.int64),
                        chosen.new_empty((rows, top), dtype=torch.int32),
                        chosen.new_empty(rows * top, dtype=torch.int32))
@@ -157,14 +175,15 @@ def dispatch(x, route: Route, out=None):
     """ginex_dispatch: the rows of ``x`` in their slots, [rows * top, width]; slots without a row are 0."""
     desc = _rows(x, "x")
     out, to = _out(out, "out", (route.source.numel(), desc.width), x.dtype, x)
-    _check(_lib.load().ginex_dispatch(C.byref(route._desc), C.byref(desc), C.byref(to), _stream()))
+    _check(_lib.load().ginex_dispatch(C.byref(_with(route, "route", x)._desc), C.byref(desc), C.byref(to),
+                                      _stream()))
     return out
 
 
 def _combine(z, route, weights, out):
     desc = _rows(z, "z")
     out, to = _out(out, "out", (route.rows, desc.width), z.dtype, z)
-    _check(_lib.load().ginex_combine(C.byref(route._desc), C.byref(desc),
+    _check(_lib.load().ginex_combine(C.byref(_with(route, "route", z)._desc), C.byref(desc),
                                      None if weights is None else weights.data_ptr(), C.byref(to),
                                      _stream()))
     return out
@@ -187,7 +206,8 @@ def combine_backward(grad, z, route: Route, weights):
     desc, zdesc = _rows(grad, "grad"), _rows(z, "z")
     dz, to = _out(None, "dz", (zdesc.rows, zdesc.width), z.dtype, z)
     dweights = torch.empty_like(weights)
-    _check(_lib.load().ginex_combine_backward(C.byref(route._desc), C.byref(desc), C.byref(zdesc),
+    _check(_lib.load().ginex_combine_backward(C.byref(_with(route, "route", z)._desc), C.byref(desc),
+                                              C.byref(zdesc),
                                               weights.data_ptr(), C.byref(to), dweights.data_ptr(),
                                               _stream()))
     return dz, dweights
@@ -201,6 +221,7 @@ class Compressed:
     scales: torch.Tensor        # uint8 [rows, blocks]
     width: int
     _desc: CodesDesc = field(init=False, repr=False, compare=False)
+    _device: int = field(init=False, repr=False, compare=False)
 
     def __post_init__(self):
         _here(self.codes, "codes", torch.int8)
@@ -210,12 +231,13 @@ class Compressed:
         _dense(self.codes, "codes", (rows, blocks * CODE_BLOCK), torch.int8)
         _dense(self.scales, "scales", (rows, blocks), torch.uint8)
         self.__dict__["_desc"] = CodesDesc(rows, self.width, self.codes.data_ptr(), self.scales.data_ptr())
+        self.__dict__["_device"] = self.codes.get_device()
 
     @classmethod
     def _made(cls, codes, scales, width):
         """Of tensors that are known to be right."""
         made = object.__new__(cls)
-        made.__dict__.update(codes=codes, scales=scales, width=width, _desc=CodesDesc(
+        made.__dict__.update(codes=codes, scales=scales, width=width, _device=codes.get_device(), _desc=CodesDesc(
             codes.shape[0], width, codes.data_ptr(), scales.data_ptr()))
         return made
 
@@ -253,7 +275,7 @@ def restore(kept: Compressed, dtype=torch.float32, out=None):
     if dtype not in _TYPES:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
     out, to = _out(out, "out", (kept.rows, kept.width), dtype, kept.codes)
-    _check(_lib.load().ginex_restore(C.byref(kept._desc), C.byref(to), _stream()))
+    _check(_lib.load().ginex_restore(C.byref(_with(kept, "kept", out)._desc), C.byref(to), _stream()))
     return out
 
 
@@ -263,8 +285,8 @@ def activate_backward(kept: Compressed, grad, activation, out=None):
     kind = _activation(activation)
     desc = _rows(grad, "grad")
     out, to = _out(out, "out", (desc.rows, desc.width), grad.dtype, grad)
-    _check(_lib.load().ginex_activate_backward(C.byref(kept._desc), kind, C.byref(desc), C.byref(to),
-                                               _stream()))
+    _check(_lib.load().ginex_activate_backward(C.byref(_with(kept, "kept", grad)._desc), kind,
+                                               C.byref(desc), C.byref(to), _stream()))
     return out
 
 
@@ -282,8 +304,8 @@ def weight_gradient(kept: Compressed, grad, route: Route = None, out=None, works
                                                      kept.width, grad.shape[1])
     if need == 0:
         raise GinexError(-1, lib.ginex_last_error().decode())
-    ws = workspace if workspace is not None and workspace.numel() >= need \
-        else _workspace(need, grad.device)
-    _check(lib.ginex_weight_gradient(C.byref(kept._desc), None if route is None else C.byref(route._desc),
+    ws = _space(workspace, need, grad)
+    _check(lib.ginex_weight_gradient(C.byref(_with(kept, "kept", grad)._desc),
+                                     None if route is None else C.byref(_with(route, "route", grad)._desc),
                                      C.byref(desc), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return out

@@ -232,6 +232,18 @@ def test_refusals(g):
         g.weight_gradient(kept, torch.zeros((4, 8), device="cuda"), r)
 
 
+def test_codes_and_workspaces_elsewhere_are_refused(g):
+    x = torch.zeros((4, 64), device="cuda")
+    kept = g.compress(x)
+    there = g.Compressed._made(kept.codes.cpu(), kept.scales.cpu(), 64)
+    for call in (lambda: g.restore(there, out=x), lambda: g.activate_backward(there, x, "relu"),
+                 lambda: g.weight_gradient(there, x)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError, match="GPU memory"):
+        g.weight_gradient(kept, x, workspace=torch.empty(1 << 20, dtype=torch.uint8))
+
+
 # ---- weight gradients --------------------------------------------------------------------------------
 
 def routed(g, rows, top, experts, seed, absent=0.1, capacity=None):

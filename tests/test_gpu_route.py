@@ -89,6 +89,37 @@ def test_route_of_many_tiles(g, rows, top, experts):
     same_route(routed(g, chosen, experts, 1_000_000, False), plain_route(chosen, experts, 1_000_000))
 
 
+# on both sides of the sizes from which the tiles' counts are scanned
+@pytest.mark.parametrize("rows, top, experts", [
+    (32_768, 2, 1024), (32_769, 2, 1024), (16_384, 8, 512), (16_385, 8, 512), (1_048_576, 4, 16), (1_048_577, 4, 16),
+    (1_048_577, 4, 1)])
+@pytest.mark.parametrize("capacity", [None, 2_000])
+def test_route_with_and_without_a_scan(g, rows, top, experts, capacity):
+    chosen = choices(rows, top, experts, seed=rows)
+    same_route(routed(g, chosen, experts, capacity, False), plain_route(chosen, experts, capacity))
+
+
+def test_route_refuses_a_workspace_elsewhere(g):
+    good = torch.zeros((40_000, 2), dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError, match="GPU memory"):
+        g.route(good, 4, workspace=torch.empty(1 << 20, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="dtype"):
+        g.route(good, 4, workspace=torch.empty(1 << 20, device="cuda"))
+    with pytest.raises(ValueError, match="contiguous"):
+        g.route(good, 4, workspace=torch.empty(1 << 21, dtype=torch.uint8, device="cuda")[::2])
+
+
+def test_a_route_elsewhere_is_refused(g):
+    r = g.route(torch.zeros((4, 2), dtype=torch.int64, device="cuda"), 4)
+    x, z = torch.zeros((4, 8), device="cuda"), torch.zeros((8, 8), device="cuda")
+    w = torch.zeros((4, 2), device="cuda")
+    there = g.Route._made(r.offsets.cpu(), r.slot.cpu(), r.source.cpu())
+    for call in (lambda: g.dispatch(x, there), lambda: g.combine(z, there, w), lambda: g.dispatch_backward(z, there),
+                 lambda: g.combine_backward(x, z, there, w), lambda: g.weight_gradient(g.compress(x), z, there)):
+        with pytest.raises(ValueError, match="route"):
+            call()
+
+
 def test_route_refusals(g):
     good = torch.zeros((4, 2), dtype=torch.int64, device="cuda")
     with pytest.raises(ValueError):
@@ -349,3 +380,29 @@ def test_rows_beyond_2_to_the_31_elements(g):
     assert torch.equal(dz[last], rows[last])
     want = x[at].double().square().sum(1)
     assert ((dw[at, 0].double() - want).abs() <= width * F32 * want).all()
+
+
+def test_gradient_of_more_rows_than_a_launch_has(g):
+    """2^25 rows of 33 chunks and up, a wave each, make 2^31 threads; one row for all of dy and of z."""
+    n, width = (1 << 25) + 3, 257
+    dy = random_rows((1, width), torch.bfloat16, 3).cuda()
+    z = random_rows((1, width), torch.bfloat16, 4).cuda()
+    chosen = torch.zeros((n, 1), dtype=torch.int32, device="cuda")
+    chosen[5] = -1                                                    # the last slot is empty
+    r = g.route(chosen, 1)
+    w = torch.ones((n, 1), device="cuda")
+    w[-2:] = 2
+    dz, dw = g.combine_backward(dy.expand(n, width), z.expand(n, width), r, w)
+    for at in range(0, n, 1 << 22):
+        part = dz[at:at + (1 << 22)]
+        want = dy.expand_as(part).clone()
+        if at + (1 << 22) >= n:
+            want[-3:-1] *= 2
+            want[-1] = 0
+        assert torch.equal(part, want)
+    want = (dy.double() * z.double()).sum()
+    bound = (width + 1) * F32 * (dy.double() * z.double()).abs().sum()
+    dw = dw[:, 0].double()
+    assert float(dw[5]) == 0
+    dw[5] = want
+    assert float((dw - want).abs().max()) <= float(bound)
