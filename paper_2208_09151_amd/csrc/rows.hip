@@ -120,9 +120,9 @@ __device__ __forceinline__ float sum_to_last(float v, int32_t group) {
 }
 
 // `group` lanes share a row: they walk its chunks and add up their products at the end.  (Two rows to a group: 774 -> 934
-// us; one choice after the other: 780 -> 878; eight together: 152 -> 171.)
-template <typename T, int K>
-__global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy, RowsOf<const T> z, RowsOf<T> dz,
+// us; one choice after the other: 780 -> 878; eight together: 152 -> 171.)  BLOCK > THREADS: the whole workgroup does.
+template <typename T, int K, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_combine_backward(RowsOf<const T> dy, RowsOf<const T> z, RowsOf<T> dz,
                                                               const int32_t* __restrict__ slot,
                                                               const float* __restrict__ weights,
                                                               const int64_t* __restrict__ end,
@@ -130,7 +130,8 @@ __global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy
                                                               int32_t top, int32_t shift, Divisor cpr, Width width,
                                                               int64_t slots) {
   constexpr int N = Chunk<T>::N;
-  const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  constexpr bool WHOLE = BLOCK > THREADS;
+  const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
   const int32_t group = 1 << shift;
   const bool has_row = t >> shift < rows;
   const int64_t r = first + (has_row ? t >> shift : rows - 1);       // (all lanes take part in the sums)
@@ -158,13 +159,30 @@ __global__ __launch_bounds__(THREADS) void k_combine_backward(RowsOf<const T> dy
         store_chunk(dz.at(s[i]), c, width, scaled);
       }
     }
+    if constexpr (WHOLE) {
+      __shared__ float sums[K][BLOCK / WAVE];
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const float sum = sum_to_last(dot[i], group);
-      if (has_row && lane == group - 1 && j + i < top) dweights[r * top + j + i] = s[i] >= 0 ? sum : 0.f;
+      for (int i = 0; i < K; ++i) {
+        const float sum = sum_to_last(dot[i], WAVE);
+        if (lane % WAVE == WAVE - 1) sums[i][lane / WAVE] = s[i] >= 0 ? sum : 0.f;
+      }
+      __syncthreads();
+      if (lane < K && j + lane < top) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < BLOCK / WAVE; ++w) sum += sums[lane][w];
+        dweights[r * top + j + lane] = sum;
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const float sum = sum_to_last(dot[i], group);
+        if (has_row && lane == group - 1 && j + i < top) dweights[r * top + j + i] = s[i] >= 0 ? sum : 0.f;
+      }
     }
   }
-  if (first == 0) clear_rest(dz, width, cpr, end, slots, t, (int64_t)gridDim.x * THREADS);
+  if (first == 0) clear_rest(dz, width, cpr, end, slots, t, (int64_t)gridDim.x * BLOCK);
 }
 
 // How many of a row's choices are in flight together.
@@ -278,13 +296,19 @@ extern "C" int32_t ginex_combine_backward(const ginex_routing_t* route, const gi
       using T = decltype(t);
       constexpr int K = decltype(k)::value;
       const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);
+      // a workgroup to a row where rows are long and few (f32, 2 slots a row, a wave and a workgroup: 64 rows of 1024 5.9 and
+      // 3.8 us, of 8192 27 and 5.3, 1024 rows of 8192 47 and 28; but 1024 rows of 512 4.8 and 8.7, of 1024 6.3 and 9.0)
+      constexpr int WHOLE = 1024;
+      const bool whole = cpr > WAVE && dy->rows <= cpr;
       int32_t shift = 0;
-      while (1 << shift < WAVE && 1 << shift < cpr) ++shift;
+      while (1 << shift < (whole ? WHOLE : WAVE) && (whole || 1 << shift < cpr)) ++shift;
+      const auto kernel = whole ? k_combine_backward<T, K, WHOLE> : k_combine_backward<T, K, THREADS>;
+      const int threads = whole ? WHOLE : THREADS;
       // (a launch has fewer than 2^32 threads)
       const int64_t step = ((int64_t)1 << 31) >> shift;
       for (int64_t r = 0; r < dy->rows; r += step) {
         const int64_t rows = dy->rows - r < step ? dy->rows - r : step;
-        hipLaunchKernelGGL((k_combine_backward<T, K>), dim3((unsigned)ceil_div(rows << shift, THREADS)), dim3(THREADS), 0, st,
+        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(rows << shift, threads)), dim3((unsigned)threads), 0, st,
                            read_rows<T>(dy), read_rows<T>(z), rows_of<T>(dz), route->slot, weights,
                            route->offsets + route->experts, dweights, r, rows, route->top, shift, Divisor((uint32_t)cpr),
                            Width::of<T>(dy->width), dz->rows);

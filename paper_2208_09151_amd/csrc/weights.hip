@@ -24,7 +24,8 @@ namespace {
 
 constexpr int JOIN_THREADS = 256;
 constexpr int STEP = 16;          // the length of a range is a multiple of it
-constexpr int PAD = 32;           // elements behind a row in LDS, see k_weights
+// Elements from a row in LDS to the next: an odd multiple of 64 bytes, see k_weights.
+constexpr int pitch_of(int columns) { return columns == 32 ? 32 : columns + 32; }
 
 typedef short half_words __attribute__((ext_vector_type(4)));
 typedef bf16 fragment __attribute__((ext_vector_type(8)));
@@ -203,8 +204,8 @@ template <typename T, int WM, int MT, int WN, int NT>
 struct Shape {
   static constexpr int THREADS = WM * WN * WAVE, TM = WM * MT * 32, TN = WN * NT * 32, TERM = TERMS<T>;
   static constexpr int BUFFERS = WM * WN == 8 ? 2 : 1;
-  static constexpr int DEPTH = TERM == 1 ? 64 : 32;       // slots in LDS at a time
-  static constexpr int XP = TM + PAD, YP = TN + PAD;
+  static constexpr int DEPTH = TERM == 1 || TN == 32 ? 64 : 32;       // slots in LDS at a time
+  static constexpr int XP = pitch_of(TM), YP = pitch_of(TN);
   static constexpr int XSIZE = DEPTH * XP, YSIZE = DEPTH * YP;            // of an array in LDS
   static constexpr int SIZE = XSIZE + TERM * YSIZE;
 };
@@ -463,10 +464,14 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
   }
 }
 
-// Experts that several ranges share: added up in order.  Experts without slots: cleared.
+// Experts that several ranges share: added up in order.  Experts without slots: cleared.  A workgroup's threads are 2^shift
+// groups, each of which adds up its share of the parts, four elements a thread; the first group adds up the groups' sums.
 __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __restrict__ offsets, int32_t experts,
-                                                               int64_t slots, int32_t ranges, int64_t size,
+                                                               int64_t slots, int32_t ranges, int64_t size, int32_t shift,
                                                                const float* __restrict__ partial, float* __restrict__ dw) {
+  typedef float four __attribute__((ext_vector_type(4)));
+  typedef four At __attribute__((aligned(4)));
+  __shared__ four sums[JOIN_THREADS];
   const int32_t mine = blockIdx.y;
   int64_t begin, end;
   slots_of(offsets, mine, slots, begin, end);
@@ -477,27 +482,40 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __
   int64_t last = end > near ? (uint32_t)(end - near - 1) / (uint32_t)length : 0;
   if (end > begin && last < first) return;
   last = last < ranges ? last : ranges - 1;
-  const int64_t i = ((int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x) * 4;
-  if (i >= size) return;
-  typedef float four __attribute__((ext_vector_type(4)));
-  typedef four At __attribute__((aligned(4)));
+  const int32_t lanes = JOIN_THREADS >> shift, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
+  const int64_t i = ((int64_t)blockIdx.x * lanes + lane) * 4;
   four sum = {};
-  if (i + 4 <= size) {
-    if (end > begin) {
-      sum = *reinterpret_cast<const At*>(partial + part_of(first - 1, true) * size + i);
+  if (end > begin && i < size) {
+    // range first - 1 and those that follow; only what the first of them has is in its second place
+    const int64_t share = (last - first + 2 + (1 << shift) - 1) >> shift;
+    int64_t r = first - 1 + group * share;
+    const int64_t behind = r + share < last + 1 ? r + share : last + 1;
+    const float* const at = partial + i;
+    if (i + 4 <= size) {
+      if (group == 0) sum = *reinterpret_cast<const At*>(at + part_of(r++, true) * size);
 #pragma unroll 4
-      for (int64_t r = first; r <= last; ++r) sum += *reinterpret_cast<const At*>(partial + part_of(r, false) * size + i);
-    }
-    *reinterpret_cast<At*>(dw + mine * size + i) = sum;
-  } else {
-    for (int64_t n = i; n < size; ++n) {
-      float one = 0.f;
-      if (end > begin) {
-        one = partial[part_of(first - 1, true) * size + n];
-        for (int64_t r = first; r <= last; ++r) one += partial[part_of(r, false) * size + n];
+      for (; r < behind; ++r) sum += *reinterpret_cast<const At*>(at + part_of(r, false) * size);
+    } else {
+      for (int n = 0; i + n < size; ++n) {
+        float one = group == 0 ? at[part_of(r, true) * size + n] : 0.f;
+        for (int64_t q = group == 0 ? r + 1 : r; q < behind; ++q) one += at[part_of(q, false) * size + n];
+        sum[n] = one;
       }
-      dw[mine * size + n] = one;
     }
+  }
+  if (shift > 0) {
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (group > 0) return;
+    for (int32_t other = 1; other < 1 << shift; ++other) sum += sums[other * lanes + lane];
+  }
+  if (i >= size) return;
+  float* const to = dw + mine * size + i;
+  if (i + 4 <= size) {
+    *reinterpret_cast<At*>(to) = sum;
+  } else {
+    for (int n = 0; n < 3; ++n)
+      if (i + n < size) to[n] = sum[n];
   }
 }
 
@@ -527,7 +545,17 @@ Tiling tiling_of(int64_t slots, int32_t experts, int64_t width, int64_t out_widt
   if (width > 128) shape(4, 2, 2, 4);
   else shape(2, 2, 4, 2);
   const bool large = out_width > 128 && slots * t.tiles() >= 256 * 1024;
-  if (!large) shape(2, 2, 2, 2);
+  // Else 128 x 128, or as narrow as the layer: what a tile has too many of is read, cut and multiplied for nothing (f32,
+  // 1 000 000 slots, 128 x 8: 111 us in tiles of 128 x 128, 50 of 128 x 32; 500 000 x 2 in 512 experts, 64 x 64: 143 and 81;
+  // 820 000, 256 x 47: 197 and 145; bf16, 820 000 x 2, 64 x 64: 100 and 64;
+  // the call of 820 000 x 2 f32, 16 x 128: 215 and 168).
+  if (!large) {
+    if (out_width <= 32) shape(4, 1, 1, 1);
+    else if (out_width <= 64 && width <= 64) shape(2, 1, 2, 1);
+    else if (out_width <= 64) shape(2, 2, 2, 1);
+    else if (width <= 64) shape(1, 2, 4, 1);
+    else shape(2, 2, 2, 2);
+  }
   // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us)
   int64_t ranges = (large ? 256 : 512) / t.tiles();
   // 128 slots at least, but a range for every expert of few slots (64 rows of 8 experts: 27 -> 14 us)
@@ -541,8 +569,11 @@ Tiling tiling_of(int64_t slots, int32_t experts, int64_t width, int64_t out_widt
 template <typename T>
 auto kernel_of(const Tiling& t, int64_t out_width) {
   if (t.nt == 4) return k_weights<T, 4, 2, 2, 4, false>;
-  if (t.wn == 4) return k_weights<T, 2, 2, 4, 2, false>;
-  return out_width < 8 ? k_weights<T, 2, 2, 2, 2, true> : k_weights<T, 2, 2, 2, 2, false>;
+  if (t.wn == 4 && t.nt == 2) return k_weights<T, 2, 2, 4, 2, false>;
+  if (t.wn == 4) return k_weights<T, 1, 2, 4, 1, false>;
+  if (t.wm == 4) return out_width < 8 ? k_weights<T, 4, 1, 1, 1, true> : k_weights<T, 4, 1, 1, 1, false>;
+  if (t.nt == 2) return k_weights<T, 2, 2, 2, 2, false>;
+  return t.mt == 2 ? k_weights<T, 2, 2, 2, 1, false> : k_weights<T, 2, 1, 2, 1, false>;
 }
 
 }  // namespace
@@ -599,8 +630,12 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
                        slots, by.ranges, read_rows<T>(dy), (int32_t)kept->width,
                        (int32_t)dy->width, (int32_t)by.tiles_m, (int32_t)by.tiles(), dw, partial);
     GINEX_LAUNCH_CHECK();
-    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(size, 4 * JOIN_THREADS), (unsigned)experts), dim3(JOIN_THREADS), 0,
-                       st, offsets, experts, slots, by.ranges, size, partial, dw);
+    // few elements: more threads for each (512 parts of 1024 elements: 46 us with one, 7 with 64)
+    const auto threads = [&](int32_t shift) { return (ceil_div(size, 4) * experts) << shift; };
+    int32_t shift = 0;
+    while (shift < 6 && 4 << shift < by.ranges && threads(shift) < 256 * 512) ++shift;
+    hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(size, 4 * (JOIN_THREADS >> shift)), (unsigned)experts),
+                       dim3(JOIN_THREADS), 0, st, offsets, experts, slots, by.ranges, size, shift, partial, dw);
     GINEX_LAUNCH_CHECK();
     return GINEX_OK;
   });

@@ -286,6 +286,20 @@ def test_weight_gradient(g, rows, top, experts, width, out, dtype, pad, shift):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [7, 32, 64, 65, 129])
+@pytest.mark.parametrize("out", [5, 8, 9, 32, 33, 64, 65, 129])
+def test_weight_gradient_of_narrow_layers(g, width, out, dtype):
+    """Widths at which the tiles change; one expert of 30 000 slots, whose parts many threads add up."""
+    r = routed(g, 33_001, 1, 3, 1, capacity=30_000)
+    x = some((33_001, width), torch.float32, 5)
+    dy = some((33_001, out), dtype, 6)
+    offsets = r.offsets.tolist()
+    dy[offsets[-1]:] = float("nan")
+    got = g.weight_gradient(g.compress(x.cuda()), strided(dy, 3, 1), r)
+    check_weights(got, plain_weights(plain_codes(x)[2], dy, offsets, r.source.cpu()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows", [0, 1, 31, 64, 1000, 4097])
 def test_weight_gradient_of_one_layer(g, rows, dtype):
     x, dy = some((rows, 72), torch.float32, 5), some((rows, 40), dtype, 6)

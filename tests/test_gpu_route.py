@@ -167,7 +167,7 @@ def test_route_refusals(g):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 256, 2, 8), (5, 3, 1, 2), (130, 64, 3, 4), (257, 100, 5, 7), (64, 333, 4, 3),
-          (33, 1025, 8, 16), (2000, 31, 9, 40), (4100, 128, 2, 6)]
+          (33, 1025, 8, 16), (2000, 31, 9, 40), (4100, 128, 2, 6), (40, 9001, 1, 3), (300, 2500, 3, 5), (3, 600, 64, 90)]
 
 
 def random_rows(shape, dtype, seed):
