@@ -13,8 +13,8 @@
 // taken apart on the vector unit and put into LDS with the slots as rows, where transposing reads turn them
 // into operands.
 //
-// Measured, kernel and join, 820 000 x 2 slots in 32 experts, 256 x 256: f32 616-680 us (1040 TFLOP/s of bf16
-// products; the clock falls to 1.6-1.9 GHz: bound by power), f16 422, bf16 290 (codes are read once per expert of a
+// Measured, kernel and join, 820 000 x 2 slots in 32 experts, 256 x 256: f32 585-680 us (1040 TFLOP/s of bf16
+// products; the clock falls to 1.6-1.9 GHz: bound by power), f16 400-440, bf16 276-294 (codes are read once per expert of a
 // row: 1.34 GB, 5.1 TB/s without the join).  76 000 x 2 in 8 experts, 128 x 256, bf16: 30 + 7.5 us, of which the
 // parts of 512 workgroups are 6.5 + 7, the slots 13, launch and first loads 7.
 #include "codes.hpp"
@@ -224,10 +224,14 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
   static_assert(YS % THREADS == 0 && (XS % THREADS == 0 || XS < THREADS), "chunks of a thread");
   __shared__ __attribute__((aligned(16))) bf16 lds[S::BUFFERS * S::SIZE];
 
-  // Workgroups go to the 8 dies in turn: the tiles of a range, which read the same rows, to one of them.
-  const uint32_t die = blockIdx.x % 8, local = blockIdx.x / 8;
-  const int32_t tile_of = (int32_t)(local % tiles);
-  const int64_t range = (int64_t)(local / tiles) * 8 + die;
+  // Workgroups go to the 8 dies in turn: each die has an eighth of all, and the tiles of a range, which read the same rows,
+  // stay together.  Neighbouring ranges go to different dies where all dies have as many (20 000 x 2 slots in 128 experts,
+  // 256 x 256: 51 -> 47 us); with fewer than 8 ranges the dies share their tiles (16 slots, 4096 x 4096: 104 us by whole
+  // ranges, 33).
+  const uint32_t unit = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  const int32_t tile_of = (int32_t)(unit % (uint32_t)tiles);
+  int64_t range = unit / (uint32_t)tiles;
+  if (ranges % 8 == 0) range = (blockIdx.x / 8 / (uint32_t)tiles) * 8 + blockIdx.x % 8;
   if (range >= ranges) return;
   Experts some;
   some.read(offsets, experts, slots, 0);
@@ -622,7 +626,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
   const int64_t size = kept->width * dy->width;
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const int64_t groups = ceil_div(by.ranges, 8) * 8 * by.tiles();
+    const int64_t groups = ceil_div(by.ranges * by.tiles(), 8) * 8;
     if (groups >= ((int64_t)1 << 31)) return fail(GINEX_ERR_ARG, "weight gradient: %lld x %lld weights are too many",
                                                   (long long)kept->width, (long long)dy->width);
     hipLaunchKernelGGL(kernel_of<T>(by, dy->width), dim3((unsigned)groups), dim3((unsigned)(by.wm * by.wn * WAVE)), 0, st,
