@@ -4,8 +4,8 @@
  * the backward pass.  Conventions are those of ginex.h: device pointers unless marked host, the
  * caller owns every buffer, 0 or a negative GINEX_ERR_* code, ginex_last_error(), arguments checked
  * on the host before anything is launched.  Every call here only enqueues on `stream`, allocates
- * nothing and may be captured into a graph.  Equal inputs give equal bits: nothing here depends on
- * the order in which workgroups run.
+ * nothing and may be captured into a graph; what it writes may not overlap its other arrays unless it
+ * says so.  Equal inputs give equal bits: nothing here depends on the order in which workgroups run.
  */
 #ifndef GINEX_TRAIN_H
 #define GINEX_TRAIN_H
@@ -113,7 +113,7 @@ int32_t ginex_activate_backward(const ginex_codes_t* kept /*host struct*/, int32
 /* Weight gradients of one linear layer per expert: with x the rows that the codes stand for,
  * dw[e, c, d] = sum over the slots s of expert e of x[source[s], c] * dy[s, d], products exact, sums in
  * f32 in an order that depends on the shapes and offsets alone; 0 for an expert without rows.  dw is
- * [experts x kept->width x dy->width], contiguous.  dy has rows * top rows, of which those from
+ * [experts x kept->width x dy->width], contiguous, below 2^33 elements an expert.  dy has rows * top rows, of which those from
  * offsets[experts] on are not read.  route NULL: one layer, one expert, slot s holds row s. */
 size_t ginex_weight_gradient_workspace_bytes(int64_t slots, int32_t experts, int64_t width,
                                              int64_t out_width);

@@ -590,6 +590,9 @@ static int32_t check_sizes(int64_t slots, int32_t experts, int64_t width, int64_
   if (experts < 1 || experts > GINEX_MAX_EXPERTS) return fail(GINEX_ERR_ARG, "experts=%d (1..%d)", experts, GINEX_MAX_EXPERTS);
   if (width < 1 || width > GINEX_MAX_WIDTH || out_width < 1 || out_width > GINEX_MAX_WIDTH)
     return fail(GINEX_ERR_ARG, "%lld x %lld weights (1..%d each)", (long long)width, (long long)out_width, GINEX_MAX_WIDTH);
+  // (the second launch has a thread for four, and fewer than 2^32 threads)
+  if (width * out_width >= (int64_t)1 << 33)
+    return fail(GINEX_ERR_ARG, "%lld x %lld weights are too many", (long long)width, (long long)out_width);
   return GINEX_OK;
 }
 
@@ -627,8 +630,6 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
     const int64_t groups = ceil_div(by.ranges * by.tiles(), 8) * 8;
-    if (groups >= ((int64_t)1 << 31)) return fail(GINEX_ERR_ARG, "weight gradient: %lld x %lld weights are too many",
-                                                  (long long)kept->width, (long long)dy->width);
     hipLaunchKernelGGL(kernel_of<T>(by, dy->width), dim3((unsigned)groups), dim3((unsigned)(by.wm * by.wn * WAVE)), 0, st,
                        kept->codes, kept->scales, kept->rows, (int32_t)code_blocks(kept->width), source, offsets, experts,
                        slots, by.ranges, read_rows<T>(dy), (int32_t)kept->width,

@@ -131,6 +131,7 @@ def test_weight_gradient_refusals():
     assert size(-1, 4, 64, 64) == 0 and "slots" in error()
     assert size(10, 0, 64, 64) == 0 and size(10, 4, 0, 64) == 0 and size(10, 4, 64, 0) == 0
     assert size(10, 1025, 64, 64) == 0 and size(0, 4, 64, 64) > 0
+    assert size(10, 4, 1 << 17, 1 << 16) == 0 and "too many" in error()
 
     def call(kept=codes(), r=routing(), dy=rows(20), dw=FAKE, ws=FAKE, ws_bytes=1 << 40):
         return lib.ginex_weight_gradient(ref(kept), ref(r), ref(dy), dw, ws, ws_bytes, None)
