@@ -15,8 +15,8 @@
 //
 // Measured, kernel and join, 820 000 x 2 slots in 32 experts, 256 x 256: f32 585-680 us (1040 TFLOP/s of bf16
 // products; the clock falls to 1.6-1.9 GHz: bound by power), f16 400-440, bf16 276-294 (codes are read once per expert of a
-// row: 1.34 GB, 5.1 TB/s without the join).  76 000 x 2 in 8 experts, 128 x 256, bf16: 30 + 7.5 us, of which the
-// parts of 512 workgroups are 6.5 + 7, the slots 13, launch and first loads 7.
+// row: 1.34 GB, 5.1 TB/s without the join).  76 000 x 2 in 8 experts, 128 x 256, bf16: 27 to 29 + 4.6 us
+// where 98 MB of slots come from HBM (16 at its rate); the parts of 512 workgroups are 17 MB.
 #include "codes.hpp"
 
 namespace ginex {
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __
   }
 }
 
-// The workgroup's shape and the number of ranges by the sizes.
+// The workgroup's shape and the number of ranges by the sizes and the terms that a gradient is cut into.
 struct Tiling {
   int32_t wm, mt, wn, nt;
   int64_t tiles_m, tiles_n;
@@ -532,7 +532,7 @@ struct Tiling {
   int64_t parts() const { return 2 * (int64_t)ranges; }
 };
 
-Tiling tiling_of(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
+Tiling tiling_of(int32_t terms, int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
   Tiling t;
   const auto shape = [&](int wm, int mt, int wn, int nt) {
     t.wm = wm;
@@ -559,6 +559,14 @@ Tiling tiling_of(int64_t slots, int32_t experts, int64_t width, int64_t out_widt
     else if (out_width <= 64) shape(2, 2, 2, 1);
     else if (width <= 64) shape(1, 2, 4, 1);
     else shape(2, 2, 2, 2);
+    // With few slots what costs is the parts that the workgroups leave, and half a tile has half a part (bf16: 76 000 x 2,
+    // 128 x 256 36 -> 32 us, 128 x 128 27 -> 22; but 500 000 x 2, 128 x 100 69 -> 72, 820 000 x 2, 256 x 100 178 -> 217.  f32:
+    // 76 000 x 2, 128 x 128 37 -> 33, but 128 x 256 51 -> 52 and 177 000 x 2, 128 x 128 56 -> 59).  With many tiles there are
+    // few parts (bf16, 2000 x 2, 1024 x 1024: 30 -> 32).
+    if (t.mt == 2 && t.nt == 2 && t.tiles() <= 16 && slots * t.tiles() < (terms == 1 ? 512 : 200) * 1024) {
+      if (terms == 1) shape(1, 2, 4, 1);
+      else shape(2, 2, 2, 1);
+    }
   }
   // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us)
   int64_t ranges = (large ? 256 : 512) / t.tiles();
@@ -599,7 +607,9 @@ static int32_t check_sizes(int64_t slots, int32_t experts, int64_t width, int64_
 extern "C" size_t ginex_weight_gradient_workspace_bytes(int64_t slots, int32_t experts, int64_t width, int64_t out_width) {
   if (check_sizes(slots, experts, width, out_width) != GINEX_OK) return 0;
   Arena a(nullptr);
-  a.take<float>(tiling_of(slots, experts, width, out_width).parts() * width * out_width);
+  const int64_t one = tiling_of(1, slots, experts, width, out_width).parts();
+  const int64_t more = tiling_of(2, slots, experts, width, out_width).parts();
+  a.take<float>((one > more ? one : more) * width * out_width);
   a.take<char>(256);
   return a.used;
 }
@@ -622,7 +632,7 @@ extern "C" int32_t ginex_weight_gradient(const ginex_codes_t* kept, const ginex_
     return fail(GINEX_ERR_ARG, "weight gradient: null or misaligned workspace (256 bytes)");
   if (ws_bytes < need) return fail(GINEX_ERR_WORKSPACE, "weight gradient: workspace %zu bytes, need %zu", ws_bytes, need);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const Tiling by = tiling_of(slots, experts, kept->width, dy->width);
+  const Tiling by = tiling_of(dy->type == GINEX_BF16 ? 1 : 2, slots, experts, kept->width, dy->width);
   const int32_t* const source = route ? route->source : nullptr;
   const int64_t* const offsets = route ? route->offsets : nullptr;
   float* const partial = static_cast<float*>(ws);
