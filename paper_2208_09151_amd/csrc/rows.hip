@@ -22,6 +22,12 @@ namespace ginex {
 namespace {
 
 constexpr int THREADS = 256;
+
+// The workgroup's place: workgroups go to the 8 dies in turn, and `together` gives a die an eighth of all beside each other.
+__device__ __forceinline__ uint32_t place_of(bool together) {
+  return together ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x;
+}
+
 // Rows from offsets[experts] on are cleared, chunk by chunk, by all threads of the launch.
 template <typename T>
 __device__ __forceinline__ void clear_rest(RowsOf<T> out, Width width, Divisor cpr, const int64_t* __restrict__ end,
@@ -52,9 +58,9 @@ template <typename T, int K, bool KEEP>
 __global__ __launch_bounds__(THREADS) void k_dispatch(RowsOf<const T> x, RowsOf<T> out, const int32_t* __restrict__ slot,
                                                       const int64_t* __restrict__ end, int32_t top, int64_t first,
                                                       uint32_t chunks, Divisor cpr, Width width, int64_t slots,
-                                                      bool clear) {
+                                                      bool clear, bool together) {
   constexpr int N = Chunk<T>::N;
-  const uint32_t t = blockIdx.x * THREADS + threadIdx.x;
+  const uint32_t t = place_of(together) * THREADS + threadIdx.x;
   if (t < chunks) {
     const uint32_t row = cpr.of(t);
     const int32_t c = (int32_t)(t - row * cpr.d) * N;
@@ -128,10 +134,10 @@ __global__ __launch_bounds__(BLOCK) void k_combine_backward(RowsOf<const T> dy, 
                                                               const int64_t* __restrict__ end,
                                                               float* __restrict__ dweights, int64_t first, int64_t rows,
                                                               int32_t top, int32_t shift, Divisor cpr, Width width,
-                                                              int64_t slots) {
+                                                              int64_t slots, bool together) {
   constexpr int N = Chunk<T>::N;
   constexpr bool WHOLE = BLOCK > THREADS;
-  const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+  const int64_t t = (int64_t)place_of(together) * BLOCK + threadIdx.x;
   const int32_t group = 1 << shift;
   const bool has_row = t >> shift < rows;
   const int64_t r = first + (has_row ? t >> shift : rows - 1);       // (all lanes take part in the sums)
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(BLOCK) void k_combine_backward(RowsOf<const T> dy, 
         if (lane % WAVE == WAVE - 1) sums[i][lane / WAVE] = s[i] >= 0 ? sum : 0.f;
       }
       __syncthreads();
-      if (lane < K && j + lane < top) {
+      if (has_row && lane < K && j + lane < top) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < BLOCK / WAVE; ++w) sum += sums[lane][w];
@@ -195,10 +201,18 @@ int32_t with_choices(int32_t top, Go go) {
 
 // Whether every row begins and ends with a line of 128 bytes.  Where lines are shared by the slots of different rows,
 // a dispatch stores through the caches, which put them together (41 017 x 8 slots of 1000 bytes: 123 -> 96 us); whole
-// lines go past them (177 000 x 2 slots of 512 bytes: 45 -> 41).
+// lines go past them (177 000 x 2 slots of 512 bytes: 45 -> 41).  And neighbouring rows, whose slots are neighbours as well,
+// go to one die, as its caches are the dies' own (`together`; dispatch of 820 000 x 100 f16, 2 slots a row: 138 -> 107 us, 300 000
+// x 333 f16 135 -> 121, 41 017 x 250 f32, 8: 95 and 96; combine's gradient 239 -> 218, 281 and 286, 170 and 168; where lines
+// are whole, 820 000 x 256 f32, 2: 412 -> 472 and 778 -> 837).
 bool whole_lines(const ginex_rows_t* r) {
   const int64_t bytes = element_bytes(r->type);
   return r->width * bytes % 128 == 0 && r->stride * bytes % 128 == 0 && reinterpret_cast<uintptr_t>(r->data) % 128 == 0;
+}
+
+unsigned blocks_of(int64_t threads, int64_t each, bool together) {
+  const int64_t blocks = ceil_div(threads, each);
+  return (unsigned)(together ? ceil_div(blocks, 8) * 8 : blocks);
 }
 
 // Rows of a launch: chunks are numbered in 31 bits.
@@ -237,10 +251,11 @@ extern "C" int32_t ginex_dispatch(const ginex_routing_t* route, const ginex_rows
       const int64_t cpr = ceil_div(x->width, Chunk<T>::N), step = rows_a_launch(cpr);
       for (int64_t r = 0; r < x->rows; r += step) {
         const int64_t chunks = (x->rows - r < step ? x->rows - r : step) * cpr;
-        const auto kernel = whole_lines(out) ? k_dispatch<T, K, false> : k_dispatch<T, K, true>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(chunks, THREADS)), dim3(THREADS), 0, st,
+        const bool shared = !whole_lines(out);
+        const auto kernel = shared ? k_dispatch<T, K, true> : k_dispatch<T, K, false>;
+        hipLaunchKernelGGL(kernel, dim3(blocks_of(chunks, THREADS, shared)), dim3(THREADS), 0, st,
                            read_rows<T>(x), rows_of<T>(out), route->slot, route->offsets + route->experts, route->top, r,
-                           (uint32_t)chunks, Divisor((uint32_t)cpr), Width::of<T>(x->width), out->rows, r == 0);
+                           (uint32_t)chunks, Divisor((uint32_t)cpr), Width::of<T>(x->width), out->rows, r == 0, shared);
         GINEX_LAUNCH_CHECK();
       }
       return GINEX_OK;
@@ -304,14 +319,15 @@ extern "C" int32_t ginex_combine_backward(const ginex_routing_t* route, const gi
       while (1 << shift < (whole ? WHOLE : WAVE) && (whole || 1 << shift < cpr)) ++shift;
       const auto kernel = whole ? k_combine_backward<T, K, WHOLE> : k_combine_backward<T, K, THREADS>;
       const int threads = whole ? WHOLE : THREADS;
+      const bool shared = !whole_lines(dz);
       // (a launch has fewer than 2^32 threads)
       const int64_t step = ((int64_t)1 << 31) >> shift;
       for (int64_t r = 0; r < dy->rows; r += step) {
         const int64_t rows = dy->rows - r < step ? dy->rows - r : step;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(rows << shift, threads)), dim3((unsigned)threads), 0, st,
+        hipLaunchKernelGGL(kernel, dim3(blocks_of(rows << shift, threads, shared)), dim3((unsigned)threads), 0, st,
                            read_rows<T>(dy), read_rows<T>(z), rows_of<T>(dz), route->slot, weights,
                            route->offsets + route->experts, dweights, r, rows, route->top, shift, Divisor((uint32_t)cpr),
-                           Width::of<T>(dy->width), dz->rows);
+                           Width::of<T>(dy->width), dz->rows, shared);
         GINEX_LAUNCH_CHECK();
       }
       return GINEX_OK;
