@@ -5,9 +5,9 @@
 //   combine, backward   dz[slot(r,j)] = w(r,j) dy[r],  dw(r,j) = <dy[r], z[slot(r,j)]>
 //
 // All of it is rows moved once, bound by HBM.  Work is laid out by row r, not by slot, so that x, y and dy
-// are read or written once whatever the number of choices, and a row's sum stays in registers.  A slot is
-// checked against the slots that exist before it is used: a routing that was not made by ginex_route cannot
-// reach memory outside the arrays.
+// are read or written once whatever the number of choices, and a row's sum stays in registers.  A slot and an
+// offset are checked against the slots that exist before anything is computed from them: a routing that was
+// not made by ginex_route cannot reach memory outside the arrays.
 //
 // Measured (bytes that have to move, over the time of a call among others; a plain copy reaches 6.2 TB/s):
 //   rows x width, slots a row     dispatch        combine         its gradient
@@ -34,9 +34,7 @@ __device__ __forceinline__ void clear_rest(RowsOf<T> out, Width width, Divisor c
                                            int64_t slots, int64_t thread, int64_t threads) {
   constexpr int N = Chunk<T>::N;
   const float zero[N] = {};
-  int64_t kept = *end;
-  kept = kept < 0 ? 0 : kept;
-  for (int64_t s = kept * cpr.d + thread; s < slots * cpr.d; s += threads) {
+  for (int64_t s = first_free_chunk(*end, slots, cpr.d) + thread; s < slots * cpr.d; s += threads) {
     const int64_t row = s / cpr.d;
     store_chunk(out.at(row), (int32_t)(s - row * cpr.d) * N, width, zero);
   }

@@ -4,6 +4,7 @@
 
 #include "common.hpp"
 #include "ginex_train.h"
+#include "slots.hpp"
 
 namespace ginex {
 
