@@ -43,8 +43,10 @@ typedef struct ginex_rows {
 } ginex_rows_t;
 
 /* Where rows go.  Row r has `top` choices of an expert; pair (r, j) is in slot slot[r * top + j], or in
- * none (-1).  The slots of expert e are offsets[e] .. offsets[e+1] - 1, its rows in ascending order of
- * (r, j); source[s] is the row in slot s, -1 for the slots from offsets[experts] on. */
+ * none (-1).  The slots of expert e are offsets[e] .. offsets[e+1] - 1, from offsets[0] = 0 on and ascending, its
+ * rows in ascending order of (r, j); source[s] is the row in slot s, -1 for the slots from offsets[experts] on.
+ * Arrays that hold anything else give results without meaning, but nothing outside the arrays is read or
+ * written for them. */
 typedef struct ginex_routing {
   int64_t rows;
   int32_t top;      /* 1 .. GINEX_MAX_TOP; rows * top < 2^31 */

@@ -23,7 +23,6 @@ namespace ginex {
 namespace {
 
 constexpr int JOIN_THREADS = 256;
-constexpr int STEP = 16;          // the length of a range is a multiple of it
 // Elements from a row in LDS to the next: an odd multiple of 64 bytes, see k_weights.
 constexpr int pitch_of(int columns) { return columns == 32 ? 32 : columns + 32; }
 
@@ -44,34 +43,13 @@ __device__ __forceinline__ void slots_of(const int64_t* __restrict__ offsets, in
                                          int64_t& end) {
   begin = offsets ? offsets[e] : 0;
   end = offsets ? offsets[e + 1] : slots;
-  begin = begin < 0 ? 0 : (begin < slots ? begin : slots);
-  end = end < begin ? begin : (end < slots ? end : slots);
+  bound_slots(slots, begin, end);
 }
 
 // A number that all lanes have, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t v) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v);
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32)) << 32 | lo);
-}
-
-// Slots of a range: the slots that are taken, over `ranges` ranges, rounded up.  (There are fewer than 2^31 slots: divisions
-// are in 32 bits, a quarter of the instructions of 64.)
-__device__ __forceinline__ int64_t range_length(int64_t taken, int64_t slots, int32_t ranges) {
-  taken = taken < 0 ? 0 : (taken < slots ? taken : slots);
-  const uint32_t length = ((uint32_t)(taken + ranges - 1) / (uint32_t)ranges + STEP - 1) / STEP * STEP;
-  return uniform((int64_t)(length > STEP ? length : STEP));
-}
-
-// Ranges begin at multiples of their length, but not near to where an expert begins: there they begin with it, which
-// spares its part in the workspace and the start of another sum.  Both cost about as much as NEAR slots do.
-constexpr int64_t NEAR = 256;
-
-__device__ __forceinline__ int64_t near_of(int64_t length) { return length / 2 < NEAR ? length / 2 : NEAR; }
-
-// Where a range that would begin at `at`, a slot of the expert that has begin .. end - 1, does begin.
-__device__ __forceinline__ int64_t range_begin_of(int64_t at, int64_t length, int64_t begin, int64_t end) {
-  const int64_t near = near_of(length);
-  return at - begin <= near ? begin : end - at <= near ? end : at;
 }
 
 // The slots of 64 experts, one to a lane: what a wave knows of the experts, read in one trip to memory.
@@ -114,10 +92,6 @@ __device__ __forceinline__ int32_t find_range(const int64_t* __restrict__ offset
   }
   return first;
 }
-
-// Where a range leaves its part of an expert that it shares: only the first of its experts can have begun in front of
-// it, and only the last can go on behind it.
-__device__ __forceinline__ int64_t part_of(int64_t range, bool first) { return 2 * range + (first ? 1 : 0); }
 
 // Waits for this wave's LDS accesses and for the other waves, not for loads from HBM that are under way.
 __device__ __forceinline__ void lds_barrier() {
@@ -235,7 +209,7 @@ __global__ __launch_bounds__(WM* WN* WAVE, 2) void k_weights(
   if (range >= ranges) return;
   Experts some;
   some.read(offsets, experts, slots, 0);
-  const int64_t length = range_length(offsets ? offsets[experts] : slots, slots, ranges);
+  const int64_t length = uniform(range_length(offsets ? offsets[experts] : slots, slots, ranges));
   const int32_t c0 = tile_of % tiles_m * TM, d0 = tile_of / tiles_m * TN;
 
   // its ends, and the first expert that has slots in it
@@ -479,19 +453,15 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_weights_join(const int64_t* __
   const int32_t mine = blockIdx.y;
   int64_t begin, end;
   slots_of(offsets, mine, slots, begin, end);
-  const int64_t length = range_length(offsets ? offsets[experts] : slots, slots, ranges);
-  // the ranges that begin inside the expert; the one in front of them has its first part
-  const int64_t near = near_of(length);
-  const int64_t first = (uint32_t)(begin + near) / (uint32_t)length + 1;
-  int64_t last = end > near ? (uint32_t)(end - near - 1) / (uint32_t)length : 0;
+  const int64_t length = uniform(range_length(offsets ? offsets[experts] : slots, slots, ranges));
+  const auto [first, last] = shared_by(begin, end, length, ranges);
   if (end > begin && last < first) return;
-  last = last < ranges ? last : ranges - 1;
   const int32_t lanes = JOIN_THREADS >> shift, lane = threadIdx.x % lanes, group = threadIdx.x / lanes;
   const int64_t i = ((int64_t)blockIdx.x * lanes + lane) * 4;
   four sum = {};
   if (end > begin && i < size) {
     // range first - 1 and those that follow; only what the first of them has is in its second place
-    const int64_t share = (last - first + 2 + (1 << shift) - 1) >> shift;
+    const int32_t share = (last - first + 2 + (1 << shift) - 1) >> shift;
     int64_t r = first - 1 + group * share;
     const int64_t behind = r + share < last + 1 ? r + share : last + 1;
     const float* const at = partial + i;
@@ -529,7 +499,7 @@ struct Tiling {
   int64_t tiles_m, tiles_n;
   int32_t ranges;
   int64_t tiles() const { return tiles_m * tiles_n; }
-  int64_t parts() const { return 2 * (int64_t)ranges; }
+  int64_t parts() const { return parts_of(ranges); }
 };
 
 Tiling tiling_of(int32_t terms, int64_t slots, int32_t experts, int64_t width, int64_t out_width) {

@@ -2,6 +2,7 @@
 them stays inside the arrays (no GPU)."""
 import ctypes as C
 import os
+import random
 import shutil
 import subprocess
 
@@ -24,6 +25,8 @@ def rules(tmp_path_factory):
     lib = C.CDLL(lib)
     lib.rules_first_free_chunk.restype = i64
     lib.rules_first_free_chunk.argtypes = [i64, i64, C.c_uint32]
+    lib.rules_ranges.restype = C.c_int32
+    lib.rules_ranges.argtypes = [C.POINTER(i64), C.c_int32, i64, C.c_int32, C.c_int32]
     return lib
 
 
@@ -32,3 +35,34 @@ def rules(tmp_path_factory):
 @pytest.mark.parametrize("end", FOREIGN)
 def test_rows_are_cleared_from_a_slot_on_that_exists(rules, end, slots, chunks):
     assert rules.rules_first_free_chunk(end, slots, chunks) == min(max(end, 0), slots) * chunks
+
+
+def ranges(rules, offsets, slots, count, made_here):
+    return rules.rules_ranges((i64 * len(offsets))(*offsets), len(offsets) - 1, slots, count, int(made_here))
+
+
+def test_ranges_share_their_slots_out(rules):
+    """Offsets as route() makes them: every slot once, and the parts that are added up are those that were left."""
+    rng = random.Random(1)
+    for _ in range(3000):
+        experts, count = rng.choice([1, 2, 8, 63, 64, 65, 200]), rng.choice([1, 2, 3, 7, 8, 32, 128, 512])
+        most = rng.choice([0, 1, 20, 300, 5000, 10 ** 6])
+        offsets = [0]
+        for _ in range(experts):
+            offsets.append(offsets[-1] + (0 if rng.random() < 0.3 else rng.randrange(most + 1)))
+        slots = offsets[-1] + rng.choice([0, 1, 1000])
+        assert ranges(rules, offsets, slots, count, True) == 0, (offsets, slots, count)
+    assert ranges(rules, [0, (1 << 31) - 1], (1 << 31) - 1, 512, True) == 0
+
+
+def test_ranges_of_offsets_made_elsewhere(rules):
+    """Offsets that descend, or that no slot has: no slot and no part that is not there."""
+    assert ranges(rules, [0, 1000, 2000, 16], 2048, 16, False) == 0
+    rng = random.Random(2)
+    for _ in range(20_000):
+        experts, count = rng.choice([1, 2, 3, 8, 65, 130]), rng.choice([1, 2, 3, 16, 64, 512])
+        slots = rng.choice([0, 1, 16, 100, 2048, 10 ** 6, (1 << 31) - 1])
+        offsets = [rng.choice(FOREIGN) if rng.random() < 0.2 else rng.randrange(slots + 1) for _ in range(experts + 1)]
+        if rng.random() < 0.5:
+            offsets[:-1] = sorted(offsets[:-1])
+        assert ranges(rules, offsets, slots, count, False) == 0, (offsets, slots, count)
