@@ -274,6 +274,7 @@ def restore(kept: Compressed, dtype=torch.float32, out=None):
     """ginex_restore: the values that the codes stand for."""
     if dtype not in _TYPES:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
+    _here(kept.codes, "kept")
     out, to = _out(out, "out", (kept.rows, kept.width), dtype, kept.codes)
     _check(_lib.load().ginex_restore(C.byref(_with(kept, "kept", out)._desc), C.byref(to), _stream()))
     return out
