@@ -12,6 +12,7 @@
 #include <cstdio>
 
 #include "ginex.h"
+#include "sizes.hpp"
 
 namespace ginex {
 
@@ -45,8 +46,6 @@ struct Arena {
     return p;
   }
 };
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- device helpers -------------------------------------------------------------
 

@@ -1,4 +1,4 @@
-// The rules of csrc/slots.hpp behind a C ABI, for tests/test_slot_rules.py (test infrastructure, host code only).
+// The rules of csrc/slots.hpp and tiling.hpp behind a C ABI, for tests/test_slot_rules.py (test infrastructure, host code only).
 #include <cstdio>
 #include <map>
 #include <set>
@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "slots.hpp"
+#include "tiling.hpp"
 
 using namespace ginex;
 
@@ -75,4 +76,11 @@ extern "C" int32_t rules_ranges(const int64_t* offsets, int32_t experts, int64_t
     }
   }
   return made_here && read.size() != left.size() ? 9 : 0;
+}
+
+// The workgroup's shape (wm, mt, wn, nt), the tiles and the ranges of a weight gradient.
+extern "C" void rules_tiling(int32_t terms, int64_t slots, int32_t experts, int64_t width, int64_t out_width, int32_t* out) {
+  const Tiling t = tiling_of(terms, slots, experts, width, out_width);
+  const int32_t found[6] = {t.wm, t.mt, t.wn, t.nt, (int32_t)t.tiles(), t.ranges};
+  for (int i = 0; i < 6; ++i) out[i] = found[i];
 }

@@ -1,5 +1,5 @@
-"""The rules of csrc/slots.hpp, compiled for the CPU: whatever offsets a routing holds, what the kernels compute from
-them stays inside the arrays (no GPU)."""
+"""The rules of csrc/slots.hpp and tiling.hpp, compiled for the CPU: whatever offsets a routing holds, what the kernels
+compute from them stays inside the arrays; which shape a weight gradient's sizes reach (no GPU)."""
 import ctypes as C
 import os
 import random
@@ -7,6 +7,8 @@ import shutil
 import subprocess
 
 import pytest
+
+import weight_shapes
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 i64 = C.c_int64
@@ -66,3 +68,25 @@ def test_ranges_of_offsets_made_elsewhere(rules):
         if rng.random() < 0.5:
             offsets[:-1] = sorted(offsets[:-1])
         assert ranges(rules, offsets, slots, count, False) == 0, (offsets, slots, count)
+
+
+def tiling(rules, dtype, slots, experts, width, out):
+    found = (C.c_int32 * 6)()
+    rules.rules_tiling(1 if dtype == "bf16" else 2, i64(slots), experts, i64(width), i64(out), found)
+    return tuple(found)
+
+
+@pytest.mark.parametrize("shape, sizes, width, out, dtype", weight_shapes.PARAMS, ids=weight_shapes.IDS)
+def test_sizes_reach_the_shape_that_they_are_there_for(rules, shape, sizes, width, out, dtype):
+    found = tiling(rules, dtype, sum(sizes) + weight_shapes.EMPTY, len(sizes), width, out)
+    assert found[:4] == shape
+
+
+def test_every_shape_has_sizes_of_every_type(rules):
+    shapes = set()
+    for dtype in weight_shapes.TYPES:
+        for slots in (1, 1000, 50_000, 300_000, 2_000_000):
+            for width in (5, 40, 100, 200, 700):
+                for out in (5, 20, 40, 100, 200, 700):
+                    shapes.add((tiling(rules, dtype, slots, 8, width, out)[:4], dtype))
+    assert shapes == {(shape, dtype) for shape, _, _, _, dtype in weight_shapes.PARAMS}
