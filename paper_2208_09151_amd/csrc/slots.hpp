@@ -31,9 +31,10 @@ GINEX_BOTH void bound_slots(int64_t slots, int64_t& begin, int64_t& end) {
 }
 
 // Slots of a range: the slots that are taken, over `ranges` ranges, rounded up.  (There are fewer than 2^31 slots: divisions
-// are in 32 bits, a quarter of the instructions of 64.)
+// are in 32 bits, a quarter of the instructions of 64.)  A single range has all slots, whatever a routing says is taken: no
+// expert can go on behind it.
 GINEX_BOTH int64_t range_length(int64_t taken, int64_t slots, int32_t ranges) {
-  taken = taken < 0 ? 0 : (taken < slots ? taken : slots);
+  taken = ranges == 1 ? slots : inside(taken, slots);
   const uint32_t length = ((uint32_t)(taken + ranges - 1) / (uint32_t)ranges + STEP - 1) / STEP * STEP;
   return (int64_t)(length > STEP ? length : STEP);
 }
@@ -51,9 +52,9 @@ GINEX_BOTH int64_t range_begin_of(int64_t at, int64_t length, int64_t begin, int
 }
 
 // Where a range leaves its part of an expert that it shares: only the first of its experts can have begun in front of
-// it, and only the last can go on behind it.
+// it, and only the last can go on behind it.  One range shares no expert and needs no room for parts.
 GINEX_BOTH int64_t part_of(int64_t range, bool first) { return 2 * range + (first ? 1 : 0); }
-GINEX_BOTH int64_t parts_of(int64_t ranges) { return 2 * ranges; }
+GINEX_BOTH int64_t parts_of(int64_t ranges) { return ranges > 1 ? 2 * ranges : 0; }
 
 // The ranges first .. last that begin inside the expert that has begin .. end - 1; with last < first it lies in one range,
 // else range first - 1 has its first part.  Offsets that do not ascend may put an expert behind all ranges: last is a range
