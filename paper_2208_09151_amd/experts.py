@@ -18,7 +18,7 @@ import sys
 
 import torch
 
-from .training import (activate, activate_backward, combine, combine_backward, compress, dispatch,
+from .training import (_first_derivative, activate, activate_backward, combine, combine_backward, compress, dispatch,
                        dispatch_backward, route, weight_gradient)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -45,6 +45,7 @@ class ExpertLinear(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_first_derivative
     def backward(ctx, grad):
         weight, = ctx.saved_tensors
         grad = grad.contiguous()
@@ -69,6 +70,7 @@ class Activation(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_first_derivative
     def backward(ctx, grad):
         return activate_backward(ctx.kept, grad.contiguous(), ctx.name), None
 
@@ -83,6 +85,7 @@ class Combine(torch.autograd.Function):
         return combine(z, r, weights)
 
     @staticmethod
+    @_first_derivative
     def backward(ctx, grad):
         z, weights = ctx.saved_tensors
         dz, dweights = combine_backward(grad.contiguous(), z, ctx.r, weights)

@@ -8,6 +8,7 @@ returns at once.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from dataclasses import dataclass, field
 
 import torch
@@ -94,6 +95,18 @@ def _out(out, what, shape, dtype, like):
     if tuple(out.shape) != shape:
         raise ValueError(f"{what}: expected shape {shape}, got {tuple(out.shape)}")
     return out, _rows(out, what)
+
+
+def _first_derivative(backward):
+    """For the backward of an autograd function: what the kernels give is no graph, and in a gradient that is to be
+    differentiated it would count as a constant.  (autograd's own once_differentiable notices only where the incoming
+    gradient requires one.)"""
+    @functools.wraps(backward)
+    def checked(ctx, *grads):
+        if torch.is_grad_enabled():
+            raise RuntimeError(f"{type(ctx).__name__}: there is no second derivative (create_graph=True asks for one)")
+        return backward(ctx, *grads)
+    return checked
 
 
 def _activation(name):
