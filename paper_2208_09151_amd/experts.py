@@ -18,7 +18,7 @@ import sys
 
 import torch
 
-from .training import (_first_derivative, activate, activate_backward, combine, combine_backward, compress, dispatch,
+from .training import (Activation, Combine, _first_derivative, activate, combine, compress, dispatch,  # noqa: F401
                        dispatch_backward, route, weight_gradient)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -60,38 +60,6 @@ class ExpertLinear(torch.autograd.Function):
         return dx, dw, None, None
 
 
-class Activation(torch.autograd.Function):
-    """An activation whose input is kept in 8 bits for its gradient."""
-
-    @staticmethod
-    def forward(ctx, x, name):
-        y, ctx.kept = activate(x, name)
-        ctx.name = name
-        return y
-
-    @staticmethod
-    @_first_derivative
-    def backward(ctx, grad):
-        return activate_backward(ctx.kept, grad.contiguous(), ctx.name), None
-
-
-class Combine(torch.autograd.Function):
-    """The slots' rows back to their rows, weighted."""
-
-    @staticmethod
-    def forward(ctx, z, weights, r):
-        ctx.r = r
-        ctx.save_for_backward(z, weights)
-        return combine(z, r, weights)
-
-    @staticmethod
-    @_first_derivative
-    def backward(ctx, grad):
-        z, weights = ctx.saved_tensors
-        dz, dweights = combine_backward(grad.contiguous(), z, ctx.r, weights)
-        return dz, dweights, None
-
-
 class ExpertLayer(torch.nn.Module):
     """``top`` of ``experts`` linear layers with an activation ("relu", "silu", "gelu") for every row.
     ``capacity``: rows an expert takes at most, as a multiple of its even share; rows beyond it do without."""
@@ -109,8 +77,8 @@ class ExpertLayer(torch.nn.Module):
             math.ceil(x.shape[0] * self.top / self.experts * self.capacity)
         r = route(chosen, self.experts, capacity=most)
         ends = r.offsets.tolist()           # (the products need them on the host)
-        y = Activation.apply(ExpertLinear.apply(x, self.weight, r, ends), self.activation)
-        return Combine.apply(y, weights, r)
+        y, _ = activate(ExpertLinear.apply(x, self.weight, r, ends), self.activation)
+        return combine(y, r, weights)
 
 
 class Classifier(torch.nn.Module):

@@ -4,6 +4,9 @@ sorted by expert and back, activations kept in 8 bits, and their use in the back
 Tensors in, tensors out, nothing computed here.  Rows are f32, bf16 or f16 tensors of two dimensions whose
 last one is dense; any stride from row to row will do.  Every call enqueues on the current stream and
 returns at once.
+
+dispatch, combine and activate keep autograd's graph where it is recorded; their gradients are the calls that are made for
+them.  Results of those, and codes, are constants to autograd.
 """
 from __future__ import annotations
 
@@ -184,9 +187,64 @@ def route(chosen, experts, capacity=None, workspace=None) -> Route:
     return made
 
 
+def _recorded(out):
+    """A call that autograd records makes its result."""
+    if out is not None:
+        raise ValueError("out: autograd records this call, whose result has to be a new tensor")
+
+
+class Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, r):
+        ctx.r = r
+        return dispatch(x, r)
+
+    @staticmethod
+    @_first_derivative
+    def backward(ctx, grad):
+        return dispatch_backward(grad.contiguous(), ctx.r), None
+
+
+class Combine(torch.autograd.Function):
+    """The slots' rows back to their rows, weighted."""
+
+    @staticmethod
+    def forward(ctx, z, weights, r):
+        ctx.r = r
+        ctx.save_for_backward(z, weights)
+        return combine(z, r, weights)
+
+    @staticmethod
+    @_first_derivative
+    def backward(ctx, grad):
+        z, weights = ctx.saved_tensors
+        dz, dweights = combine_backward(grad.contiguous(), z, ctx.r, weights)
+        return dz, dweights, None
+
+
+class Activation(torch.autograd.Function):
+    """An activation whose input is kept in 8 bits for its gradient; the codes are put into the list ``made``."""
+
+    @staticmethod
+    def forward(ctx, x, name, made=None):
+        y, ctx.kept = activate(x, name)
+        ctx.name = name
+        if made is not None:
+            made.append(ctx.kept)
+        return y
+
+    @staticmethod
+    @_first_derivative
+    def backward(ctx, grad):
+        return activate_backward(ctx.kept, grad.contiguous(), ctx.name), None, None
+
+
 def dispatch(x, route: Route, out=None):
     """ginex_dispatch: the rows of ``x`` in their slots, [rows * top, width]; slots without a row are 0."""
     desc = _rows(x, "x")
+    if x.requires_grad and torch.is_grad_enabled():
+        _recorded(out)
+        return Dispatch.apply(x, route)
     out, to = _out(out, "out", (route.source.numel(), desc.width), x.dtype, x)
     _check(_lib.load().ginex_dispatch(C.byref(_with(route, "route", x)._desc), C.byref(desc), C.byref(to),
                                       _stream()))
@@ -205,6 +263,9 @@ def _combine(z, route, weights, out):
 def combine(z, route: Route, weights, out=None):
     """ginex_combine: y[r] = sum_j weights[r, j] z[slot[r, j]]; ``weights`` f32 [rows, top]."""
     _dense(weights, "weights", (route.rows, route.top), torch.float32)
+    if torch.is_grad_enabled() and (weights.requires_grad or getattr(z, "requires_grad", False)):
+        _recorded(out)
+        return Combine.apply(z, weights, route)
     return _combine(z, route, weights, out)
 
 
@@ -279,6 +340,10 @@ def activate(x, activation, out=None):
     backward pass.  ``out`` may be ``x``."""
     kind = _activation(activation)
     desc = _rows(x, "x")
+    if x.requires_grad and torch.is_grad_enabled():
+        _recorded(out)
+        made = []
+        return Activation.apply(x, activation, made), made[0]
     out, to = _out(out, "out", (desc.rows, desc.width), x.dtype, x)
     return out, _compress(x, desc, kind, to)
 

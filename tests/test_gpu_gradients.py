@@ -27,3 +27,55 @@ def test_second_derivatives_are_refused(activation, by):
         torch.autograd.grad(first.sum(), at)
     first, = torch.autograd.grad(layer(x).sum() + (at ** 3).sum(), at)
     assert not first.requires_grad
+
+
+def routed(g, rows, top, experts, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    chosen = torch.randint(-1, experts, (rows, top), generator=gen, device="cuda")
+    return g.route(chosen, experts, capacity=max(1, rows * top // experts)), gen
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_results_keep_the_graph(g, dtype):
+    """dispatch, combine and activate of tensors that require a gradient: the gradients of the calls that are made for it."""
+    r, gen = routed(g, 70, 3, 5)
+    x = torch.randn((70, 33), generator=gen, device="cuda").to(dtype).requires_grad_()
+    w = torch.randn((70, 3), generator=gen, device="cuda").requires_grad_()
+    dy = torch.randn((70, 33), generator=gen, device="cuda").to(dtype)
+    z = g.dispatch(x, r)
+    h, kept = g.activate(z, "silu")
+    y = g.combine(h, r, w)
+    y.backward(dy)
+    with torch.no_grad():
+        z2 = g.dispatch(x, r)
+        h2, kept2 = g.activate(z2, "silu")
+        y2 = g.combine(h2, r, w)
+        dh, dw = g.combine_backward(dy, h2, r, w)
+        dx = g.dispatch_backward(g.activate_backward(kept2, dh, "silu"), r)
+    assert not (z2.requires_grad or h2.requires_grad or y2.requires_grad)
+    assert torch.equal(y, y2) and torch.equal(kept.codes, kept2.codes) and torch.equal(kept.scales, kept2.scales)
+    assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw)
+
+
+@pytest.mark.parametrize("needs", ["z", "weights"])
+def test_one_of_two_gradients(g, needs):
+    r, gen = routed(g, 70, 3, 5)
+    z = torch.randn((210, 20), generator=gen, device="cuda").requires_grad_(needs == "z")
+    w = torch.randn((70, 3), generator=gen, device="cuda").requires_grad_(needs == "weights")
+    g.combine(z, r, w).sum().backward()         # (a gradient of stride 0)
+    dz, dw = g.combine_backward(torch.ones((70, 20), device="cuda"), z.detach(), r, w.detach())
+    assert torch.equal(z.grad, dz) if needs == "z" else z.grad is None
+    assert torch.equal(w.grad, dw) if needs == "weights" else w.grad is None
+
+
+def test_a_result_that_is_recorded_is_a_new_tensor(g):
+    r, gen = routed(g, 70, 3, 5)
+    x = torch.randn((70, 20), generator=gen, device="cuda").requires_grad_()
+    w = torch.randn((70, 3), generator=gen, device="cuda")
+    z = torch.empty((210, 20), device="cuda")
+    for call in (lambda: g.dispatch(x, r, out=z), lambda: g.combine(z, r, w.requires_grad_(), out=torch.empty_like(w)),
+                 lambda: g.activate(x, "relu", out=x), lambda: g.activate(x, "relu", out=torch.empty_like(x))):
+        with pytest.raises(ValueError, match="out"):
+            call()
+    with torch.no_grad():
+        assert g.dispatch(x, r, out=z) is z
