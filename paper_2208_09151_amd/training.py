@@ -352,7 +352,8 @@ def restore(kept: Compressed, dtype=torch.float32, out=None):
     """ginex_restore: the values that the codes stand for."""
     if dtype not in _TYPES:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    _here(kept.codes, "kept")
+    if out is None and (kept._device < 0 or kept._device != torch.cuda.current_device()):
+        raise ValueError(f"kept: on {kept.codes.device}, which is not the current GPU")
     out, to = _out(out, "out", (kept.rows, kept.width), dtype, kept.codes)
     _check(_lib.load().ginex_restore(C.byref(_with(kept, "kept", out)._desc), C.byref(to), _stream()))
     return out
