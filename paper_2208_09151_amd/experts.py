@@ -18,8 +18,8 @@ import sys
 
 import torch
 
-from .training import (Activation, Combine, _first_derivative, activate, combine, compress, dispatch,  # noqa: F401
-                       dispatch_backward, route, weight_gradient)
+from .training import (Activation, Combine, Compressed, Route, _first_derivative, activate, combine,  # noqa: F401
+                       compress, dispatch, dispatch_backward, route, weight_gradient)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -40,23 +40,25 @@ class ExpertLinear(torch.autograd.Function):
         for e, a, b in _spans(ends):
             torch.mm(rows[a:b], weight[e], out=out[a:b])
         out[ends[-1]:].zero_()
-        ctx.kept, ctx.r, ctx.ends = compress(x), r, ends
-        ctx.save_for_backward(weight)
+        kept = compress(x)
+        ctx.width, ctx.ends = kept.width, ends
+        ctx.save_for_backward(weight, kept.codes, kept.scales, *r._tensors())
         return out
 
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        weight, = ctx.saved_tensors
+        weight, codes, scales, *route = ctx.saved_tensors
+        r = Route._made(*route)
         grad = grad.contiguous()
         dx = dw = None
         if ctx.needs_input_grad[1]:
-            dw = weight_gradient(ctx.kept, grad, ctx.r).to(weight.dtype)
+            dw = weight_gradient(Compressed._made(codes, scales, ctx.width), grad, r).to(weight.dtype)
         if ctx.needs_input_grad[0]:
             drows = torch.empty((grad.shape[0], weight.shape[1]), dtype=grad.dtype, device=grad.device)
             for e, a, b in _spans(ctx.ends):
                 torch.mm(grad[a:b], weight[e].t(), out=drows[a:b])
-            dx = dispatch_backward(drows, ctx.r)
+            dx = dispatch_backward(drows, r)
         return dx, dw, None, None
 
 

@@ -149,6 +149,9 @@ class Route:
             rows, top, offsets.numel() - 1, offsets.data_ptr(), slot.data_ptr(), source.data_ptr()))
         return made
 
+    def _tensors(self):
+        return self.offsets, self.slot, self.source
+
     @property
     def rows(self) -> int:
         return self.slot.shape[0]
@@ -194,15 +197,17 @@ def _recorded(out):
 
 
 class Dispatch(torch.autograd.Function):
+    """Rows to their slots."""
+
     @staticmethod
     def forward(ctx, x, r):
-        ctx.r = r
+        ctx.save_for_backward(*r._tensors())
         return dispatch(x, r)
 
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        return dispatch_backward(grad.contiguous(), ctx.r), None
+        return dispatch_backward(grad.contiguous(), Route._made(*ctx.saved_tensors)), None
 
 
 class Combine(torch.autograd.Function):
@@ -210,15 +215,14 @@ class Combine(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, z, weights, r):
-        ctx.r = r
-        ctx.save_for_backward(z, weights)
+        ctx.save_for_backward(z, weights, *r._tensors())
         return combine(z, r, weights)
 
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        z, weights = ctx.saved_tensors
-        dz, dweights = combine_backward(grad.contiguous(), z, ctx.r, weights)
+        z, weights, *route = ctx.saved_tensors
+        dz, dweights = combine_backward(grad.contiguous(), z, Route._made(*route), weights)
         return dz, dweights, None
 
 
@@ -227,16 +231,18 @@ class Activation(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, name, made=None):
-        y, ctx.kept = activate(x, name)
-        ctx.name = name
+        y, kept = activate(x, name)
+        ctx.save_for_backward(kept.codes, kept.scales)
+        ctx.width, ctx.name = kept.width, name
         if made is not None:
-            made.append(ctx.kept)
+            made.append(kept)
         return y
 
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        return activate_backward(ctx.kept, grad.contiguous(), ctx.name), None, None
+        kept = Compressed._made(*ctx.saved_tensors, ctx.width)
+        return activate_backward(kept, grad.contiguous(), ctx.name), None, None
 
 
 def dispatch(x, route: Route, out=None):

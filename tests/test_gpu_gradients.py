@@ -79,3 +79,37 @@ def test_a_result_that_is_recorded_is_a_new_tensor(g):
             call()
     with torch.no_grad():
         assert g.dispatch(x, r, out=z) is z
+
+
+def test_what_is_saved_goes_through_the_hooks(g):
+    """Codes and routes as well: moved to the host and back between forward and backward pass, they give the same."""
+    from paper_2208_09151_amd.experts import ExpertLayer
+    torch.manual_seed(2)
+    layer = ExpertLayer(64, 32, 4, 2, "gelu", 1.0).cuda()
+    x = torch.randn((50, 64), device="cuda", requires_grad=True)
+    want = torch.autograd.grad(layer(x).sum(), [x, *layer.parameters()])
+    moved = []
+
+    def pack(t):
+        moved.append(t.dtype)
+        return t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        loss = layer(x).sum()
+    got = torch.autograd.grad(loss, [x, *layer.parameters()])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # codes of the rows and of the activations' inputs, the route of either pass
+    assert moved.count(torch.int8) == 2 and moved.count(torch.uint8) == 2 and torch.int32 in moved
+
+
+def test_codes_and_routes_that_have_changed_are_noticed(g):
+    r, gen = routed(g, 70, 3, 5)
+    x = torch.randn((70, 20), generator=gen, device="cuda").requires_grad_()
+    y, kept = g.activate(x, "relu")
+    kept.codes.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    y = g.dispatch(x, r)
+    r.slot.fill_(-1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
