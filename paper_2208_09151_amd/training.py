@@ -89,6 +89,12 @@ def _rows(t, what):
     return RowsDesc(t.data_ptr(), n, width, stride, kind)
 
 
+def _overwritten(t):
+    """autograd hears of it, which may have kept the tensor."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 def _out(out, what, shape, dtype, like):
     """A tensor for the result and its descriptor."""
     if out is None:
@@ -97,7 +103,9 @@ def _out(out, what, shape, dtype, like):
     _here(out, what, dtype)
     if tuple(out.shape) != shape:
         raise ValueError(f"{what}: expected shape {shape}, got {tuple(out.shape)}")
-    return out, _rows(out, what)
+    desc = _rows(out, what)
+    _overwritten(out)
+    return out, desc
 
 
 def _first_derivative(backward):
@@ -384,8 +392,10 @@ def weight_gradient(kept: Compressed, grad, route: Route = None, out=None, works
     shape = (kept.width, grad.shape[1])
     if route is not None:
         shape = (route.experts, *shape)
-    out = _dense(out, "out", shape, torch.float32) if out is not None \
-        else torch.empty(shape, dtype=torch.float32, device=grad.device)
+    if out is not None:
+        _overwritten(_dense(out, "out", shape, torch.float32))
+    else:
+        out = torch.empty(shape, dtype=torch.float32, device=grad.device)
     need = lib.ginex_weight_gradient_workspace_bytes(grad.shape[0], shape[0] if route is not None else 1,
                                                      kept.width, grad.shape[1])
     if need == 0:

@@ -113,3 +113,25 @@ def test_codes_and_routes_that_have_changed_are_noticed(g):
     r.slot.fill_(-1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+def test_a_result_written_into_a_saved_tensor_is_noticed(g):
+    """Every call with an output of the caller's counts as one in place."""
+    r, gen = routed(g, 70, 3, 5)
+    x = torch.randn((70, 20), generator=gen, device="cuda")
+    z = torch.randn((210, 20), generator=gen, device="cuda")
+    w = torch.randn((70, 3), generator=gen, device="cuda")
+    kept = g.compress(x)
+    dw = torch.empty((20, 20), device="cuda")
+    for call, out in [(lambda t: g.dispatch(x, r, out=t), z), (lambda t: g.combine(z, r, w, out=t), x),
+                      (lambda t: g.dispatch_backward(z, r, out=t), x), (lambda t: g.activate(x, "relu", out=t), x),
+                      (lambda t: g.restore(kept, out=t), x), (lambda t: g.activate_backward(kept, x, "relu", out=t), x),
+                      (lambda t: g.weight_gradient(kept, x, out=t), dw)]:
+        by = torch.ones_like(out, requires_grad=True)
+        loss = (by * out).sum()                 # keeps `out` for the gradient of `by`
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        out = torch.empty_like(z)
+        assert g.dispatch(x, r, out=out) is out
