@@ -114,10 +114,9 @@ def train(config=1, steps=40, hidden=64, experts=8, classes=8, rate=0.02, report
     cfg = w.cfg
     cache = ginex.FeatureCache(w.features, cfg.cap)
     nodes = train_nodes(cfg.num_nodes, cfg.train_frac, cfg.seed, "cuda")
-    gen_state = torch.random.get_rng_state()
-    torch.manual_seed(0)
-    model = Classifier(cfg.feat_dim, hidden, classes, experts).cuda()
-    torch.random.set_rng_state(gen_state)
+    with torch.random.fork_rng(devices=[]):
+        torch.random.default_generator.manual_seed(0)       # (torch.manual_seed would seed the GPU's, too)
+        model = Classifier(cfg.feat_dim, hidden, classes, experts).cuda()
     adam = torch.optim.Adam(model.parameters(), lr=rate)
     losses = []
     while len(losses) < steps:

@@ -135,3 +135,14 @@ def test_a_result_written_into_a_saved_tensor_is_noticed(g):
     with torch.inference_mode():
         out = torch.empty_like(z)
         assert g.dispatch(x, r, out=out) is out
+
+
+def test_a_training_run_leaves_the_random_numbers_alone():
+    from paper_2208_09151_amd.experts import train
+    torch.manual_seed(3)
+    before = torch.get_rng_state(), torch.cuda.get_rng_state()
+    first = train(config=1, steps=1, report=None)
+    assert torch.equal(torch.get_rng_state(), before[0]) and torch.equal(torch.cuda.get_rng_state(), before[1])
+    torch.manual_seed(4)
+    # the same weights: the neighbours' sums alone are added up in any order
+    assert abs(train(config=1, steps=1, report=None)[0] - first[0]) < 1e-4
