@@ -113,8 +113,9 @@ int32_t ginex_activate_backward(const ginex_codes_t* kept /*host struct*/, int32
                                 const ginex_rows_t* dx /*host struct*/, void* stream);
 
 /* Weight gradients of one linear layer per expert: with x the rows that the codes stand for,
- * dw[e, c, d] = sum over the slots s of expert e of x[source[s], c] * dy[s, d], products exact, sums in
- * f32 in an order that depends on the shapes and offsets alone; 0 for an expert without rows.  dw is
+ * dw[e, c, d] = sum over the slots s of expert e of x[source[s], c] * dy[s, d], products exact (an f32 dy
+ * below 2^-110 counts without what it has below 2^-133), sums in f32 in an order that depends on the shapes
+ * and offsets alone; 0 for an expert without rows.  dw is
  * [experts x kept->width x dy->width], contiguous, below 2^33 elements an expert.  dy has rows * top rows, of which those from
  * offsets[experts] on are not read.  route NULL: one layer, one expert, slot s holds row s. */
 size_t ginex_weight_gradient_workspace_bytes(int64_t slots, int32_t experts, int64_t width,

@@ -8,8 +8,8 @@
 // ranges share leaves its parts in the workspace, and a second launch adds them up in their order, so that
 // equal inputs give equal bits.
 //
-// Codes are exact in bf16, and so are the terms that a gradient is cut into: all products are exact, and the
-// sums are the matrix cores' f32.  Codes and gradients come from HBM into registers two steps ahead, are
+// Codes are exact in bf16, and so are the terms that a gradient is cut into: all products are exact (an f32 gradient
+// below 2^-110 loses what it has below 2^-133, bf16's least bit), and the sums are the matrix cores' f32.  Codes and gradients come from HBM into registers two steps ahead, are
 // taken apart on the vector unit and put into LDS with the slots as rows, where transposing reads turn them
 // into operands.
 //
@@ -31,7 +31,8 @@ typedef short half_words __attribute__((ext_vector_type(4)));
 typedef bf16 fragment __attribute__((ext_vector_type(8)));
 typedef float tile __attribute__((ext_vector_type(16)));
 
-// A gradient as a sum of bf16 numbers, exactly: the significand's bits eight at a time (bf16 has 8, f16 11, f32 24).
+// A gradient as a sum of bf16 numbers: the significand's bits eight at a time (bf16 has 8, f16 11, f32 24).  That is exact
+// where the last bit is worth 2^-133 or more, which is all of bf16 and f16, and f32 from 2^-110 on.
 template <typename T>
 constexpr int TERMS = 1;
 template <>
@@ -125,7 +126,8 @@ struct Eight {
   }
 };
 
-// Term t is the upper half (sign, exponent, 8 bits of significand) of what the terms before it have left.  What an
+// Term t is the upper half (sign, exponent, 8 bits of significand) of what the terms before it have left: of a normal number it
+// leaves 16 bits, of one below 2^-126 what is worth less than 2^-133.  What an
 // infinity or a NaN leaves is that of the largest number: finite, so that its first term alone decides.
 template <typename T>
 struct Terms {
