@@ -29,10 +29,11 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream():
+def _stream(device=None):
+    """Of the current GPU, whose number a caller may have already."""
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 def _here(t, what, dtype=None):
@@ -277,7 +278,7 @@ def _combine(z, route, weights, out):
 def combine(z, route: Route, weights, out=None):
     """ginex_combine: y[r] = sum_j weights[r, j] z[slot[r, j]]; ``weights`` f32 [rows, top]."""
     _dense(weights, "weights", (route.rows, route.top), torch.float32)
-    if torch.is_grad_enabled() and (weights.requires_grad or getattr(z, "requires_grad", False)):
+    if (weights.requires_grad or getattr(z, "requires_grad", False)) and torch.is_grad_enabled():
         _recorded(out)
         return Combine.apply(z, weights, route)
     return _combine(z, route, weights, out)
@@ -366,10 +367,11 @@ def restore(kept: Compressed, dtype=torch.float32, out=None):
     """ginex_restore: the values that the codes stand for."""
     if dtype not in _TYPES:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    if out is None and (kept._device < 0 or kept._device != torch.cuda.current_device()):
+    current = torch.cuda.current_device() if kept._device >= 0 else None
+    if kept._device != current:
         raise ValueError(f"kept: on {kept.codes.device}, which is not the current GPU")
     out, to = _out(out, "out", (kept.rows, kept.width), dtype, kept.codes)
-    _check(_lib.load().ginex_restore(C.byref(_with(kept, "kept", out)._desc), C.byref(to), _stream()))
+    _check(_lib.load().ginex_restore(C.byref(kept._desc), C.byref(to), _stream(current)))
     return out
 
 
