@@ -25,6 +25,9 @@ extern "C" {
 #define GINEX_ACT_RELU 1 /* x < 0 ? 0 : x */
 #define GINEX_ACT_SILU 2 /* x / (1 + exp(-x)) */
 #define GINEX_ACT_GELU 3 /* x * Phi(x), Phi the normal distribution function (no approximation by tanh) */
+/* Both and their derivatives are computed in f32 and rounded once.  Of rows in f32 silu is good to 2^-20 of its value and gelu
+ * to 2^-18 + x^2 2^-22 of it; of rows in 16 bits exp and 1/x are the hardware's (1 unit each, exp's argument rounded) and Phi
+ * is good to 2^-19 + x^2 2^-23 of it, below the rounding of the result.  Results below 2^-119 may be 0. */
 
 #define GINEX_MAX_EXPERTS 1024
 #define GINEX_MAX_TOP 64

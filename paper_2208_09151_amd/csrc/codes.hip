@@ -6,11 +6,13 @@
 // share a block of 32 channels and find its largest magnitude by exchanging lanes.  Chunks are numbered
 // through all rows, padded to whole blocks, so that no lane idles for a width that is no power of two.
 //
-// Measured (bytes that have to move, over the time of a call among others; a plain copy reaches 6.2 TB/s):
+// Measured (bytes that have to move, over the time of a call among others, inputs and outputs of 4 to 10 calls in turn, so
+// that none are in the caches of 256 MB; a plain copy reaches 6.2 TB/s, what writes more than it reads somewhat more):
 //                        compress       with silu      with gelu      restore        silu's gradient  gelu's
-//   820 000 x 256 f32    172 us 6.1     302 us 6.3     306 us 6.2     145 us 7.3     306 us 6.2       310 us 6.1 TB/s
-//   820 000 x 256 bf16   103    6.2     168    6.3     172    6.1      88    7.2     176    6.0       175    6.0
-//   300 000 x 333 f16     50    6.1      79    6.3      95    5.3      52    5.9      83    6.1       110    4.6
+//   820 000 x 256 f32    171 us 6.2     302 us 6.3     302 us 6.3     161 us 6.5     309 us 6.1       307 us 6.2 TB/s
+//   820 000 x 256 bf16   108    5.9     170    6.2     180    5.9      99    6.4     177    6.0       186    5.7
+//   300 000 x 333 f16     54    5.7      92    5.5     103    4.9      60    5.2      89    5.7        99    5.1
+// (Codes that are still in the caches: restore of the first 145 us.)
 #include "codes.hpp"
 
 namespace ginex {
@@ -22,7 +24,8 @@ constexpr int THREADS = 256;
 constexpr int UNROLL = 2;
 
 // exp and 1/x: the library's and the division for f32; for results of 8 or 11 bits the instructions (1 unit each, and
-// exp's argument is rounded once more: off by |x| 2^-24), without which 16-bit rows are bound by the vector unit.
+// exp's argument is rounded once more: off by |x| 2^-24), without which 16-bit rows are bound by the vector unit.  1/x is 0
+// where it would be below 2^-126: of silu that is x < -87, whose value is below 2^-119.
 template <bool FINE>
 __device__ __forceinline__ float exp_of(float x) {
   return FINE ? expf(x) : __builtin_amdgcn_exp2f(x * 1.44269504f);
@@ -33,7 +36,7 @@ __device__ __forceinline__ float inverse(float x) {
 }
 
 // Phi(-|x|) = erfc(z) / 2, z = |x| / sqrt 2, with bell = exp(-x^2 / 2):  exp(z^2) erfc(z) / 2 = t Q(t), t = 1 / (1 + a z),
-// is smooth on all of [0, 1]; Q is a polynomial fitted to the least relative error here (weighted least squares at
+// is smooth on all of [0, 1] (t by the instruction, also in f32: 1 unit); Q is a polynomial fitted to the least relative error here (weighted least squares at
 // Chebyshev's points): 6e-9 of degree 10 for f32, 7e-7 of degree 7 for 16 bits.  One exponential serves Phi and its slope;
 // erfcf took 363 instead of 300 us (gelu, 820 000 x 256 f32).
 template <bool FINE>

@@ -9,8 +9,9 @@
 //
 // Bound by launches and their latencies: up to 8192 pairs one workgroup in one launch (up to 512 pairs 2.3 us,
 // 7000 7.8), else the tiles' counts and the places, in which every workgroup adds up the counts of the tiles
-// itself (354 000 pairs 4.7 + 7.6 us, 1.64 M 4.6 + 18); with a scan between them, five launches, 1.64 M pairs
-// took 35 us in all and 152 000 20 instead of 15.
+// itself (354 000 pairs 4.8 + 7.3 us, 1.64 M 5.8 + 18 in 32 experts: 401 workgroups that read 51 KB of counts each, where
+// the pairs' bytes would take 4); with a scan between them, five launches, 1.64 M pairs took 35 us in all and 152 000 20
+// instead of 15.
 #include "primitives.hpp"
 #include "train.hpp"
 

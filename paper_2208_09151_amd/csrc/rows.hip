@@ -9,13 +9,14 @@
 // offset are checked against the slots that exist before anything is computed from them: a routing that was
 // not made by ginex_route cannot reach memory outside the arrays.
 //
-// Measured (bytes that have to move, over the time of a call among others; a plain copy reaches 6.2 TB/s):
+// Measured (bytes that have to move, over the time of a call among others, inputs of 4 to 10 calls in turn, so that none are
+// in the caches of 256 MB; a plain copy reaches 6.2 TB/s):
 //   rows x width, slots a row     dispatch        combine         its gradient
-//   820 000 x 256 f32, 2          412 us 6.1      431 us 5.9      774 us 5.4 TB/s
-//   820 000 x 256 bf16, 2         213    5.9      226    5.6      413    5.1
-//   177 000 x 128 f32, 2           41    6.7       43    6.4       80    5.7
-//   41 017 x 250 f32, 8            96    3.8       66    5.7      168    4.2   (slots that share lines)
-//   41 017 x 256 f32, 8            65    5.8       69    5.5      152    4.7
+//   820 000 x 256 f32, 2          413 us 6.1      429 us 5.9      776 us 5.4 TB/s
+//   820 000 x 256 bf16, 2         216    5.9      220    5.8      409    5.2
+//   177 000 x 128 f32, 2           49    5.6       50    5.5       85    5.4   (all of it in the caches: 40, 41, 80)
+//   41 017 x 250 f32, 8            87    4.3       71    5.2      170    4.1   (slots that share lines)
+//   41 017 x 256 f32, 8            73    5.2       71    5.4      154    4.7
 #include "train.hpp"
 
 namespace ginex {

@@ -52,7 +52,8 @@ inline Tiling tiling_of(int32_t terms, int64_t slots, int32_t experts, int64_t w
       else shape(2, 2, 2, 1);
     }
   }
-  // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us)
+  // one large workgroup to a CU, or two small ones (of three that it has room for; with three: 65 -> 71 us).  Rounded down:
+  // a layer of 129 to 255 large tiles has one range and leaves CUs idle, one of somewhat more takes a second round for few.
   int64_t ranges = (large ? 256 : 512) / t.tiles();
   // 128 slots at least, but a range for every expert of few slots (64 rows of 8 experts: 27 -> 14 us)
   const int64_t each = ceil_div(slots, STEP) < experts ? ceil_div(slots, STEP) : experts;

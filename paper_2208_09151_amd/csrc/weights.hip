@@ -3,7 +3,7 @@
 //   dw[e][c][d] = sum over the slots s of expert e of  x(source[s], c) * dy(s, d)
 //
 // A product of two matrices whose long axis, the slots, is cut into ranges of equal length whatever the
-// experts, so that few experts or uneven ones still fill the GPU evenly.  A workgroup goes through its
+// experts, so that few experts or uneven ones do not leave most of the GPU idle.  A workgroup goes through its
 // range expert by expert.  An expert that lies in one range is written where it belongs; one that several
 // ranges share leaves its parts in the workspace, and a second launch adds them up in their order, so that
 // equal inputs give equal bits.
@@ -13,10 +13,12 @@
 // taken apart on the vector unit and put into LDS with the slots as rows, where transposing reads turn them
 // into operands.
 //
-// Measured, kernel and join, 820 000 x 2 slots in 32 experts, 256 x 256: f32 585-680 us (1040 TFLOP/s of bf16
-// products; the clock falls to 1.6-1.9 GHz: bound by power), f16 400-440, bf16 276-294 (codes are read once per expert of a
-// row: 1.34 GB, 5.1 TB/s without the join).  76 000 x 2 in 8 experts, 128 x 256, bf16: 27 to 29 + 4.6 us
-// where 98 MB of slots come from HBM (16 at its rate); the parts of 512 workgroups are 17 MB.
+// Measured, kernel + join, 820 000 x 2 slots in 32 experts, 256 x 256 (medians of calls in a row; the counters are of calls
+// with pauses between them, in which the clock falls less): f32 593 + 15 us, 1087 TFLOP/s of bf16 products, the matrix cores
+// busy in 60 % of the cycles at 1.95 GHz instead of 2.4; f16 396 + 15, 55 % at 2.1 GHz; bf16 264 + 15, 34 % at 2.4 GHz and 1.37 GB
+// from HBM, 5.2 TB/s (codes are read once per expert of a row).  So f32 and f16 are bound by power and by the vector unit,
+// which cuts the terms, bf16 by HBM.  76 000 x 2 in 8 experts, 128 x 256, bf16: 31 + 5 us where 89 MB come from HBM (14 us
+// at its rate); the parts of 512 workgroups are 17 MB.
 #include "codes.hpp"
 #include "tiling.hpp"
 

@@ -6,8 +6,10 @@ cache and the gather in front, the training operators behind.
 ``ExpertLayer`` sends every row to the experts its router likes best, one linear layer and an activation
 each, and adds their answers up by the router's weights.  What the backward pass needs of the rows and of
 the activations' inputs is kept in 8 bits (8.25 with the scales, instead of 32): the rows once, not once per
-expert, as the weight gradient looks them up by the route.  The products of forward pass and input gradient
-are torch's, an expert at a time.
+expert, as the weight gradient looks them up by the route.  The experts' answers are kept as they are, for the
+gradient of the router's weights.  The products of forward pass and input gradient are torch's, an expert at a
+time, and need the experts' sizes on the host: the layer waits for the GPU once and cannot be captured into a
+graph.
 """
 from __future__ import annotations
 
