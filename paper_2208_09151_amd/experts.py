@@ -51,11 +51,11 @@ class ExpertLinear(torch.autograd.Function):
     @_first_derivative
     def backward(ctx, grad):
         weight, codes, scales, *route = ctx.saved_tensors
-        r = Route._made(*route)
+        r = Route(*route)
         grad = grad.contiguous()
         dx = dw = None
         if ctx.needs_input_grad[1]:
-            dw = weight_gradient(Compressed._made(codes, scales, ctx.width), grad, r).to(weight.dtype)
+            dw = weight_gradient(Compressed(codes, scales, ctx.width), grad, r).to(weight.dtype)
         if ctx.needs_input_grad[0]:
             drows = torch.empty((grad.shape[0], weight.shape[1]), dtype=grad.dtype, device=grad.device)
             for e, a, b in _spans(ctx.ends):

@@ -216,7 +216,7 @@ class Dispatch(torch.autograd.Function):
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        return dispatch_backward(grad.contiguous(), Route._made(*ctx.saved_tensors)), None
+        return dispatch_backward(grad.contiguous(), Route(*ctx.saved_tensors)), None
 
 
 class Combine(torch.autograd.Function):
@@ -231,7 +231,7 @@ class Combine(torch.autograd.Function):
     @_first_derivative
     def backward(ctx, grad):
         z, weights, *route = ctx.saved_tensors
-        dz, dweights = combine_backward(grad.contiguous(), z, Route._made(*route), weights)
+        dz, dweights = combine_backward(grad.contiguous(), z, Route(*route), weights)
         return dz, dweights, None
 
 
@@ -250,7 +250,7 @@ class Activation(torch.autograd.Function):
     @staticmethod
     @_first_derivative
     def backward(ctx, grad):
-        kept = Compressed._made(*ctx.saved_tensors, ctx.width)
+        kept = Compressed(*ctx.saved_tensors, ctx.width)
         return activate_backward(kept, grad.contiguous(), ctx.name), None, None
 
 

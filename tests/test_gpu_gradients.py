@@ -146,3 +146,17 @@ def test_a_training_run_leaves_the_random_numbers_alone():
     torch.manual_seed(4)
     # the same weights: the neighbours' sums alone are added up in any order
     assert abs(train(config=1, steps=1, report=None)[0] - first[0]) < 1e-4
+
+
+@pytest.mark.parametrize("change", [lambda t: t.cpu(), lambda t: t.repeat(2, *[1] * (t.dim() - 1))[::2], lambda t: t[:-1]])
+def test_saved_tensors_that_come_back_otherwise_are_refused(g, change):
+    """Hooks may return anything: codes and routes are looked at again before the library gets their addresses."""
+    r, gen = routed(g, 70, 3, 5)
+    x = torch.randn((70, 20), generator=gen, device="cuda").requires_grad_()
+    w = torch.randn((70, 3), generator=gen, device="cuda")
+    z = torch.randn((210, 20), generator=gen, device="cuda").requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: change(t) if t.dtype != torch.float32 else t):
+        results = [g.dispatch(x, r), g.combine(z, r, w), g.activate(x, "silu")[0]]
+    for y in results:
+        with pytest.raises((ValueError, g.GinexError)):
+            y.sum().backward()
