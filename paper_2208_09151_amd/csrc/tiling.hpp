@@ -33,10 +33,10 @@ inline Tiling tiling_of(int32_t terms, int64_t slots, int32_t experts, int64_t w
   if (width > 128) shape(4, 2, 2, 4);
   else shape(2, 2, 4, 2);
   const bool large = out_width > 128 && slots * t.tiles() >= 256 * 1024;
-  // Else 128 x 128, or as narrow as the layer: what a tile has too many of is read, cut and multiplied for nothing (f32,
-  // 1 000 000 slots, 128 x 8: 111 us in tiles of 128 x 128, 50 of 128 x 32; 500 000 x 2 in 512 experts, 64 x 64: 143 and 81;
-  // 820 000, 256 x 47: 197 and 145; bf16, 820 000 x 2, 64 x 64: 100 and 64;
-  // the call of 820 000 x 2 f32, 16 x 128: 215 and 168).
+  // Else 128 x 128, or as narrow as the layer: what a tile has too many of is read, cut and multiplied for nothing (us of a
+  // call, here and below with inputs that are not in the caches, in tiles of 128 x 128 and of the layer's: f32, 1 000 000 slots,
+  // 128 x 8: 104 and 52; 500 000 x 2 in 512 experts, 64 x 64: 123 and 86; 820 000, 256 x 47: 171 and 124; 820 000 x 2, 16 x 128:
+  // 193 and 160; bf16, 820 000 x 2, 64 x 64: 89 and 70).
   if (!large) {
     if (out_width <= 32) shape(4, 1, 1, 1);
     else if (out_width <= 64 && width <= 64) shape(2, 1, 2, 1);
@@ -44,9 +44,9 @@ inline Tiling tiling_of(int32_t terms, int64_t slots, int32_t experts, int64_t w
     else if (width <= 64) shape(1, 2, 4, 1);
     else shape(2, 2, 2, 2);
     // With few slots what costs is the parts that the workgroups leave, and half a tile has half a part (bf16: 76 000 x 2,
-    // 128 x 256 36 -> 32 us, 128 x 128 27 -> 22; but 500 000 x 2, 128 x 100 69 -> 72, 820 000 x 2, 256 x 100 178 -> 217.  f32:
-    // 76 000 x 2, 128 x 128 37 -> 33, but 128 x 256 51 -> 52 and 177 000 x 2, 128 x 128 56 -> 59).  With many tiles there are
-    // few parts (bf16, 2000 x 2, 1024 x 1024: 30 -> 32).
+    // 128 x 256 37.7 -> 36.7 us, 128 x 128 27.9 -> 25.7; but 500 000 x 2, 128 x 100 72 -> 81, 820 000 x 2, 256 x 100 183 -> 219.
+    // f32: 76 000 x 2, 128 x 128 38.2 both, with parts in the caches 37 -> 33; but 128 x 256 55.7 -> 56.6 and 177 000 x 2,
+    // 128 x 128 62.8 -> 64.1).  With many tiles there are few parts (bf16, 2000 x 2, 1024 x 1024: 27 -> 30).
     if (t.mt == 2 && t.nt == 2 && t.tiles() <= 16 && slots * t.tiles() < (terms == 1 ? 512 : 200) * 1024) {
       if (terms == 1) shape(1, 2, 4, 1);
       else shape(2, 2, 2, 1);
