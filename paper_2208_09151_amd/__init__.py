@@ -13,3 +13,5 @@ from .pipeline import Executor, InspectorPipeline  # noqa: F401
 from .training import (Compressed, Route, activate, activate_backward, combine,  # noqa: F401
                        combine_backward, compress, dispatch, dispatch_backward, restore, route,
                        weight_gradient)
+from .layers import (bias_gradient, expert_layer, layer_norm, layer_norm_backward, linear,  # noqa: F401
+                     linear_backward, lookup, lookup_backward)

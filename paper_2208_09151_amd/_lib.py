@@ -1,4 +1,4 @@
-"""ctypes loader for libginex.so; declares every entry point of include/ginex.h and ginex_train.h."""
+"""ctypes loader for libginex.so; declares every entry point of include/ginex.h, ginex_train.h and ginex_layers.h."""
 from __future__ import annotations
 
 import ctypes as C
@@ -31,6 +31,11 @@ class RoutingDesc(C.Structure):
 
 class CodesDesc(C.Structure):
     _fields_ = [("rows", i64), ("width", i64), ("codes", vp), ("scales", vp)]
+
+
+class WeightsDesc(C.Structure):
+    _fields_ = [("data", vp), ("experts", i32), ("turned", i32), ("width", i64), ("out", i64),
+                ("stride", i64), ("expert_stride", i64), ("type", i32)]
 
 
 SIGNATURES = {
@@ -77,6 +82,23 @@ TRAIN_SIGNATURES = {
     "ginex_weight_gradient": (i32, [_CODES, _ROUTING, _ROWS, vp, vp, sz, vp]),
 }
 
+_WEIGHTS, f32 = C.POINTER(WeightsDesc), C.c_float
+
+# include/ginex_layers.h
+LAYER_SIGNATURES = {
+    "ginex_linear": (i32, [_ROWS, _WEIGHTS, vp, i32, _ROWS, _ROUTING, i32, _ROWS, _CODES, vp]),
+    "ginex_bias_gradient_workspace_bytes": (sz, [i64, i32, i64]),
+    "ginex_bias_gradient": (i32, [_ROWS, _ROUTING, vp, vp, sz, vp]),
+    "ginex_expert_layer_workspace_bytes": (sz, [i64, i32, i32, i64, i64]),
+    "ginex_expert_layer": (i32, [_ROWS, _ROWS, _WEIGHTS, vp, i32, i32, _ROWS, vp, sz, vp]),
+    "ginex_layer_norm": (i32, [_ROWS, vp, vp, f32, _ROWS, vp, vp]),
+    "ginex_layer_norm_backward_workspace_bytes": (sz, [i64, i64]),
+    "ginex_layer_norm_backward": (i32, [_ROWS, _ROWS, vp, vp, _ROWS, vp, vp, vp, sz, vp]),
+    "ginex_lookup": (i32, [_ROWS, vp, i32, f32, _ROWS, vp]),
+    "ginex_lookup_backward_workspace_bytes": (sz, [i64, i64, i64]),
+    "ginex_lookup_backward": (i32, [_ROWS, vp, i32, f32, _ROWS, vp, sz, vp]),
+}
+
 _lib = None
 
 
@@ -89,7 +111,7 @@ def stale() -> bool:
     sources = [os.path.join(csrc, f) for f in os.listdir(csrc)
                if f.endswith((".hip", ".hpp", ".cpp"))]
     include = os.path.join(os.path.dirname(_PKG), "include")
-    sources += [os.path.join(include, f) for f in ("ginex.h", "ginex_train.h")]
+    sources += [os.path.join(include, f) for f in ("ginex.h", "ginex_train.h", "ginex_layers.h")]
     return any(os.path.getmtime(s) > built for s in sources if os.path.exists(s))
 
 
@@ -109,7 +131,7 @@ def load():
             else:
                 raise RuntimeError(f"{LIB_PATH} has not been built and {HIPCC} is not installed")
         lib = C.CDLL(LIB_PATH)
-        for name, (res, args) in [*SIGNATURES.items(), *TRAIN_SIGNATURES.items()]:
+        for name, (res, args) in [*SIGNATURES.items(), *TRAIN_SIGNATURES.items(), *LAYER_SIGNATURES.items()]:
             fn = getattr(lib, name)     # AttributeError if the library lacks a declared symbol
             fn.restype = res
             fn.argtypes = args

@@ -13,6 +13,7 @@
 //   820 000 x 256 bf16   108    5.9     170    6.2     180    5.9      99    6.4     177    6.0       186    5.7
 //   300 000 x 333 f16     54    5.7      92    5.5     103    4.9      60    5.2      89    5.7        99    5.1
 // (Codes that are still in the caches: restore of the first 145 us.)
+#include "activations.hpp"
 #include "codes.hpp"
 
 namespace ginex {
@@ -22,74 +23,6 @@ constexpr int THREADS = 256;
 // Chunks of a thread, their loads issued together (compress, 820 000 x 256 f32: 179 us with one, 175 with two, 174 with four;
 // silu 313, 309 and 322; 300 000 x 333 f16: 57, 49 and 49, silu's gradient 90, 83 and 87).
 constexpr int UNROLL = 2;
-
-// exp and 1/x: the library's and the division for f32; for results of 8 or 11 bits the instructions (1 unit each, and
-// exp's argument is rounded once more: off by |x| 2^-24), without which 16-bit rows are bound by the vector unit.  1/x is 0
-// where it would be below 2^-126: of silu that is x < -87, whose value is below 2^-119.
-template <bool FINE>
-__device__ __forceinline__ float exp_of(float x) {
-  return FINE ? expf(x) : __builtin_amdgcn_exp2f(x * 1.44269504f);
-}
-template <bool FINE>
-__device__ __forceinline__ float inverse(float x) {
-  return FINE ? 1.f / x : __builtin_amdgcn_rcpf(x);
-}
-
-// Phi(-|x|) = erfc(z) / 2, z = |x| / sqrt 2, with bell = exp(-x^2 / 2):  exp(z^2) erfc(z) / 2 = t Q(t), t = 1 / (1 + a z),
-// is smooth on all of [0, 1] (t by the instruction, also in f32: 1 unit); Q is a polynomial fitted to the least relative error here (weighted least squares at
-// Chebyshev's points): 6e-9 of degree 10 for f32, 7e-7 of degree 7 for 16 bits.  One exponential serves Phi and its slope;
-// erfcf took 363 instead of 300 us (gelu, 820 000 x 256 f32).
-template <bool FINE>
-__device__ __forceinline__ float tail(float x, float bell) {
-  if (FINE) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.282842712f, 1.f));
-    float q = -1.460759161e-02f;
-    q = fmaf(q, t, 7.022352350e-02f);
-    q = fmaf(q, t, -1.177639811e-01f);
-    q = fmaf(q, t, 6.878112558e-02f);
-    q = fmaf(q, t, -2.344789024e-02f);
-    q = fmaf(q, t, 4.195833894e-02f);
-    q = fmaf(q, t, 5.950411182e-02f);
-    q = fmaf(q, t, 8.586964844e-02f);
-    q = fmaf(q, t, 1.038068641e-01f);
-    q = fmaf(q, t, 1.128379301e-01f);
-    q = fmaf(q, t, 1.128379174e-01f);
-    return q * t * bell;
-  }
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.325269119f, 1.f));
-  float q = 3.385725232e-02f;
-  q = fmaf(q, t, -1.133149230e-01f);
-  q = fmaf(q, t, 8.459589749e-02f);
-  q = fmaf(q, t, 2.630502449e-02f);
-  q = fmaf(q, t, 9.342400306e-02f);
-  q = fmaf(q, t, 1.155909210e-01f);
-  q = fmaf(q, t, 1.297786344e-01f);
-  q = fmaf(q, t, 1.297635293e-01f);
-  return q * t * bell;
-}
-
-template <int ACT, bool FINE>
-__device__ __forceinline__ float activated(float x) {
-  if (ACT == GINEX_ACT_RELU) return x < 0.f ? 0.f : x;
-  if (ACT == GINEX_ACT_SILU) return FINE ? x / (1.f + exp_of<FINE>(-x)) : x * inverse<FINE>(1.f + exp_of<FINE>(-x));
-  if (ACT == GINEX_ACT_GELU) {
-    const float below = tail<FINE>(x, exp_of<FINE>(-0.5f * x * x));
-    return x * (x < 0.f ? below : 1.f - below);
-  }
-  return x;
-}
-
-// dy f'(x)
-template <int ACT, bool FINE>
-__device__ __forceinline__ float sloped(float x, float dy) {
-  if (ACT == GINEX_ACT_RELU) return x > 0.f ? dy : (x <= 0.f ? 0.f : x);
-  if (ACT == GINEX_ACT_SILU) {
-    const float sigma = inverse<FINE>(1.f + exp_of<FINE>(-x));
-    return dy * (sigma * fmaf(x, 1.f - sigma, 1.f));
-  }
-  const float bell = exp_of<FINE>(-0.5f * x * x), below = tail<FINE>(x, bell);
-  return dy * fmaf(x * bell, 0.39894228040143268f, x < 0.f ? below : 1.f - below);
-}
 
 // The codes of a chunk, as one word of N bytes.
 template <int N>
@@ -102,13 +35,6 @@ template <>
 struct Word<8> {
   typedef uint64_t type;
 };
-
-// Four numbers of the form 1.5 2^23 + q: their lowest bytes are the q in two's complement.
-__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
-  const uint32_t ab = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0c0c0400u);
-  const uint32_t cd = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000c0cu);
-  return ab | cd;
-}
 
 // The largest of the 4 or 8 neighbouring lanes that share a block, in all of them.
 template <int CTRL>
@@ -226,18 +152,6 @@ int32_t by_launches(int64_t rows, int64_t width, Go go) {
     go(r, (uint32_t)((rows - r < step ? rows - r : step) * cpr), Divisor((uint32_t)cpr));
     GINEX_LAUNCH_CHECK();
   }
-  return GINEX_OK;
-}
-
-int32_t check_activation(int32_t activation, int32_t least) {
-  if (activation < least || activation > GINEX_ACT_GELU) return fail(GINEX_ERR_ARG, "unknown activation %d", activation);
-  return GINEX_OK;
-}
-
-int32_t check_kept(const char* what, const ginex_rows_t* r, const ginex_codes_t* kept) {
-  if (r->rows != kept->rows || r->width != kept->width)
-    return fail(GINEX_ERR_ARG, "%s is %lld x %lld, the codes %lld x %lld", what, (long long)r->rows, (long long)r->width,
-                (long long)kept->rows, (long long)kept->width);
   return GINEX_OK;
 }
 

@@ -29,4 +29,11 @@ __device__ __forceinline__ float code_step(uint32_t scale) {
   return scale == NO_NUMBER ? __uint_as_float(0x7FC00000) : ldexpf(1.f, (int)scale - 133);
 }
 
+// Four numbers of the form 1.5 2^23 + q: their lowest bytes are the q in two's complement.
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  const uint32_t ab = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0c0c0400u);
+  const uint32_t cd = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000c0cu);
+  return ab | cd;
+}
+
 }  // namespace ginex

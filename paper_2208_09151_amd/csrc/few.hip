@@ -1,0 +1,446 @@
+// Few rows: a linear layer, or a whole layer of experts in two launches.
+//
+//   scores(r, e) = <x[r], router[e]>, the experts of the `top` largest, p(r, :) their softmax          (first launch)
+//   y[r] = sum over j of p(r, j) f(x[r] W_e(r,j) + bias_e(r,j))                                      (second launch)
+//
+// What counts is how fast the weights arrive, and before that the latency of a handful of dependent steps.  A workgroup has 64
+// columns of one expert and all rows that are sent to it; its waves share the width, and each streams its part of the weights
+// from HBM straight into the registers of the matrix instructions (columns are the first operand, rows the second, 16 at a
+// time; weights with dense columns are turned over in registers).  The waves' sums meet in LDS.  In a layer of experts each
+// leaves f(..) of its pairs in the workspace, and of the workgroups of the same columns the one that comes last adds them up,
+// in the order of j.
+#include "activations.hpp"
+#include "codes.hpp"
+#include "layers.hpp"
+
+namespace ginex {
+namespace {
+
+constexpr int THREADS = 512, WAVES = THREADS / WAVE;
+constexpr int TILES = GINEX_MAX_FEW_ROWS / 16;            // of 16 rows
+constexpr int PITCH = WAVE_COLUMNS + 4;                   // of a row of sums in LDS: 16 rows of 4 words use every bank once
+constexpr int MOST_PAIRS = GINEX_MAX_FEW_ROWS * GINEX_MAX_FEW_TOP;
+
+__device__ __forceinline__ double sum_of_wave(double v) {
+#pragma unroll
+  for (int d = 1; d < WAVE; d *= 2) v += __shfl_xor(v, d, WAVE);
+  return v;
+}
+
+// A score as a number that is larger where the score is; NaN is the largest, 0 is smaller than all.
+__device__ __forceinline__ uint64_t rank_of(double v) {
+  if (v != v) return ~(uint64_t)0;
+  const uint64_t bits = (uint64_t)__double_as_longlong(v + 0.0);      // (-0 is 0)
+  return bits >> 63 ? ~bits : bits | (uint64_t)1 << 63;
+}
+
+// What the two launches share.
+struct Plan {
+  int32_t* chosen;      // [rows x top]
+  float* share;         // [rows x top]
+  uint32_t* done;       // workgroups of 64 columns that are through
+  float* part;          // [rows x top x out]
+};
+
+// A workgroup a row.  Products in f64 are exact for all types, so what is chosen does not depend on how a sum is rounded
+// (but for scores that are equal to 2^-50 or so).
+template <typename T>
+__global__ __launch_bounds__(THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
+                                                       int32_t top, Width width, Plan plan, int32_t tiles) {
+  constexpr int N = Chunk<T>::N, U = 4, EACH = GINEX_MAX_EXPERTS / WAVE;
+  __shared__ double scores[GINEX_MAX_EXPERTS];
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  const T* const row = x.at(blockIdx.x);
+  if (blockIdx.x == 0)
+    for (int32_t i = threadIdx.x; i < tiles; i += THREADS) plan.done[i] = 0;
+  for (int32_t e0 = wave; e0 < experts; e0 += U * WAVES) {
+    double sum[U] = {};
+    for (int32_t c = lane * N; c < width.width; c += WAVE * N) {
+      float a[N], b[U][N];
+      load_chunk(row, c, width, a);
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_chunk(router.at(e0 + u * WAVES < experts ? e0 + u * WAVES : e0), c, width, b[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int n = 0; n < N; ++n) sum[u] = fma((double)a[n], (double)b[u][n], sum[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const double total = sum_of_wave(sum[u]);
+      if (lane == 0 && e0 + u * WAVES < experts) scores[e0 + u * WAVES] = total;
+    }
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  uint64_t rank[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) rank[i] = lane + i * WAVE < experts ? rank_of(scores[lane + i * WAVE]) : 0;
+  int32_t mine = 0;           // lane j has choice j
+  for (int32_t j = 0; j < top; ++j) {
+    uint64_t best = rank[0];
+    int32_t at = lane;
+#pragma unroll
+    for (int i = 1; i < EACH; ++i)
+      if (rank[i] > best) {
+        best = rank[i];
+        at = lane + i * WAVE;
+      }
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) {
+      const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)best, d, WAVE);
+      const int32_t where = __shfl_xor(at, d, WAVE);
+      if (other > best || (other == best && where < at)) {
+        best = other;
+        at = where;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (at == lane + i * WAVE) rank[i] = 0;
+    if (lane == j) mine = at;
+  }
+  const double score = scores[mine], most = __shfl(score, 0, WAVE);
+  const double weight = lane < top ? exp(score - most) : 0.0, total = sum_of_wave(weight);
+  if (lane < top) {
+    plan.chosen[(int64_t)blockIdx.x * top + lane] = mine;
+    plan.share[(int64_t)blockIdx.x * top + lane] = (float)(weight / total);
+  }
+}
+
+// Four neighbouring columns of a row of weights, from column n on; what is behind the last one is 0.
+template <typename T>
+__device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t n, int32_t columns) {
+  typename Four<T>::Wide v;
+  if (columns < 4) {
+#pragma unroll
+    for (int l = 0; l < 4; ++l) v[l] = n + l < columns ? row[n + l] : (T)0.f;
+    return v;
+  }
+  const int32_t over = n + 4 - columns;       // the last ones are read so that they end with the row, and moved
+  v = *reinterpret_cast<const typename Four<T>::At*>(row + (over > 0 ? columns - 4 : n));
+  if (over > 0) {
+#pragma unroll
+    for (int l = 0; l < 4; ++l) {
+      T to = (T)0.f;
+#pragma unroll
+      for (int m = l + 1; m < 4; ++m) to = m == l + over ? v[m] : to;
+      v[l] = to;
+    }
+  }
+  return v;
+}
+
+// Rows of one expert and their sums: x[row(i)] W for i < count, in `room` [wave][row][column] in the end, 16 rows at a time.
+// `row_of(i)` is the row of x, negative for a row of zeros.
+template <typename T, bool TURNED, typename RowOf>
+__device__ __forceinline__ void few_sums(RowsOf<const T> x, const T* __restrict__ w, int64_t stride, int32_t width, Width out,
+                                         int32_t n0, int32_t count, RowOf row_of, float4v (&sum)[TILES][4]) {
+  constexpr int N = Chunk<T>::N, STEP = 4 * N, UNIT = 2 * STEP;       // a unit is 128 bytes of a row
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), group = lane / 16;
+  const Width along = {width, (int32_t)((width + N - 1) / N * N - width)};
+  const T* row[TILES];
+  bool there[TILES];
+#pragma unroll
+  for (int m = 0; m < TILES; ++m) {
+    const int32_t i = m * 16 + lane % 16;
+    const int64_t r = row_of(i < count ? i : 0);
+    there[m] = r >= 0;
+    row[m] = x.at(r >= 0 ? r : 0);
+  }
+  const int32_t n = n0 + lane % 16 * 4;         // this lane's columns: row lane % 16 of operand j is column n + j
+  for (int32_t k0 = wave * UNIT; k0 < width; k0 += WAVES * UNIT) {
+    ChunkWords<T> fb[2][4];
+    if (TURNED) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int32_t at = n + j < out.width ? n + j : out.width - 1;
+          fb[s][j] = load_words(w + at * stride, k0 + s * STEP + group * N, along);
+        }
+    } else {
+      typename Four<T>::Wide raw[2][N];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int32_t k = k0 + s * STEP + group * N + i;
+          raw[s][i] = four_of(w + (int64_t)(k < width ? k : width - 1) * stride, n < out.width ? n : out.width - 1, out.width);
+          if (k >= width) raw[s][i] = (typename Four<T>::Wide)(T)0.f;
+        }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < N; ++i) fb[s][j].wide[i] = raw[s][i][j];
+    }
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+      if (m * 16 >= count) break;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        ChunkWords<T> fa = load_words(row[m], k0 + s * STEP + group * N, along);
+        if (!there[m]) fa.words = words4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[m][j] = product(fb[s][j], fa, sum[m][j]);
+      }
+    }
+  }
+}
+
+// The waves' sums of 16 rows, added up: thread t gets rows t / 64 and t / 64 + 8 of column t % 64.
+__device__ __forceinline__ void join_waves(const float4v (&sum)[4], float (*room)[16][PITCH], float (&v)[2]) {
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  __syncthreads();
+  // lane's row is lane % 16; component i of operand j's sums is column 16 (lane / 16) + 4 i + j
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<float4v*>(&room[wave][lane % 16][lane / 16 * 16 + 4 * i]) = float4v{sum[0][i], sum[1][i], sum[2][i], sum[3][i]};
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v[h] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v[h] += room[w][wave + h * WAVES][lane];
+  }
+}
+
+template <typename T, bool TURNED>
+__global__ __launch_bounds__(THREADS) void k_few_experts(RowsOf<const T> x, int32_t pairs, int32_t top, int32_t rows,
+                                                         WeightsOf<T> weights, const T* __restrict__ bias, int32_t width,
+                                                         Width out, int32_t activation, Plan plan, RowsOf<T> y) {
+  __shared__ uint32_t used[GINEX_MAX_EXPERTS / 32];
+  __shared__ int32_t list[GINEX_MAX_FEW_ROWS];          // the expert's pairs
+  __shared__ int32_t listed, is_last;
+  __shared__ float room[WAVES][16][PITCH];
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  // the experts that are chosen at all: the workgroup has the blockIdx.y-th of them
+  if (threadIdx.x < GINEX_MAX_EXPERTS / 32) used[threadIdx.x] = 0;
+  int32_t mine[MOST_PAIRS / THREADS];
+#pragma unroll
+  for (int i = 0; i < MOST_PAIRS / THREADS; ++i) {
+    const int32_t p = threadIdx.x + i * THREADS;
+    mine[i] = p < pairs ? plan.chosen[p] : -1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MOST_PAIRS / THREADS; ++i)
+    if (mine[i] >= 0) atomicOr(&used[mine[i] / 32], 1u << mine[i] % 32);
+  __syncthreads();
+  const uint32_t word = lane < GINEX_MAX_EXPERTS / 32 ? used[lane] : 0;
+  const uint32_t upto = wave_inclusive_scan((uint32_t)__popc(word)), distinct = of_lane(upto, WAVE - 1);
+  if (blockIdx.y >= distinct) return;
+  const int at = __ffsll((unsigned long long)__ballot(upto > blockIdx.y)) - 1;
+  uint32_t bits = of_lane(word, at);
+  for (uint32_t skip = blockIdx.y - (of_lane(upto, at) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
+  const int32_t expert = at * 32 + __ffs((int)bits) - 1;
+  // its pairs, in their order (a row has an expert once: no more than there are rows)
+  if (wave == 0) {
+    int32_t have = 0;
+    for (int32_t p0 = 0; p0 < pairs; p0 += WAVE) {
+      const bool is = p0 + lane < pairs && plan.chosen[p0 + lane] == expert;
+      const uint64_t who = __ballot(is);
+      const int32_t place = have + __popcll(who & (((uint64_t)1 << lane) - 1));
+      if (is && place < GINEX_MAX_FEW_ROWS) list[place] = p0 + lane;
+      have += __popcll(who);
+    }
+    if (lane == 0) listed = have < GINEX_MAX_FEW_ROWS ? have : GINEX_MAX_FEW_ROWS;
+  }
+  __syncthreads();
+  const int32_t count = listed, n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
+  float4v sum[TILES][4] = {};
+  few_sums<T, TURNED>(x, weights.of(expert), weights.stride, width, out, n0, count,
+                      [&](int32_t i) { return (int64_t)(list[i] / top); }, sum);
+  const float b = bias && c < out.width ? (float)bias[(int64_t)expert * out.width + c] : 0.f;
+#pragma unroll
+  for (int m = 0; m < TILES; ++m) {
+    if (m * 16 >= count) break;
+    float v[2];
+    join_waves(sum[m], room, v);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t i = m * 16 + wave + h * WAVES;
+      if (i < count && c < out.width)
+        __hip_atomic_store(plan.part + (int64_t)list[i] * out.width + c, activated_by<sizeof(T) == 4>(activation, v[h] + b),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  // The last workgroup of these columns to come here finds what the others have left, whichever die they were on.
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0)
+    is_last = __hip_atomic_fetch_add(plan.done + blockIdx.x, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == distinct - 1;
+  __syncthreads();
+  if (!is_last) return;
+  __threadfence();
+  if (c >= out.width) return;
+  for (int32_t r = wave; r < rows; r += WAVES) {
+    float total = 0.f;
+    for (int32_t j = 0; j < top; ++j) {
+      const int32_t p = r * top + j;
+      total = fmaf(plan.share[p],
+                   __hip_atomic_load(plan.part + (int64_t)p * out.width + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), total);
+    }
+    y.at(r)[c] = (T)total;
+  }
+}
+
+// A group a workgroup: an expert's slots, those without one, or all rows.
+template <typename T, bool TURNED>
+__global__ __launch_bounds__(THREADS) void k_few_linear(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights,
+                                                        const int32_t* __restrict__ source,
+                                                        const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
+                                                        int32_t width, Width out, Epilogue e) {
+  __shared__ float room[WAVES][16][PITCH];
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  const int32_t expert = blockIdx.y;
+  int64_t begin = 0, end = slots;
+  if (offsets) {
+    if (expert < experts) {
+      begin = offsets[expert];
+      end = offsets[expert + 1];
+      bound_slots(slots, begin, end);
+    } else {
+      begin = inside(offsets[experts], slots);
+    }
+  }
+  const int32_t count = (int32_t)(end - begin), n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
+  if (count <= 0) return;
+  const bool none = expert == experts;        // slots without an expert are cleared
+  float4v sum[TILES][4] = {};
+  if (!none)
+    few_sums<T, TURNED>(x, weights.of(expert), weights.stride, width, out, n0, count,
+                        [&](int32_t i) -> int64_t {
+                          const int64_t r = source ? (int64_t)source[begin + i] : begin + i;
+                          return r < rows ? r : -1;
+                        },
+                        sum);
+  const float b = !none && e.bias && c < out.width
+                      ? (float)static_cast<const T*>(e.bias)[(int64_t)expert * out.width + c] : 0.f;
+#pragma unroll
+  for (int m = 0; m < TILES; ++m) {
+    if (m * 16 >= count) break;
+    float v[2];
+    join_waves(sum[m], room, v);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t i = m * 16 + wave + h * WAVES;
+      if (i >= count) continue;               // (the same for the wave)
+      const int64_t r = begin + i;
+      v[h] = c < out.width ? v[h] + b : 0.f;
+      if (e.codes) {
+        // a block is half of the wave
+        uint32_t most = __float_as_uint(v[h]) & 0x7FFFFFFFu;
+#pragma unroll
+        for (int d = 1; d < GINEX_CODE_BLOCK; d *= 2) {
+          const uint32_t other = (uint32_t)__shfl_xor((int)most, d, WAVE);
+          most = most > other ? most : other;
+        }
+        const uint32_t scale = scale_byte(most);
+        constexpr float whole = 12582912.f;
+        const float q = __builtin_amdgcn_fmed3f(fmaf(v[h], to_codes(scale), whole), whole - 127.f, whole + 127.f);
+        if (c < e.blocks * GINEX_CODE_BLOCK) {
+          e.codes[r * ((int64_t)e.blocks * GINEX_CODE_BLOCK) + c] = scale == NO_NUMBER ? 0 : (int8_t)__float_as_uint(q);
+          if (c % GINEX_CODE_BLOCK == 0) e.scales[r * e.blocks + c / GINEX_CODE_BLOCK] = (uint8_t)scale;
+        }
+      }
+      if (c >= out.width) continue;
+      float to = none ? 0.f : activated_by<sizeof(T) == 4>(e.activation, v[h]);
+      if (e.residual && !none) to += (float)static_cast<const T*>(e.residual)[r * e.residual_stride + c];
+      static_cast<T*>(e.y)[r * e.y_stride + c] = (T)to;
+    }
+  }
+}
+
+struct FewSpace {
+  Plan plan;
+  size_t bytes;
+};
+FewSpace few_space(void* ws, int64_t rows, int32_t top, int64_t out) {
+  Arena arena(ws);
+  FewSpace s;
+  s.plan.chosen = arena.take<int32_t>(rows * top);
+  s.plan.share = arena.take<float>(rows * top);
+  s.plan.done = arena.take<uint32_t>(ceil_div(out, WAVE_COLUMNS));
+  s.plan.part = arena.take<float>(rows * top * out);
+  s.bytes = arena.used + 256;
+  return s;
+}
+
+int32_t check_few(int64_t rows, int32_t top, int32_t experts, int64_t width, int64_t out) {
+  if (rows < 0 || rows > GINEX_MAX_FEW_ROWS) return fail(GINEX_ERR_ARG, "rows=%lld (0..%d)", (long long)rows, GINEX_MAX_FEW_ROWS);
+  if (experts < 1 || experts > GINEX_MAX_EXPERTS) return fail(GINEX_ERR_ARG, "experts=%d (1..%d)", experts, GINEX_MAX_EXPERTS);
+  if (top < 1 || top > GINEX_MAX_FEW_TOP || top > experts)
+    return fail(GINEX_ERR_ARG, "top=%d of %d experts (1..%d)", top, experts, GINEX_MAX_FEW_TOP);
+  if (width < 1 || width > GINEX_MAX_WIDTH || out < 1 || out > GINEX_MAX_WIDTH)
+    return fail(GINEX_ERR_ARG, "width %lld or out %lld (1..%d)", (long long)width, (long long)out, GINEX_MAX_WIDTH);
+  return GINEX_OK;
+}
+
+}  // namespace
+
+int32_t linear_few(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot, int64_t slots,
+                   const Epilogue& epilogue, hipStream_t st) {
+  return with_type(x->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    const auto kernel = w->turned ? k_few_linear<T, true> : k_few_linear<T, false>;
+    const dim3 grid((unsigned)ceil_div(w->out, WAVE_COLUMNS), route ? (unsigned)route->experts + 1 : 1);
+    hipLaunchKernelGGL(kernel, grid, dim3(THREADS), 0, st, read_rows<T>(x), x->rows, weights_of<T>(w),
+                       route && !by_slot ? route->source : nullptr, route ? route->offsets : nullptr, w->experts, slots,
+                       (int32_t)w->width, Width::of<T>(w->out), epilogue);
+    GINEX_LAUNCH_CHECK();
+    return GINEX_OK;
+  });
+}
+
+}  // namespace ginex
+
+using namespace ginex;
+
+extern "C" size_t ginex_expert_layer_workspace_bytes(int64_t rows, int32_t top, int32_t experts, int64_t width, int64_t out) {
+  if (check_few(rows, top, experts, width, out)) return 0;
+  return few_space(nullptr, rows, top, out).bytes;
+}
+
+extern "C" int32_t ginex_expert_layer(const ginex_rows_t* x, const ginex_rows_t* router, const ginex_weights_t* weights,
+                                      const void* bias, int32_t top, int32_t activation, const ginex_rows_t* y, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  if (int32_t rc = check_rows("x", x, false)) return rc;
+  if (int32_t rc = check_rows("router", router, false)) return rc;
+  if (int32_t rc = check_weights(weights)) return rc;
+  if (int32_t rc = check_rows("y", y, true)) return rc;
+  if (int32_t rc = check_activation(activation, GINEX_ACT_NONE)) return rc;
+  if (int32_t rc = check_same("x", x, "router", router)) return rc;
+  if (x->type != weights->type || x->type != y->type) return fail(GINEX_ERR_ARG, "x, weights and y differ in type");
+  if (int32_t rc = check_few(x->rows, top, weights->experts, weights->width, weights->out)) return rc;
+  if (x->width != weights->width)
+    return fail(GINEX_ERR_ARG, "x is %lld wide, the weights take %lld", (long long)x->width, (long long)weights->width);
+  if (y->width != weights->out)
+    return fail(GINEX_ERR_ARG, "y is %lld wide, the weights give %lld", (long long)y->width, (long long)weights->out);
+  if (y->rows != x->rows) return fail(GINEX_ERR_ARG, "x has %lld rows, y %lld", (long long)x->rows, (long long)y->rows);
+  if (router->rows != weights->experts)
+    return fail(GINEX_ERR_ARG, "router has %lld rows for %d experts", (long long)router->rows, weights->experts);
+  if (int32_t rc = check_vector("bias", bias, x->type)) return rc;
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(GINEX_ERR_ARG, "workspace: null or misaligned");
+  const FewSpace space = few_space(ws, x->rows, top, weights->out);
+  if (ws_bytes < space.bytes) return fail(GINEX_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", space.bytes, ws_bytes);
+  if (x->rows == 0) return GINEX_OK;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return with_type(x->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    const int32_t rows = (int32_t)x->rows, pairs = rows * top;
+    const int32_t tiles = (int32_t)ceil_div(weights->out, WAVE_COLUMNS);
+    hipLaunchKernelGGL(k_few_route<T>, dim3((unsigned)rows), dim3(THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
+                       weights->experts, top, Width::of<T>(x->width), space.plan, tiles);
+    GINEX_LAUNCH_CHECK();
+    const auto kernel = weights->turned ? k_few_experts<T, true> : k_few_experts<T, false>;
+    const int32_t most = pairs < weights->experts ? pairs : weights->experts;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)most), dim3(THREADS), 0, st, read_rows<T>(x), pairs, top, rows,
+                       weights_of<T>(weights), static_cast<const T*>(bias), (int32_t)weights->width,
+                       Width::of<T>(weights->out), activation, space.plan, rows_of<T>(y));
+    GINEX_LAUNCH_CHECK();
+    return GINEX_OK;
+  });
+}

@@ -1,0 +1,350 @@
+// Lookup of rows of a table, and the table's gradient:
+//
+//   out[i] = scale table[ids[i]],   dtable[v] = scale * sum over the i with ids[i] = v of dy[i]
+//
+// Both are bound by HBM.  The gradient adds nothing up by atomics, whose order would be another in every run: (id, position)
+// pairs are sorted by id, stable, and the sorted positions are cut into runs of RUN.  A group of lanes, one for every chunk of
+// 16 bytes of a row, goes through a run.  Ids that begin and end in it are written to the table's gradient; what is left of
+// those that began in front of the run or go on behind it are parts in the workspace, at most two a run.  A second launch adds
+// the parts of an id up in their order, and clears the rows that no id names.
+#include "layers.hpp"
+#include "primitives.hpp"
+
+namespace ginex {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int RUN = 32;           // sorted positions of a group
+constexpr int LONG = 64;          // parts of an id that one group adds up; of more the workgroup does
+
+// ids as sorted by: what is no row of the table comes last.
+template <typename Id>
+struct IdsWithPositions {
+  const Id* ids;
+  uint32_t rows;
+  __device__ __forceinline__ uint64_t operator()(int64_t j) const {
+    const uint64_t id = (uint64_t)(int64_t)ids[j];
+    return (id < rows ? id : rows) << 32 | (uint64_t)j;
+  }
+};
+
+// U chunks a thread, THREADS apart; ids first, then rows, then stores.
+template <typename T, typename Id>
+__global__ __launch_bounds__(THREADS) void k_lookup(RowsOf<const T> table, int64_t rows, const Id* __restrict__ ids,
+                                                    RowsOf<T> out, int64_t first, uint32_t chunks, Divisor cpr,
+                                                    Width width, float scale) {
+  constexpr int N = Chunk<T>::N, U = 4;
+  int32_t c[U];
+  int64_t i[U], id[U];
+  const uint32_t t0 = blockIdx.x * (U * THREADS) + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    uint32_t t = t0 + u * THREADS;
+    t = t < chunks ? t : chunks - 1;
+    const uint32_t row = cpr.of(t);
+    c[u] = (int32_t)(t - row * cpr.d) * N;
+    i[u] = first + row;
+    id[u] = ids[i[u]];
+  }
+  ChunkWords<T> v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    // (a table of no rows may have no memory)
+    if (rows > 0) v[u] = load_words(table.at((uint64_t)id[u] < (uint64_t)rows ? id[u] : 0), c[u], width);
+    else v[u].words = words4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (t0 + u * THREADS >= chunks) break;
+    float f[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) f[n] = (uint64_t)id[u] < (uint64_t)rows ? scale * (float)v[u].wide[n] : 0.f;
+    store_chunk(out.at(i[u]), c[u], width, f);
+  }
+}
+
+__device__ __forceinline__ uint32_t id_of(uint64_t word) { return (uint32_t)(word >> 32); }
+
+// A chunk of f32 sums in the workspace.
+template <int N>
+__device__ __forceinline__ void store_part(float* to, int32_t c, int32_t width, const float (&v)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (c + n < width) to[c + n] = v[n];
+}
+
+template <typename T>
+__device__ __forceinline__ void store_scaled(T* row, int32_t c, Width width, float scale, float (&v)[Chunk<T>::N]) {
+#pragma unroll
+  for (int n = 0; n < Chunk<T>::N; ++n) v[n] *= scale;
+  store_chunk(row, c, width, v);
+}
+
+// parts [runs x 2 x width]: of the id that began in front of the run, and of the one that goes on behind it.  named[v]: id v
+// is there.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void k_lookup_sums(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
+                                                         RowsOf<const T> dy, RowsOf<T> dtable, int32_t shift, Width width,
+                                                         float scale, float* __restrict__ part, uint8_t* __restrict__ named) {
+  constexpr int N = Chunk<T>::N, U = 8;
+  const int64_t run = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> shift;
+  const int64_t begin = run * RUN;
+  if (begin >= n) return;
+  const int64_t end = begin + RUN < n ? begin + RUN : n;
+  const int32_t lane = threadIdx.x & ((1 << shift) - 1), c = ((int32_t)(blockIdx.y << shift) + lane) * N;
+  const uint32_t in_front = begin > 0 ? id_of(sorted[begin - 1]) : 0xFFFFFFFFu;
+  const uint32_t behind = end < n ? id_of(sorted[end]) : 0xFFFFFFFFu;
+  float* const parts = part + run * 2 * width.width;
+  float sum[N] = {};
+  uint32_t id = id_of(sorted[begin]);
+  bool began = id != in_front;              // whether the id that is summed began in this run
+  if (id >= rows) return;
+  const auto flush = [&](bool ends) {
+    if (began && ends) {
+      if (c < width.width) store_scaled(dtable.at(id), c, width, scale, sum);
+    } else {
+      store_part(parts + (began ? width.width : 0), c, width.width, sum);
+    }
+    if (began && c == 0) named[id] = 1;
+  };
+  for (int64_t p = begin; p < end; p += U) {
+    uint64_t word[U];
+    float v[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) word[u] = sorted[p + u < end ? p + u : end - 1];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_chunk(dy.at((uint32_t)word[u]), c, width, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p + u >= end) break;
+      const uint32_t next = id_of(word[u]);
+      if (next != id) {
+        flush(true);
+        id = next;
+        began = true;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.f;
+        if (id >= rows) return;             // ids without a row are the last
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += v[u][i];
+    }
+  }
+  flush(id != behind);
+}
+
+// The run in which the id of a part ends, at or behind run `from`.
+__device__ __forceinline__ int64_t last_run_of(const uint64_t* __restrict__ sorted, int64_t n, uint32_t id, int64_t from) {
+  int64_t lo = from * RUN, hi = n;          // sorted[lo] has the id, behind hi none does
+  while (hi - lo > 1) {
+    const int64_t mid = lo + (hi - lo) / 2;
+    if (id_of(sorted[mid]) == id) lo = mid;
+    else hi = mid;
+  }
+  return lo / RUN;
+}
+
+template <typename T>
+__global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
+                                                         RowsOf<T> dtable, int32_t shift, Width width, float scale,
+                                                         const float* __restrict__ part, const uint8_t* __restrict__ named) {
+  constexpr int N = Chunk<T>::N, U = 4;
+  __shared__ int64_t long_last[THREADS];
+  __shared__ float sums[THREADS][N + 1];
+  const int32_t groups = THREADS >> shift, lane = threadIdx.x & ((1 << shift) - 1), own = threadIdx.x >> shift;
+  const int32_t c = ((int32_t)(blockIdx.y << shift) + lane) * N;
+  const int64_t runs = (n + RUN - 1) / RUN, run = (int64_t)blockIdx.x * groups + own;
+
+  const auto add_parts = [&](float (&sum)[N], int64_t from, int64_t upto, int64_t step) {
+    for (int64_t h = from; h <= upto; h += U * step) {
+      float v[U][N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = h + u * step <= upto ? h + u * step : h;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[u][i] = c + i < width.width ? part[at * 2 * width.width + c + i] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += h + u * step <= upto ? v[u][i] : 0.f;
+    }
+  };
+
+  // an id that begins in this run and goes on behind it
+  bool opens = false;
+  uint32_t id = 0;
+  int64_t last = -1;
+  if (run < runs && (run + 1) * RUN < n) {
+    id = id_of(sorted[(run + 1) * RUN]);
+    opens = id < rows && id_of(sorted[(run + 1) * RUN - 1]) == id && (run == 0 || id_of(sorted[run * RUN - 1]) != id);
+    if (opens) last = last_run_of(sorted, n, id, run + 1);
+  }
+  const bool is_long = opens && last - run > LONG;
+  if (opens && !is_long) {
+    float sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = c + i < width.width ? part[(run * 2 + 1) * width.width + c + i] : 0.f;
+    add_parts(sum, run + 1, last, 1);
+    if (c < width.width) store_scaled(dtable.at(id), c, width, scale, sum);
+  }
+  if (lane == 0) long_last[own] = is_long ? last : -1;
+  __syncthreads();
+  for (int32_t g = 0; g < groups; ++g) {
+    const int64_t upto = long_last[g];
+    if (upto < 0) continue;                 // (the same for all threads)
+    const int64_t from = (int64_t)blockIdx.x * groups + g;
+    float sum[N] = {};
+    add_parts(sum, from + 1 + own, upto, groups);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    if (own == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] = c + i < width.width ? part[(from * 2 + 1) * width.width + c + i] : 0.f;
+      for (int32_t k = 0; k < groups; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += sums[(k << shift) + lane][i];
+      if (c < width.width) store_scaled(dtable.at(id_of(sorted[(from + 1) * RUN])), c, width, scale, sum);
+    }
+    __syncthreads();
+  }
+
+  // rows that no id names
+  for (int64_t v = run; v < rows; v += (int64_t)gridDim.x * groups) {
+    if (named[v] || c >= width.width) continue;
+    const float zero[N] = {};
+    store_chunk(dtable.at(v), c, width, zero);
+  }
+}
+
+struct LookupSpace {
+  uint64_t *a, *b;
+  uint32_t* hist;
+  float* part;
+  uint8_t* named;
+  size_t bytes;
+};
+LookupSpace lookup_space(void* ws, int64_t n, int64_t rows, int64_t width) {
+  Arena arena(ws);
+  LookupSpace s;
+  s.a = arena.take<uint64_t>(n);
+  s.b = arena.take<uint64_t>(n);
+  s.hist = arena.take<uint32_t>(radix_plan(n).hist_elems);
+  s.part = arena.take<float>(ceil_div(n, RUN) * 2 * width);
+  s.named = arena.take<uint8_t>(ceil_div(rows, 4) * 4);
+  s.bytes = arena.used + 256;
+  return s;
+}
+
+int32_t check_lookup_sizes(int64_t ids, int64_t rows, int64_t width) {
+  // (a launch has fewer than 2^32 threads)
+  if (ids < 0 || ids > ((int64_t)1 << 30)) return fail(GINEX_ERR_ARG, "ids=%lld (0..2^30)", (long long)ids);
+  if (rows < 0 || rows >= ((int64_t)1 << 31)) return fail(GINEX_ERR_ARG, "rows=%lld", (long long)rows);
+  if (width < 1 || width > GINEX_MAX_WIDTH) return fail(GINEX_ERR_ARG, "width=%lld (1..%d)", (long long)width, GINEX_MAX_WIDTH);
+  return GINEX_OK;
+}
+
+int32_t check_ids(const void* ids, int32_t ids_64, int64_t n) {
+  if (ids_64 != 0 && ids_64 != 1) return fail(GINEX_ERR_ARG, "ids_64=%d", ids_64);
+  if ((n > 0 && !ids) || reinterpret_cast<uintptr_t>(ids) % (ids_64 ? 8 : 4))
+    return fail(GINEX_ERR_ARG, "ids: null or misaligned");
+  return GINEX_OK;
+}
+
+template <typename Id>
+hipError_t sort_ids(const void* ids, int64_t n, int64_t rows, const LookupSpace& s, hipStream_t st, uint64_t** sorted) {
+  int bits = 1;
+  while (bits < 32 && rows >> bits) ++bits;         // (of the value `rows`, too)
+  const int passes = radix_passes(bits, n);
+  uint64_t *from = nullptr, *to = s.a;
+  int shift = 32;
+  for (int k = 0; k < passes; ++k) {
+    const int width = radix_pass_width(bits, passes, k);
+    const IdsWithPositions<Id> first = {static_cast<const Id*>(ids), (uint32_t)rows};
+    const hipError_t e = k == 0 ? radix_pass(first, to, n, shift, width, s.hist, st)
+                                : radix_pass(RadixWords{from}, to, n, shift, width, s.hist, st);
+    if (e != hipSuccess) return e;
+    from = to;
+    to = from == s.a ? s.b : s.a;
+    shift += width;
+  }
+  *sorted = from;
+  return hipSuccess;
+}
+
+}  // namespace
+}  // namespace ginex
+
+using namespace ginex;
+
+extern "C" int32_t ginex_lookup(const ginex_rows_t* table, const void* ids, int32_t ids_64, float scale,
+                                const ginex_rows_t* out, void* stream) {
+  if (int32_t rc = check_rows("table", table, false)) return rc;
+  if (int32_t rc = check_rows("out", out, true)) return rc;
+  if (int32_t rc = check_same("table", table, "out", out)) return rc;
+  if (int32_t rc = check_ids(ids, ids_64, out->rows)) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return with_type(out->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    constexpr int EACH = 4 * THREADS;
+    const int64_t cpr = ceil_div(out->width, Chunk<T>::N), step = (((int64_t)1 << 31) - EACH) / cpr;
+    for (int64_t r = 0; r < out->rows; r += step) {
+      const int64_t chunks = (out->rows - r < step ? out->rows - r : step) * cpr;
+      const dim3 grid((unsigned)ceil_div(chunks, EACH));
+      if (ids_64)
+        hipLaunchKernelGGL((k_lookup<T, int64_t>), grid, dim3(THREADS), 0, st, read_rows<T>(table), table->rows,
+                           static_cast<const int64_t*>(ids), rows_of<T>(out), r, (uint32_t)chunks, Divisor((uint32_t)cpr),
+                           Width::of<T>(out->width), scale);
+      else
+        hipLaunchKernelGGL((k_lookup<T, int32_t>), grid, dim3(THREADS), 0, st, read_rows<T>(table), table->rows,
+                           static_cast<const int32_t*>(ids), rows_of<T>(out), r, (uint32_t)chunks, Divisor((uint32_t)cpr),
+                           Width::of<T>(out->width), scale);
+      GINEX_LAUNCH_CHECK();
+    }
+    return GINEX_OK;
+  });
+}
+
+extern "C" size_t ginex_lookup_backward_workspace_bytes(int64_t ids, int64_t rows, int64_t width) {
+  if (check_lookup_sizes(ids, rows, width)) return 0;
+  return lookup_space(nullptr, ids, rows, width).bytes;
+}
+
+extern "C" int32_t ginex_lookup_backward(const ginex_rows_t* dy, const void* ids, int32_t ids_64, float scale,
+                                         const ginex_rows_t* dtable, void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t rc = check_rows("dy", dy, false)) return rc;
+  if (int32_t rc = check_rows("dtable", dtable, true)) return rc;
+  if (int32_t rc = check_same("dy", dy, "dtable", dtable)) return rc;
+  if (int32_t rc = check_ids(ids, ids_64, dy->rows)) return rc;
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(GINEX_ERR_ARG, "workspace: null or misaligned");
+  const int64_t n = dy->rows, rows = dtable->rows;
+  if (int32_t rc = check_lookup_sizes(n, rows, dy->width)) return rc;
+  const LookupSpace s = lookup_space(ws, n, rows, dy->width);
+  if (ws_bytes < s.bytes) return fail(GINEX_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", s.bytes, ws_bytes);
+  if (rows == 0) return GINEX_OK;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  GINEX_HIP(fill_async(reinterpret_cast<uint32_t*>(s.named), ceil_div(rows, 4), 0u, st));
+  uint64_t* sorted = nullptr;
+  if (n > 0) GINEX_HIP(ids_64 ? sort_ids<int64_t>(ids, n, rows, s, st, &sorted) : sort_ids<int32_t>(ids, n, rows, s, st, &sorted));
+  return with_type(dy->type, [&](auto t) -> int32_t {
+    using T = decltype(t);
+    const int64_t cpr = ceil_div(dy->width, Chunk<T>::N), runs = ceil_div(n, RUN);
+    int32_t shift = 0;
+    while (shift < 6 && 1 << shift < cpr) ++shift;
+    const unsigned across = (unsigned)ceil_div(cpr, 1 << shift);
+    const Width width = Width::of<T>(dy->width);
+    if (n > 0) {
+      hipLaunchKernelGGL(k_lookup_sums<T>, dim3((unsigned)ceil_div(runs, THREADS >> shift), across), dim3(THREADS), 0, st,
+                         sorted, n, (uint32_t)rows, read_rows<T>(dy), rows_of<T>(dtable), shift, width, scale, s.part, s.named);
+      GINEX_LAUNCH_CHECK();
+    }
+    // a group for every run, and enough of them for the rows that are cleared
+    int64_t groups = rows < 16384 ? rows : 16384;
+    groups = groups > runs ? groups : runs;
+    hipLaunchKernelGGL(k_lookup_join<T>, dim3((unsigned)ceil_div(groups, THREADS >> shift), across), dim3(THREADS), 0, st, sorted,
+                       n, (uint32_t)rows, rows_of<T>(dtable), shift, width, scale, s.part, s.named);
+    GINEX_LAUNCH_CHECK();
+    return GINEX_OK;
+  });
+}

@@ -115,6 +115,13 @@ __device__ __forceinline__ void store_chunk(T* row, int32_t c, Width w, const fl
   store_words(row, c, w, u);
 }
 
+// Waits for this wave's LDS accesses and for the other waves, not for loads from HBM that are under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // n / d for n below 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers
 // using multiplication", 1994).
 struct Divisor {
@@ -195,6 +202,18 @@ inline int32_t check_same(const char* a_is, const ginex_rows_t* a, const char* b
   if (a->type != b->type) return fail(GINEX_ERR_ARG, "%s and %s differ in type", a_is, b_is);
   if (a->width != b->width)
     return fail(GINEX_ERR_ARG, "%s and %s differ in width: %lld and %lld", a_is, b_is, (long long)a->width, (long long)b->width);
+  return GINEX_OK;
+}
+
+inline int32_t check_activation(int32_t activation, int32_t least) {
+  if (activation < least || activation > GINEX_ACT_GELU) return fail(GINEX_ERR_ARG, "unknown activation %d", activation);
+  return GINEX_OK;
+}
+
+inline int32_t check_kept(const char* what, const ginex_rows_t* r, const ginex_codes_t* kept) {
+  if (r->rows != kept->rows || r->width != kept->width)
+    return fail(GINEX_ERR_ARG, "%s is %lld x %lld, the codes %lld x %lld", what, (long long)r->rows, (long long)r->width,
+                (long long)kept->rows, (long long)kept->width);
   return GINEX_OK;
 }
 

@@ -97,13 +97,6 @@ __device__ __forceinline__ int32_t find_range(const int64_t* __restrict__ offset
   return first;
 }
 
-// Waits for this wave's LDS accesses and for the other waves, not for loads from HBM that are under way.
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // The upper halves of two f32: two bf16 in a word.
 __device__ __forceinline__ uint32_t upper_halves(float first, float second) {
   return __builtin_amdgcn_perm(__float_as_uint(second), __float_as_uint(first), 0x07060302u);
