@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libginex.so")
 SOURCES = ["core.cpp", "gather.hip", "sampler.hip", "changeset.hip", "neighbor_cache.hip",
-           "static_policy.hip", "route.hip", "rows.hip", "codes.hip", "weights.hip", "linear.hip", "few.hip",
+           "static_policy.hip", "route.hip", "rows.hip", "codes.hip", "weights.hip", "linear.hip", "resident.hip", "few.hip",
            "bias.hip", "norm.hip", "lookup.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall",

@@ -16,15 +16,38 @@
 namespace ginex {
 namespace {
 
-constexpr int THREADS = 512, WAVES = THREADS / WAVE;
-constexpr int TILES = GINEX_MAX_FEW_ROWS / 16;            // of 16 rows
+constexpr int ROUTE_THREADS = 1024, ROUTE_WAVES = ROUTE_THREADS / WAVE;
 constexpr int PITCH = WAVE_COLUMNS + 4;                   // of a row of sums in LDS: 16 rows of 4 words use every bank once
 constexpr int MOST_PAIRS = GINEX_MAX_FEW_ROWS * GINEX_MAX_FEW_TOP;
 
-__device__ __forceinline__ double sum_of_wave(double v) {
-#pragma unroll
-  for (int d = 1; d < WAVE; d *= 2) v += __shfl_xor(v, d, WAVE);
-  return v;
+// The sum over a wave, in its last lane: lane by lane inside rows of 16 (DPP), then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double plus_lane(double v) {
+  return v + __longlong_as_double((long long)dpp_or_zero<CTRL, ROWS>((uint64_t)__double_as_longlong(v)));
+}
+__device__ __forceinline__ double sum_to_last(double v) {
+  v = plus_lane<0x111, 0xF>(v);     // row_shr:1
+  v = plus_lane<0x112, 0xF>(v);
+  v = plus_lane<0x114, 0xF>(v);
+  v = plus_lane<0x118, 0xF>(v);
+  v = plus_lane<0x142, 0xA>(v);     // row_bcast:15
+  return plus_lane<0x143, 0xC>(v);  // row_bcast:31
+}
+
+// The largest number of a wave, in all lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t or_lane(uint32_t v) {
+  const uint32_t other = dpp_or_zero<CTRL, ROWS>(v);
+  return v > other ? v : other;
+}
+__device__ __forceinline__ uint32_t most_of_wave(uint32_t v) {
+  v = or_lane<0x111, 0xF>(v);
+  v = or_lane<0x112, 0xF>(v);
+  v = or_lane<0x114, 0xF>(v);
+  v = or_lane<0x118, 0xF>(v);
+  v = or_lane<0x142, 0xA>(v);
+  v = or_lane<0x143, 0xC>(v);
+  return of_lane(v, WAVE - 1);
 }
 
 // A score as a number that is larger where the score is; NaN is the largest, 0 is smaller than all.
@@ -38,38 +61,46 @@ __device__ __forceinline__ uint64_t rank_of(double v) {
 struct Plan {
   int32_t* chosen;      // [rows x top]
   float* share;         // [rows x top]
-  uint32_t* done;       // workgroups of 64 columns that are through
+  uint32_t* done;       // pairs of which 64 columns are through
   float* part;          // [rows x top x out]
 };
 
 // A workgroup a row.  Products in f64 are exact for all types, so what is chosen does not depend on how a sum is rounded
 // (but for scores that are equal to 2^-50 or so).
 template <typename T>
-__global__ __launch_bounds__(THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
+__global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
                                                        int32_t top, Width width, Plan plan, int32_t tiles) {
   constexpr int N = Chunk<T>::N, U = 4, EACH = GINEX_MAX_EXPERTS / WAVE;
   __shared__ double scores[GINEX_MAX_EXPERTS];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   const T* const row = x.at(blockIdx.x);
   if (blockIdx.x == 0)
-    for (int32_t i = threadIdx.x; i < tiles; i += THREADS) plan.done[i] = 0;
-  for (int32_t e0 = wave; e0 < experts; e0 += U * WAVES) {
+    for (int32_t i = threadIdx.x; i < tiles; i += ROUTE_THREADS) plan.done[i] = 0;
+  for (int32_t e0 = wave; e0 < experts; e0 += U * ROUTE_WAVES) {
     double sum[U] = {};
-    for (int32_t c = lane * N; c < width.width; c += WAVE * N) {
-      float a[N], b[U][N];
-      load_chunk(row, c, width, a);
+    // two chunks of U experts in flight
+    for (int32_t c0 = lane * N; c0 < width.width; c0 += 2 * WAVE * N) {
+      ChunkWords<T> a[2], b[2][U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) load_chunk(router.at(e0 + u * WAVES < experts ? e0 + u * WAVES : e0), c, width, b[u]);
+      for (int k = 0; k < 2; ++k) {
+        const int32_t c = c0 + k * WAVE * N;
+        a[k] = load_words(row, c, width);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u)
+          b[k][u] = load_words(router.at(e0 + u * ROUTE_WAVES < experts ? e0 + u * ROUTE_WAVES : e0), c, width);
+      }
 #pragma unroll
-        for (int n = 0; n < N; ++n) sum[u] = fma((double)a[n], (double)b[u][n], sum[u]);
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int n = 0; n < N; ++n) sum[u] = fma((double)(float)a[k].wide[n], (double)(float)b[k][u].wide[n], sum[u]);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const double total = sum_of_wave(sum[u]);
-      if (lane == 0 && e0 + u * WAVES < experts) scores[e0 + u * WAVES] = total;
-    }
+    for (int u = 0; u < U; ++u) sum[u] = sum_to_last(sum[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (lane == WAVE - 1 && e0 + u * ROUTE_WAVES < experts) scores[e0 + u * ROUTE_WAVES] = sum[u];
   }
   __syncthreads();
   if (wave > 0) return;
@@ -79,119 +110,78 @@ __global__ __launch_bounds__(THREADS) void k_few_route(RowsOf<const T> x, RowsOf
   int32_t mine = 0;           // lane j has choice j
   for (int32_t j = 0; j < top; ++j) {
     uint64_t best = rank[0];
-    int32_t at = lane;
+    uint32_t at = lane;
 #pragma unroll
     for (int i = 1; i < EACH; ++i)
-      if (rank[i] > best) {
+      if (i * WAVE < experts && rank[i] > best) {
         best = rank[i];
         at = lane + i * WAVE;
       }
-#pragma unroll
-    for (int d = 1; d < WAVE; d *= 2) {
-      const uint64_t other = (uint64_t)__shfl_xor((unsigned long long)best, d, WAVE);
-      const int32_t where = __shfl_xor(at, d, WAVE);
-      if (other > best || (other == best && where < at)) {
-        best = other;
-        at = where;
-      }
-    }
+    // the largest rank, its upper half first, and of those that have it the first expert
+    const uint32_t hi = most_of_wave((uint32_t)(best >> 32));
+    const uint32_t lo = most_of_wave(best >> 32 == hi ? (uint32_t)best : 0);
+    at = ~most_of_wave(best == ((uint64_t)hi << 32 | lo) ? ~at : 0);
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      if (at == lane + i * WAVE) rank[i] = 0;
-    if (lane == j) mine = at;
+      if (i * WAVE < experts && at == (uint32_t)(lane + i * WAVE)) rank[i] = 0;
+    if (lane == j) mine = (int32_t)at;
   }
   const double score = scores[mine], most = __shfl(score, 0, WAVE);
-  const double weight = lane < top ? exp(score - most) : 0.0, total = sum_of_wave(weight);
+  const double weight = lane < top ? exp(score - most) : 0.0, total = __shfl(sum_to_last(weight), WAVE - 1, WAVE);
   if (lane < top) {
     plan.chosen[(int64_t)blockIdx.x * top + lane] = mine;
     plan.share[(int64_t)blockIdx.x * top + lane] = (float)(weight / total);
   }
 }
 
-// Four neighbouring columns of a row of weights, from column n on; what is behind the last one is 0.
-template <typename T>
-__device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t n, int32_t columns) {
-  typename Four<T>::Wide v;
-  if (columns < 4) {
-#pragma unroll
-    for (int l = 0; l < 4; ++l) v[l] = n + l < columns ? row[n + l] : (T)0.f;
-    return v;
-  }
-  const int32_t over = n + 4 - columns;       // the last ones are read so that they end with the row, and moved
-  v = *reinterpret_cast<const typename Four<T>::At*>(row + (over > 0 ? columns - 4 : n));
-  if (over > 0) {
-#pragma unroll
-    for (int l = 0; l < 4; ++l) {
-      T to = (T)0.f;
-#pragma unroll
-      for (int m = l + 1; m < 4; ++m) to = m == l + over ? v[m] : to;
-      v[l] = to;
-    }
-  }
-  return v;
-}
-
-// Rows of one expert and their sums: x[row(i)] W for i < count, in `room` [wave][row][column] in the end, 16 rows at a time.
+// Rows of one expert and their sums: x[row(i)] W for i < count <= 16; of column 4 (lane % 16) + j of the workgroup's in operand j.
 // `row_of(i)` is the row of x, negative for a row of zeros.
-template <typename T, bool TURNED, typename RowOf>
+template <typename T, bool TURNED, int WAVES, typename RowOf>
 __device__ __forceinline__ void few_sums(RowsOf<const T> x, const T* __restrict__ w, int64_t stride, int32_t width, Width out,
-                                         int32_t n0, int32_t count, RowOf row_of, float4v (&sum)[TILES][4]) {
+                                         int32_t n0, int32_t count, RowOf row_of, float4v (&sum)[4]) {
   constexpr int N = Chunk<T>::N, STEP = 4 * N, UNIT = 2 * STEP;       // a unit is 128 bytes of a row
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), group = lane / 16;
   const Width along = {width, (int32_t)((width + N - 1) / N * N - width)};
-  const T* row[TILES];
-  bool there[TILES];
-#pragma unroll
-  for (int m = 0; m < TILES; ++m) {
-    const int32_t i = m * 16 + lane % 16;
-    const int64_t r = row_of(i < count ? i : 0);
-    there[m] = r >= 0;
-    row[m] = x.at(r >= 0 ? r : 0);
-  }
-  const int32_t n = n0 + lane % 16 * 4;         // this lane's columns: row lane % 16 of operand j is column n + j
+  const int64_t r = row_of(lane % 16 < count ? lane % 16 : 0);
+  const T* const row = x.at(r >= 0 ? r : 0);
+  const int32_t n = n0 + lane % 16 * 4;
   for (int32_t k0 = wave * UNIT; k0 < width; k0 += WAVES * UNIT) {
-    ChunkWords<T> fb[2][4];
-    if (TURNED) {
+    ChunkWords<T> fa[2], fb[2][4];
+    typename Four<T>::Wide raw[2][N];
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
+      const int32_t k1 = k0 + s * STEP + group * N;
+      if (TURNED) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int32_t at = n + j < out.width ? n + j : out.width - 1;
-          fb[s][j] = load_words(w + at * stride, k0 + s * STEP + group * N, along);
-        }
-    } else {
-      typename Four<T>::Wide raw[2][N];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int j = 0; j < 4; ++j) fb[s][j] = load_words(w + (n + j < out.width ? n + j : out.width - 1) * stride, k1, along);
+      } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int32_t k = k0 + s * STEP + group * N + i;
+          const int32_t k = k1 + i;
           raw[s][i] = four_of(w + (int64_t)(k < width ? k : width - 1) * stride, n < out.width ? n : out.width - 1, out.width);
           if (k >= width) raw[s][i] = (typename Four<T>::Wide)(T)0.f;
         }
+      }
+      fa[s] = load_words(row, k1, along);
+    }
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {
+      if (!TURNED) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int i = 0; i < N; ++i) fb[s][j].wide[i] = raw[s][i][j];
-    }
-#pragma unroll
-    for (int m = 0; m < TILES; ++m) {
-      if (m * 16 >= count) break;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        ChunkWords<T> fa = load_words(row[m], k0 + s * STEP + group * N, along);
-        if (!there[m]) fa.words = words4{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[m][j] = product(fb[s][j], fa, sum[m][j]);
       }
+      if (r < 0) fa[s].words = words4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] = product(fb[s][j], fa[s], sum[j]);
     }
   }
 }
 
-// The waves' sums of 16 rows, added up: thread t gets rows t / 64 and t / 64 + 8 of column t % 64.
-__device__ __forceinline__ void join_waves(const float4v (&sum)[4], float (*room)[16][PITCH], float (&v)[2]) {
+// The waves' sums of 16 rows, added up: wave w gets rows w, w + WAVES, .. of the column that is its lane's.
+template <int WAVES>
+__device__ __forceinline__ void join_waves(const float4v (&sum)[4], float (*room)[16][PITCH], float (&v)[16 / WAVES]) {
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   __syncthreads();
   // lane's row is lane % 16; component i of operand j's sums is column 16 (lane / 16) + 4 i + j
@@ -200,99 +190,124 @@ __device__ __forceinline__ void join_waves(const float4v (&sum)[4], float (*room
     *reinterpret_cast<float4v*>(&room[wave][lane % 16][lane / 16 * 16 + 4 * i]) = float4v{sum[0][i], sum[1][i], sum[2][i], sum[3][i]};
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < 16 / WAVES; ++h) {
     v[h] = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) v[h] += room[w][wave + h * WAVES][lane];
   }
 }
 
-template <typename T, bool TURNED>
-__global__ __launch_bounds__(THREADS) void k_few_experts(RowsOf<const T> x, int32_t pairs, int32_t top, int32_t rows,
-                                                         WeightsOf<T> weights, const T* __restrict__ bias, int32_t width,
-                                                         Width out, int32_t activation, Plan plan, RowsOf<T> y) {
+template <typename T, bool TURNED, int WAVES>
+__global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, int32_t pairs, int32_t top, int32_t rows,
+                                                                    WeightsOf<T> weights, const T* __restrict__ bias,
+                                                                    int32_t width, Width out, int32_t activation, Plan plan,
+                                                                    RowsOf<T> y) {
+  constexpr int THREADS = WAVES * WAVE;
   __shared__ uint32_t used[GINEX_MAX_EXPERTS / 32];
-  __shared__ int32_t list[GINEX_MAX_FEW_ROWS];          // the expert's pairs
-  __shared__ int32_t listed, is_last;
+  __shared__ int32_t chosen[MOST_PAIRS], list[16];      // the experts of all pairs, and the workgroup's pairs
+  __shared__ int32_t is_last;
   __shared__ float room[WAVES][16][PITCH];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
-  // the experts that are chosen at all: the workgroup has the blockIdx.y-th of them
-  if (threadIdx.x < GINEX_MAX_EXPERTS / 32) used[threadIdx.x] = 0;
-  int32_t mine[MOST_PAIRS / THREADS];
+  int32_t expert, count;
+  if (rows == 1) {                  // a row's experts are all different
+    if (blockIdx.z > 0) return;
+    expert = plan.chosen[blockIdx.y];
+    if (threadIdx.x == 0) list[0] = blockIdx.y;
+    count = 1;
+    __syncthreads();
+  } else {
+    // the experts that are chosen at all: the workgroup has the blockIdx.y-th of them
+    if (threadIdx.x < GINEX_MAX_EXPERTS / 32) used[threadIdx.x] = 0;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < MOST_PAIRS / THREADS; ++i) {
-    const int32_t p = threadIdx.x + i * THREADS;
-    mine[i] = p < pairs ? plan.chosen[p] : -1;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < MOST_PAIRS / THREADS; ++i)
-    if (mine[i] >= 0) atomicOr(&used[mine[i] / 32], 1u << mine[i] % 32);
-  __syncthreads();
-  const uint32_t word = lane < GINEX_MAX_EXPERTS / 32 ? used[lane] : 0;
-  const uint32_t upto = wave_inclusive_scan((uint32_t)__popc(word)), distinct = of_lane(upto, WAVE - 1);
-  if (blockIdx.y >= distinct) return;
-  const int at = __ffsll((unsigned long long)__ballot(upto > blockIdx.y)) - 1;
-  uint32_t bits = of_lane(word, at);
-  for (uint32_t skip = blockIdx.y - (of_lane(upto, at) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
-  const int32_t expert = at * 32 + __ffs((int)bits) - 1;
-  // its pairs, in their order (a row has an expert once: no more than there are rows)
-  if (wave == 0) {
-    int32_t have = 0;
+    for (int i = 0; i < MOST_PAIRS / THREADS; ++i) {
+      const int32_t p = threadIdx.x + i * THREADS;
+      if (p < pairs) {
+        const int32_t e = plan.chosen[p];
+        chosen[p] = e;
+        atomicOr(&used[e / 32], 1u << e % 32);
+      }
+    }
+    __syncthreads();
+    const uint32_t word = lane < GINEX_MAX_EXPERTS / 32 ? used[lane] : 0;
+    const uint32_t upto = wave_inclusive_scan((uint32_t)__popc(word));
+    if (blockIdx.y >= of_lane(upto, WAVE - 1)) return;
+    const int at = __ffsll((unsigned long long)__ballot(upto > blockIdx.y)) - 1;
+    uint32_t bits = of_lane(word, at);
+    for (uint32_t skip = blockIdx.y - (of_lane(upto, at) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
+    expert = at * 32 + __ffs((int)bits) - 1;
+    // its pairs in their order, of which this workgroup has 16; every wave finds them
+    int32_t have = -(int32_t)blockIdx.z * 16;
     for (int32_t p0 = 0; p0 < pairs; p0 += WAVE) {
-      const bool is = p0 + lane < pairs && plan.chosen[p0 + lane] == expert;
+      const bool is = p0 + lane < pairs && chosen[p0 + lane] == expert;
       const uint64_t who = __ballot(is);
       const int32_t place = have + __popcll(who & (((uint64_t)1 << lane) - 1));
-      if (is && place < GINEX_MAX_FEW_ROWS) list[place] = p0 + lane;
+      if (is && wave == 0 && place >= 0 && place < 16) list[place] = p0 + lane;
       have += __popcll(who);
     }
-    if (lane == 0) listed = have < GINEX_MAX_FEW_ROWS ? have : GINEX_MAX_FEW_ROWS;
+    if (have <= 0) return;
+    count = have < 16 ? have : 16;
+    __syncthreads();
   }
-  __syncthreads();
-  const int32_t count = listed, n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
-  float4v sum[TILES][4] = {};
-  few_sums<T, TURNED>(x, weights.of(expert), weights.stride, width, out, n0, count,
-                      [&](int32_t i) { return (int64_t)(list[i] / top); }, sum);
+  const int32_t n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
+  float4v sum[4] = {};
+  few_sums<T, TURNED, WAVES>(x, weights.of(expert), weights.stride, width, out, n0, count,
+                             [&](int32_t i) { return (int64_t)(list[i] / top); }, sum);
   const float b = bias && c < out.width ? (float)bias[(int64_t)expert * out.width + c] : 0.f;
+  float v[16 / WAVES];
+  join_waves<WAVES>(sum, room, v);
 #pragma unroll
-  for (int m = 0; m < TILES; ++m) {
-    if (m * 16 >= count) break;
-    float v[2];
-    join_waves(sum[m], room, v);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t i = m * 16 + wave + h * WAVES;
-      if (i < count && c < out.width)
-        __hip_atomic_store(plan.part + (int64_t)list[i] * out.width + c, activated_by<sizeof(T) == 4>(activation, v[h] + b),
-                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+  for (int h = 0; h < 16 / WAVES; ++h) {
+    const int32_t i = wave + h * WAVES;
+    if (i < count && c < out.width)
+      __hip_atomic_store(plan.part + (int64_t)list[i] * out.width + c, activated_by<sizeof(T) == 4>(activation, v[h] + b),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  // The last workgroup of these columns to come here finds what the others have left, whichever die they were on.
-  __threadfence();
+  // The last workgroup of these columns to come here finds what the others have left, whichever die they were on: stores and
+  // loads of that go past the dies' caches, and every wave waits for its stores before one thread counts its pairs.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)
-    is_last = __hip_atomic_fetch_add(plan.done + blockIdx.x, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == distinct - 1;
+    is_last = (int32_t)__hip_atomic_fetch_add(plan.done + blockIdx.x, (uint32_t)count, __ATOMIC_ACQ_REL,
+                                              __HIP_MEMORY_SCOPE_AGENT) + count == pairs;
   __syncthreads();
-  if (!is_last) return;
-  __threadfence();
-  if (c >= out.width) return;
-  for (int32_t r = wave; r < rows; r += WAVES) {
-    float total = 0.f;
-    for (int32_t j = 0; j < top; ++j) {
-      const int32_t p = r * top + j;
-      total = fmaf(plan.share[p],
-                   __hip_atomic_load(plan.part + (int64_t)p * out.width + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), total);
+  if (!is_last || c >= out.width) return;
+  // a wave has some rows, whose pairs are neighbours: U of them in flight
+  constexpr int U = 16;
+  const float* const part = plan.part + c;
+  const int32_t each = (rows + WAVES - 1) / WAVES;
+  const int32_t first = wave * each * top, end = (wave + 1) * each < rows ? (wave + 1) * each * top : pairs;
+  int32_t r = wave * each, j = 0;
+  float total = 0.f;
+  for (int32_t p0 = first; p0 < end; p0 += U) {
+    float v[U], share[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t p = p0 + u < end ? p0 + u : end - 1;
+      share[u] = plan.share[p];
+      v[u] = __hip_atomic_load(part + (int64_t)p * out.width, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    y.at(r)[c] = (T)total;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool there = p0 + u < end;
+      total = there ? fmaf(share[u], v[u], total) : total;
+      j += there ? 1 : 0;
+      if (j == top) {
+        y.at(r)[c] = (T)total;
+        total = 0.f;
+        j = 0;
+        ++r;
+      }
+    }
   }
 }
 
 // A group a workgroup: an expert's slots, those without one, or all rows.
-template <typename T, bool TURNED>
-__global__ __launch_bounds__(THREADS) void k_few_linear(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights,
-                                                        const int32_t* __restrict__ source,
-                                                        const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
-                                                        int32_t width, Width out, Epilogue e) {
+template <typename T, bool TURNED, int WAVES>
+__global__ __launch_bounds__(WAVES* WAVE) void k_few_linear(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights,
+                                                                   const int32_t* __restrict__ source,
+                                                                   const int64_t* __restrict__ offsets, int32_t experts,
+                                                                   int64_t slots, int32_t width, Width out, Epilogue e) {
   __shared__ float room[WAVES][16][PITCH];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   const int32_t expert = blockIdx.y;
@@ -306,51 +321,48 @@ __global__ __launch_bounds__(THREADS) void k_few_linear(RowsOf<const T> x, int64
       begin = inside(offsets[experts], slots);
     }
   }
-  const int32_t count = (int32_t)(end - begin), n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
-  if (count <= 0) return;
+  begin += (int64_t)blockIdx.z * 16;        // 16 rows a workgroup
+  if (begin >= end) return;
+  const int32_t count = (int32_t)(end - begin < 16 ? end - begin : 16), n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
   const bool none = expert == experts;        // slots without an expert are cleared
-  float4v sum[TILES][4] = {};
+  float4v sum[4] = {};
   if (!none)
-    few_sums<T, TURNED>(x, weights.of(expert), weights.stride, width, out, n0, count,
-                        [&](int32_t i) -> int64_t {
-                          const int64_t r = source ? (int64_t)source[begin + i] : begin + i;
-                          return r < rows ? r : -1;
-                        },
-                        sum);
+    few_sums<T, TURNED, WAVES>(x, weights.of(expert), weights.stride, width, out, n0, count,
+                               [&](int32_t i) -> int64_t {
+                                 const int64_t r = source ? (int64_t)source[begin + i] : begin + i;
+                                 return r < rows ? r : -1;
+                               },
+                               sum);
   const float b = !none && e.bias && c < out.width
                       ? (float)static_cast<const T*>(e.bias)[(int64_t)expert * out.width + c] : 0.f;
+  float v[16 / WAVES];
+  join_waves<WAVES>(sum, room, v);
 #pragma unroll
-  for (int m = 0; m < TILES; ++m) {
-    if (m * 16 >= count) break;
-    float v[2];
-    join_waves(sum[m], room, v);
+  for (int h = 0; h < 16 / WAVES; ++h) {
+    const int32_t i = wave + h * WAVES;
+    if (i >= count) continue;               // (the same for the wave)
+    const int64_t r = begin + i;
+    v[h] = c < out.width ? v[h] + b : 0.f;
+    if (e.codes) {
+      // a block is half of the wave
+      uint32_t most = __float_as_uint(v[h]) & 0x7FFFFFFFu;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t i = m * 16 + wave + h * WAVES;
-      if (i >= count) continue;               // (the same for the wave)
-      const int64_t r = begin + i;
-      v[h] = c < out.width ? v[h] + b : 0.f;
-      if (e.codes) {
-        // a block is half of the wave
-        uint32_t most = __float_as_uint(v[h]) & 0x7FFFFFFFu;
-#pragma unroll
-        for (int d = 1; d < GINEX_CODE_BLOCK; d *= 2) {
-          const uint32_t other = (uint32_t)__shfl_xor((int)most, d, WAVE);
-          most = most > other ? most : other;
-        }
-        const uint32_t scale = scale_byte(most);
-        constexpr float whole = 12582912.f;
-        const float q = __builtin_amdgcn_fmed3f(fmaf(v[h], to_codes(scale), whole), whole - 127.f, whole + 127.f);
-        if (c < e.blocks * GINEX_CODE_BLOCK) {
-          e.codes[r * ((int64_t)e.blocks * GINEX_CODE_BLOCK) + c] = scale == NO_NUMBER ? 0 : (int8_t)__float_as_uint(q);
-          if (c % GINEX_CODE_BLOCK == 0) e.scales[r * e.blocks + c / GINEX_CODE_BLOCK] = (uint8_t)scale;
-        }
+      for (int d = 1; d < GINEX_CODE_BLOCK; d *= 2) {
+        const uint32_t other = (uint32_t)__shfl_xor((int)most, d, WAVE);
+        most = most > other ? most : other;
       }
-      if (c >= out.width) continue;
-      float to = none ? 0.f : activated_by<sizeof(T) == 4>(e.activation, v[h]);
-      if (e.residual && !none) to += (float)static_cast<const T*>(e.residual)[r * e.residual_stride + c];
-      static_cast<T*>(e.y)[r * e.y_stride + c] = (T)to;
+      const uint32_t scale = scale_byte(most);
+      constexpr float whole = 12582912.f;
+      const float q = __builtin_amdgcn_fmed3f(fmaf(v[h], to_codes(scale), whole), whole - 127.f, whole + 127.f);
+      if (c < e.blocks * GINEX_CODE_BLOCK) {
+        e.codes[r * ((int64_t)e.blocks * GINEX_CODE_BLOCK) + c] = scale == NO_NUMBER ? 0 : (int8_t)__float_as_uint(q);
+        if (c % GINEX_CODE_BLOCK == 0) e.scales[r * e.blocks + c / GINEX_CODE_BLOCK] = (uint8_t)scale;
+      }
     }
+    if (c >= out.width) continue;
+    float to = none ? 0.f : activated_by<sizeof(T) == 4>(e.activation, v[h]);
+    if (e.residual && !none) to += (float)static_cast<const T*>(e.residual)[r * e.residual_stride + c];
+    static_cast<T*>(e.y)[r * e.y_stride + c] = (T)to;
   }
 }
 
@@ -379,19 +391,34 @@ int32_t check_few(int64_t rows, int32_t top, int32_t experts, int64_t width, int
   return GINEX_OK;
 }
 
+// Calls `go` with the waves of a workgroup: as many as the width has units of 128 bytes, 4, 8, or 16 where there are few
+// workgroups.
+template <typename Go>
+int32_t with_waves(int64_t width, int32_t bytes, int64_t groups, Go go) {
+  const int64_t units = ceil_div(width * bytes, 128);
+  if (units <= 4) return go(std::integral_constant<int, 4>{});
+  if (units <= 8 || groups > 256) return go(std::integral_constant<int, 8>{});
+  return go(std::integral_constant<int, 16>{});
+}
+
 }  // namespace
 
 int32_t linear_few(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot, int64_t slots,
                    const Epilogue& epilogue, hipStream_t st) {
   return with_type(x->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const auto kernel = w->turned ? k_few_linear<T, true> : k_few_linear<T, false>;
-    const dim3 grid((unsigned)ceil_div(w->out, WAVE_COLUMNS), route ? (unsigned)route->experts + 1 : 1);
-    hipLaunchKernelGGL(kernel, grid, dim3(THREADS), 0, st, read_rows<T>(x), x->rows, weights_of<T>(w),
-                       route && !by_slot ? route->source : nullptr, route ? route->offsets : nullptr, w->experts, slots,
-                       (int32_t)w->width, Width::of<T>(w->out), epilogue);
-    GINEX_LAUNCH_CHECK();
-    return GINEX_OK;
+    const int64_t groups = ceil_div(w->out, WAVE_COLUMNS) * (route && slots > w->experts ? w->experts : route ? slots : 1);
+    return with_waves(w->width, sizeof(T), groups, [&](auto waves) -> int32_t {
+      constexpr int WAVES = decltype(waves)::value;
+      const auto kernel = w->turned ? k_few_linear<T, true, WAVES> : k_few_linear<T, false, WAVES>;
+      const dim3 grid((unsigned)ceil_div(w->out, WAVE_COLUMNS), route ? (unsigned)route->experts + 1 : 1,
+                      (unsigned)ceil_div(slots, 16));
+      hipLaunchKernelGGL(kernel, grid, dim3(WAVES * WAVE), 0, st, read_rows<T>(x), x->rows, weights_of<T>(w),
+                         route && !by_slot ? route->source : nullptr, route ? route->offsets : nullptr, w->experts, slots,
+                         (int32_t)w->width, Width::of<T>(w->out), epilogue);
+      GINEX_LAUNCH_CHECK();
+      return GINEX_OK;
+    });
   });
 }
 
@@ -432,15 +459,19 @@ extern "C" int32_t ginex_expert_layer(const ginex_rows_t* x, const ginex_rows_t*
     using T = decltype(t);
     const int32_t rows = (int32_t)x->rows, pairs = rows * top;
     const int32_t tiles = (int32_t)ceil_div(weights->out, WAVE_COLUMNS);
-    hipLaunchKernelGGL(k_few_route<T>, dim3((unsigned)rows), dim3(THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
+    hipLaunchKernelGGL(k_few_route<T>, dim3((unsigned)rows), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
                        weights->experts, top, Width::of<T>(x->width), space.plan, tiles);
     GINEX_LAUNCH_CHECK();
-    const auto kernel = weights->turned ? k_few_experts<T, true> : k_few_experts<T, false>;
     const int32_t most = pairs < weights->experts ? pairs : weights->experts;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)most), dim3(THREADS), 0, st, read_rows<T>(x), pairs, top, rows,
-                       weights_of<T>(weights), static_cast<const T*>(bias), (int32_t)weights->width,
-                       Width::of<T>(weights->out), activation, space.plan, rows_of<T>(y));
-    GINEX_LAUNCH_CHECK();
-    return GINEX_OK;
+    return with_waves(weights->width, sizeof(T), (int64_t)tiles * most, [&](auto waves) -> int32_t {
+      constexpr int WAVES = decltype(waves)::value;
+      const auto kernel = weights->turned ? k_few_experts<T, true, WAVES> : k_few_experts<T, false, WAVES>;
+      const dim3 grid((unsigned)tiles, (unsigned)most, (unsigned)ceil_div(rows, 16));
+      hipLaunchKernelGGL(kernel, grid, dim3(WAVES * WAVE), 0, st, read_rows<T>(x), pairs, top, rows, weights_of<T>(weights),
+                         static_cast<const T*>(bias), (int32_t)weights->width, Width::of<T>(weights->out), activation,
+                         space.plan, rows_of<T>(y));
+      GINEX_LAUNCH_CHECK();
+      return GINEX_OK;
+    });
   });
 }

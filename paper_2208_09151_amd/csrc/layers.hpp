@@ -40,6 +40,29 @@ struct Four {
   typedef Wide At __attribute__((aligned(sizeof(T))));
 };
 
+// Four neighbouring columns of a row of weights, from column n on; what is behind the last one is 0.
+template <bool WIDE = false, typename T>
+__device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t n, int32_t columns) {
+  typename Four<T>::Wide v;
+  if (!WIDE && columns < 4) {
+#pragma unroll
+    for (int l = 0; l < 4; ++l) v[l] = n + l < columns ? row[n + l] : (T)0.f;
+    return v;
+  }
+  const int32_t over = n + 4 - columns;       // the last ones are read so that they end with the row, and moved
+  v = *reinterpret_cast<const typename Four<T>::At*>(row + (over > 0 ? columns - 4 : n));
+  if (over > 0) {
+#pragma unroll
+    for (int l = 0; l < 4; ++l) {
+      T to = (T)0.f;
+#pragma unroll
+      for (int m = l + 1; m < 4; ++m) to = m == l + over ? v[m] : to;
+      v[l] = to;
+    }
+  }
+  return v;
+}
+
 // What happens to the sums of a linear layer.
 struct Epilogue {
   const void* bias;
@@ -57,6 +80,11 @@ struct Epilogue {
 constexpr int64_t FEW_ROWS = GINEX_MAX_FEW_ROWS;
 int32_t linear_few(const ginex_rows_t* x, const ginex_weights_t* weights, const ginex_routing_t* route, bool by_slot,
                    int64_t slots, const Epilogue& epilogue, hipStream_t st);
+
+// A linear layer of many rows whose weights find room in LDS; false: not for these sizes.
+bool resident_fits(const ginex_weights_t* weights, int64_t slots, bool routed);
+int32_t linear_resident(const ginex_rows_t* x, const ginex_weights_t* weights, const ginex_routing_t* route, bool by_slot,
+                        int64_t slots, const Epilogue& epilogue, hipStream_t st);
 
 // The rows that a tile has: `first` .. `end` - 1, at most as many as a tile takes are its own.  expert == experts: the rows that no
 // expert has.
@@ -95,6 +123,22 @@ __device__ __forceinline__ bool find_tile(const int64_t* __restrict__ offsets, i
     before = of_lane(upto, WAVE - 1);
   }
   return false;
+}
+
+// How many tiles there are.
+__device__ __forceinline__ uint32_t count_tiles(const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
+                                                int32_t height) {
+  uint32_t tiles = 0;
+  for (int32_t e = lane_id(); e <= experts; e += WAVE) {
+    int64_t begin = inside(offsets[e], slots), end = slots;
+    if (e < experts) {
+      begin = offsets[e];
+      end = offsets[e + 1];
+      bound_slots(slots, begin, end);
+    }
+    tiles += (uint32_t)(end - begin + height - 1) / (uint32_t)height;
+  }
+  return wave_reduce_sum(tiles);
 }
 
 // As many tiles as find_tile can find: every group of slots has one that is not full.

@@ -7,9 +7,7 @@
 // dense direction (weights that have it as the other one are turned over on the way, in registers).  The columns are the
 // matrix instruction's first operand and are dealt to its rows so that a lane ends up with 16 neighbouring columns of one
 // row: bias, activation, residual, codes and rounding are done in registers and stored in whole chunks.
-#include "activations.hpp"
-#include "codes.hpp"
-#include "layers.hpp"
+#include "epilogue.hpp"
 
 namespace ginex {
 namespace {
@@ -21,53 +19,6 @@ constexpr int CHUNKS = 8;         // of a row in LDS: 128 bytes
 __device__ __forceinline__ int row_chunk(int r, int c) { return r * CHUNKS + (c ^ (r & 7)); }
 __device__ __forceinline__ int column_chunk(int n, int c) {
   return n * CHUNKS + (c ^ (((n ^ n >> 2) & 3) | (n >> 4 & 1) << 2));
-}
-
-// What a lane has of a row, 16 columns from c on: rounded and stored, with what belongs to it.
-template <typename T>
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t r, int32_t c, Width width, float (&v)[LANE_COLUMNS]) {
-  constexpr int N = Chunk<T>::N;
-  if (e.codes) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < LANE_COLUMNS; ++i) {
-      if (c + i >= width.width) v[i] = 0.f;
-      const uint32_t magnitude = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-      top = top > magnitude ? top : magnitude;
-    }
-    const uint32_t other = (uint32_t)__shfl_xor((int)top, 16, WAVE);      // the other half of the block
-    const uint32_t scale = scale_byte(top > other ? top : other);
-    const float by = to_codes(scale);
-    constexpr float whole = 12582912.f;       // 1.5 2^23: v by + whole is rounded to a whole number, halves to even
-    words2 word[2];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float q[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        q[i] = __builtin_amdgcn_fmed3f(fmaf(v[4 * k + i], by, whole), whole - 127.f, whole + 127.f);
-      word[k / 2][k % 2] = scale == NO_NUMBER ? 0 : low_bytes(q[0], q[1], q[2], q[3]);
-    }
-    if (c < e.blocks * GINEX_CODE_BLOCK) {
-      words2* const at = reinterpret_cast<words2*>(e.codes + r * ((int64_t)e.blocks * GINEX_CODE_BLOCK) + c);
-      at[0] = word[0];
-      at[1] = word[1];
-      if (c % GINEX_CODE_BLOCK == 0) e.scales[r * e.blocks + c / GINEX_CODE_BLOCK] = (uint8_t)scale;
-    }
-  }
-  T* const to = static_cast<T*>(e.y) + r * e.y_stride;
-  const T* const and_ = static_cast<const T*>(e.residual) + r * e.residual_stride;
-#pragma unroll
-  for (int k = 0; k < LANE_COLUMNS / N; ++k) {
-    const int32_t at = c + k * N;
-    if (at >= width.width) continue;
-    float res[N] = {};
-    if (e.residual) load_chunk(and_, at, width, res);
-    ChunkWords<T> u;
-#pragma unroll
-    for (int i = 0; i < N; ++i) u.wide[i] = (T)(activated_by<sizeof(T) == 4>(e.activation, v[k * N + i]) + res[i]);
-    store_words<true>(to, at, width, u);
-  }
 }
 
 // WM x WN waves of 16 MT rows and 64 columns.  TURNED: the weights have the width as their dense direction.
@@ -100,13 +51,10 @@ __global__ __launch_bounds__(THREADS, 2) void k_linear(RowsOf<const T> x, int64_
   const int wm = wave % WM, wn = wave / WM, group = lane / 16;
   const int32_t c0 = n0 + wn * WAVE_COLUMNS + group * LANE_COLUMNS;
   if (tile.expert == experts) {                 // slots without an expert
-    epilogue.activation = GINEX_ACT_NONE;
-    epilogue.residual = nullptr;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int64_t r = tile.first + (wm * MT + m) * 16 + lane % 16;
-      float v[LANE_COLUMNS] = {};
-      if (r < tile.end) finish<T>(epilogue, r, c0, out, v);
+      if (r < tile.end) clear_columns<T>(epilogue, r, c0, out);
     }
     return;
   }
@@ -209,24 +157,19 @@ __global__ __launch_bounds__(THREADS, 2) void k_linear(RowsOf<const T> x, int64_
     }
   }
 
-  float bias[LANE_COLUMNS] = {};
-  if (epilogue.bias) {
-    const T* const of = static_cast<const T*>(epilogue.bias) + (int64_t)tile.expert * out.width;
-#pragma unroll
-    for (int k = 0; k < LANE_COLUMNS / N; ++k) {
-      float v[N];
-      load_chunk(of, c0 + k * N, out, v);
-#pragma unroll
-      for (int i = 0; i < N; ++i) bias[k * N + i] = v[i];
-    }
-  }
+  float bias[LANE_COLUMNS];
+  load_bias<T>(epilogue, tile.expert, c0, out, bias);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int64_t r = tile.first + (wm * MT + m) * 16 + lane % 16;
     float v[LANE_COLUMNS];
 #pragma unroll
     for (int i = 0; i < LANE_COLUMNS; ++i) v[i] = sum[m][i / 4][i % 4] + bias[i];
-    if (r < tile.end) finish<T>(epilogue, r, c0, out, v);
+    if (r < tile.end) {
+      Columns<T> residual;
+      if (epilogue.residual) residual.load(static_cast<const T*>(epilogue.residual) + r * epilogue.residual_stride, c0, out);
+      finish<T>(epilogue, r, c0, n0 + (wn + 1) * WAVE_COLUMNS <= out.width, out, v, residual);
+    }
   }
 }
 
@@ -309,15 +252,17 @@ extern "C" int32_t ginex_linear(const ginex_rows_t* x, const ginex_weights_t* we
                              (int32_t)code_blocks(weights->out),
                              activation};
   if (slots <= FEW_ROWS) return linear_few(x, weights, route, by_slot != 0, slots, epilogue, st);
+  if (resident_fits(weights, slots, route != nullptr))
+    return linear_resident(x, weights, route, by_slot != 0, slots, epilogue, st);
   return with_type(x->type, [&](auto t) -> int32_t {
     using T = decltype(t);
     const int64_t groups = route ? route->experts : 1;
     const auto tiles = [&](int height) { return (slots / height + groups) * ceil_div(weights->out, 128); };
     if (weights->out <= WAVE_COLUMNS) {
-      if (tiles(128) >= 1024) return launch<T, 4, 4, 1>(x, weights, route, by_slot, slots, epilogue, st);
+      if (tiles(128) >= 1024) return launch<T, 2, 4, 1>(x, weights, route, by_slot, slots, epilogue, st);
       return launch<T, 1, 4, 1>(x, weights, route, by_slot, slots, epilogue, st);
     }
-    if (tiles(128) >= 512) return launch<T, 4, 2, 2>(x, weights, route, by_slot, slots, epilogue, st);
+    if (tiles(128) >= 512) return launch<T, 2, 2, 2>(x, weights, route, by_slot, slots, epilogue, st);
     return launch<T, 1, 2, 2>(x, weights, route, by_slot, slots, epilogue, st);
   });
 }

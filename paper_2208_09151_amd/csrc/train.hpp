@@ -45,11 +45,12 @@ union ChunkWords {
 // The chunk of the row that begins at `row` from column c on, a multiple of N, as it is; columns behind the width are 0.
 // The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
 // others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
-template <typename T>
+// WIDE: the row has a chunk at least.
+template <bool WIDE = false, typename T>
 __device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Width w) {
   constexpr int N = Chunk<T>::N;
   ChunkWords<T> u;
-  if (w.width < N) {
+  if (!WIDE && w.width < N) {
 #pragma unroll
     for (int i = 0; i < N; ++i) u.wide[i] = c + i < w.width ? row[c + i] : (T)0.f;
     return u;
