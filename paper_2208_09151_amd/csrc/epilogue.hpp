@@ -17,10 +17,18 @@ struct Columns {
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) chunk[k] = load_words<WIDE>(row, c + k * N, width);
   }
-  // of a row that has them all
-  __device__ __forceinline__ void load_whole(const T* at) {
+  // In two halves: the loads, of a row that has a chunk at least, ...
+  __device__ __forceinline__ void read(const T* row, int32_t c, Width width) {
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) chunk[k].wide = *reinterpret_cast<const typename Chunk<T>::At*>(at + k * N);
+    for (int k = 0; k < CHUNKS; ++k) {
+      const int32_t at = c + k * N;
+      chunk[k].wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (at < width.width - N ? at : width.width - N));
+    }
+  }
+  // ... and what becomes of them.
+  __device__ __forceinline__ void place(int32_t c, Width width) {
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) chunk[k] = placed<T>(chunk[k], c + k * N, width);
   }
   __device__ __forceinline__ float of(int i) const { return (float)chunk[i / N].wide[i % N]; }
 };
@@ -33,7 +41,7 @@ __device__ __forceinline__ void activate_columns(float (&v)[LANE_COLUMNS]) {
 
 // Codes of 16 columns from c on; the block's other half is 16 lanes away.
 template <typename T>
-__device__ __forceinline__ void keep_columns(const Epilogue& e, int64_t r, int32_t c, Width width,
+__device__ __forceinline__ void keep_columns(const Epilogue& e, int64_t r, bool mine, int32_t c, Width width,
                                              const float (&v)[LANE_COLUMNS]) {
   uint32_t top = 0;
 #pragma unroll
@@ -56,7 +64,7 @@ __device__ __forceinline__ void keep_columns(const Epilogue& e, int64_t r, int32
     }
     word[k / 2][k % 2] = scale == NO_NUMBER ? 0 : low_bytes(q[0], q[1], q[2], q[3]);
   }
-  if (c >= e.blocks * GINEX_CODE_BLOCK) return;
+  if (!mine || c >= e.blocks * GINEX_CODE_BLOCK) return;
   words2* const at = reinterpret_cast<words2*>(e.codes + r * ((int64_t)e.blocks * GINEX_CODE_BLOCK) + c);
   at[0] = word[0];
   at[1] = word[1];
@@ -79,16 +87,42 @@ __device__ __forceinline__ void store_columns(const Epilogue& e, int64_t r, int3
   }
 }
 
-// Sums and bias of 16 columns of row r, and the residual's if there is one, in `residual`.  All lanes that have row r call it.
+// The same without a branch where the row's chunks are whole, for rows that are `mine`.
 template <typename T>
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t r, int32_t c, bool whole, Width width, float (&v)[LANE_COLUMNS],
-                                       const Columns<T>& residual) {
-  if (e.codes) keep_columns<T>(e, r, c, width, v);
+__device__ __forceinline__ void store_columns_masked(const Epilogue& e, int64_t r, bool mine, int32_t c, Width width,
+                                                     const float (&v)[LANE_COLUMNS]) {
+  constexpr int N = Chunk<T>::N;
+  T* const to = static_cast<T*>(e.y) + r * e.y_stride + c;
+  ChunkWords<T> u[LANE_COLUMNS / N];
+#pragma unroll
+  for (int k = 0; k < LANE_COLUMNS / N; ++k)
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[k].wide[i] = (T)v[k * N + i];
+#pragma unroll
+  for (int k = 0; k < LANE_COLUMNS / N; ++k)
+    if (mine && c + (k + 1) * N <= width.width) *reinterpret_cast<typename Chunk<T>::At*>(to + k * N) = u[k].wide;
+  if (width.missing == 0) return;
+#pragma unroll
+  for (int k = 0; k < LANE_COLUMNS / N; ++k)
+    if (mine && c + k * N < width.width && c + (k + 1) * N > width.width) store_words<true>(to - c, c + k * N, width, u[k]);
+}
+
+// Sums and bias of 16 columns of row r: their codes, and what y gets but for the residual, in `v`.  All lanes call it; the row
+// is there if it is `mine`.
+template <typename T>
+__device__ __forceinline__ void finish_values(const Epilogue& e, int64_t r, bool mine, int32_t c, Width width,
+                                              float (&v)[LANE_COLUMNS]) {
+  if (e.codes) keep_columns<T>(e, r, mine, c, width, v);
   switch (e.activation) {           // (the same for all lanes)
     case GINEX_ACT_RELU: activate_columns<GINEX_ACT_RELU, T>(v); break;
     case GINEX_ACT_SILU: activate_columns<GINEX_ACT_SILU, T>(v); break;
     case GINEX_ACT_GELU: activate_columns<GINEX_ACT_GELU, T>(v); break;
   }
+}
+template <typename T>
+__device__ __forceinline__ void finish(const Epilogue& e, int64_t r, int32_t c, bool whole, Width width, float (&v)[LANE_COLUMNS],
+                                       const Columns<T>& residual) {
+  finish_values<T>(e, r, true, c, width, v);
   if (e.residual) {
 #pragma unroll
     for (int i = 0; i < LANE_COLUMNS; ++i) v[i] += residual.of(i);
@@ -100,7 +134,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t r, int32_t c, 
 template <typename T>
 __device__ __forceinline__ void clear_columns(const Epilogue& e, int64_t r, int32_t c, Width width) {
   const float zero[LANE_COLUMNS] = {};
-  if (e.codes) keep_columns<T>(e, r, c, width, zero);
+  if (e.codes) keep_columns<T>(e, r, true, c, width, zero);
   store_columns<T>(e, r, c, false, width, zero);
 }
 

@@ -22,7 +22,6 @@ __device__ __forceinline__ float4v product(const ChunkWords<float>& a, const Chu
   for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a.wide[i], b.wide[i], sum, 0, 0, 0);
   return sum;
 }
-
 template <typename T>
 struct WeightsOf {
   const T* data;

@@ -11,24 +11,87 @@
 namespace ginex {
 namespace {
 
-constexpr int WAVES = 8, THREADS = WAVES * WAVE, HEIGHT = 16 * WAVES;
+constexpr int WAVES = 8, THREADS = WAVES * WAVE;
 constexpr int MOST_LDS = 160 * 1024;
 
-// NB x 64 columns, a chunk of columns and of width at least; rows are fetched S steps (64 bytes of every row) at a time.
-template <typename T, int NB, int S>
+// Rows are taken in units of 128 bytes, of which lane l has the 32 bytes from 32 (l / 16) on.  16-bit numbers are two operands of the matrix instructions as they are.  f32 is a sum of three bf16, each the rounded rest of
+// those before it (8 bits of significand each, the rest exact), of whose products the six largest count: what is left out is
+// below 2^-26 of a product, an eighth of what f32's rounding of a sum may lose.  Six bf16 instructions take 96 cycles where the f32
+// ones take 256 (820 000 x 256 -> 256: THE-TERMS us instead of 954).  What is no number, or none in bf16, leaves a sum that is
+// none, and such a tile is computed again with the f32 instructions.
+template <typename T>
+struct Operand {
+  static constexpr int PARTS = 2;
+  typedef T Kind;
+};
+template <>
+struct Operand<float> {
+  static constexpr int PARTS = 3;
+  typedef bf16 Kind;
+};
+
+// A lane's 32 bytes, as operands.
+template <typename T>
+__device__ __forceinline__ void parts_of(const ChunkWords<T> (&from)[2], ChunkWords<T> (&to)[2]) {
+  to[0] = from[0];
+  to[1] = from[1];
+}
+__device__ __forceinline__ void parts_of(const ChunkWords<float> (&from)[2], ChunkWords<bf16> (&to)[3]) {
+  typedef float pair __attribute__((ext_vector_type(2)));
+  typedef bf16 half_pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    pair v = {from[i / 2].wide[i % 2 * 2], from[i / 2].wide[i % 2 * 2 + 1]};
+#pragma unroll
+    for (int z = 0; z < 3; ++z) {
+      const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half_pair));
+      to[z].words[i] = two;
+      v[0] -= __uint_as_float(two << 16);
+      v[1] -= __uint_as_float(two & 0xFFFF0000u);
+    }
+  }
+}
+
+// The products of a unit of weights with one of each of MT x 16 rows.
+template <typename T, int MT>
+__device__ __forceinline__ void products_of(const ChunkWords<T> (&w)[2], const ChunkWords<T> (&x)[MT][2], float4v* sum, int apart) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sum[m * apart] = product(w[k], x[m][k], sum[m * apart]);
+}
+template <typename T, int MT>
+__device__ __forceinline__ void products_of(const ChunkWords<T> (&w)[3], const ChunkWords<T> (&x)[MT][3], float4v* sum, int apart) {
+  // (the smallest first)
+  constexpr int of_w[6] = {2, 1, 0, 1, 0, 0}, of_x[6] = {0, 1, 2, 0, 1, 0};
+#pragma unroll
+  for (int k = 0; k < 6; ++k)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) sum[m * apart] = product(w[of_w[k]], x[m][of_x[k]], sum[m * apart]);
+}
+
+// NB x 64 columns, a chunk of columns and of width at least; rows are fetched S units ahead, MT x 16 of
+// them to a wave.  A wave waits for the oldest of its loads alone, so none of them, and no store, stands behind a branch
+// that depends on data or sizes: the compiler would have to wait for all.  RES: there is a residual.
+template <typename T, int MT, int NB, int S, bool RES>
 __global__ __launch_bounds__(THREADS, 2) void k_resident(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights, int32_t turned,
                                                          const int32_t* __restrict__ source,
                                                          const int64_t* __restrict__ offsets, int32_t experts, int64_t slots,
                                                          int32_t width, Width out, int32_t workers, int32_t blocks,
-                                                         Epilogue epilogue) {
-  constexpr int N = Chunk<T>::N, STEP = 4 * N, NT = 4 * NB;
+                                                         int32_t across, Epilogue epilogue) {
+  using O = Operand<T>;
+  using K = typename O::Kind;
+  constexpr int N = Chunk<T>::N, UNIT = 8 * N, NT = 4 * NB, PARTS = O::PARTS;
   extern __shared__ words4 lds[];
-  const int32_t steps = (width + STEP - 1) / STEP;
-  float* const lds_bias = reinterpret_cast<float*>(lds + steps * NT * WAVE);
+  const int32_t units = (width + UNIT - 1) / UNIT, all = NT * across, height = 16 * MT * WAVES / across;
+  float* const lds_bias = reinterpret_cast<float*>(lds + units * all * PARTS * WAVE);
   // Workgroups go to the 8 dies in turn; those with the same rows follow each other on one die.
   const int32_t turn = blockIdx.x / 8, worker = turn / blocks * 8 + blockIdx.x % 8;
-  const int32_t n0 = turn % blocks * NB * WAVE_COLUMNS;
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), group = lane / 16;
+  const int32_t block0 = turn % blocks * across * NB * WAVE_COLUMNS;
+  const int lane = lane_id(), group = lane / 16;
+  // a wave's place: its columns, and among the waves that have those
+  const int wave_of = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), wave = wave_of / across, part = wave_of % across;
+  const int32_t n0 = block0 + part * NB * WAVE_COLUMNS;
   const Width along = {width, (int32_t)((width + N - 1) / N * N - width)};
 
   // A number that the compiler does not know: what depends on it is not computed in front of a loop and kept in registers.
@@ -36,209 +99,306 @@ __global__ __launch_bounds__(THREADS, 2) void k_resident(RowsOf<const T> x, int6
     asm volatile("" : "+v"(v));
     return v;
   };
+  // Weights in the order in which the matrix instructions take them: operand row 4 g + i of product 4 b + j is column
+  // 64 b + 16 g + 4 j + i.
   const auto put_weights = [&](int32_t expert) {
     const T* const w = weights.of(expert);
     const int32_t thread = anew(threadIdx.x);
     if (turned) {
 #pragma unroll 4
-      for (int32_t q = thread; q < steps * NT * WAVE; q += THREADS) {
-        const int32_t l = q % WAVE, t = q / WAVE % NT, k = q / WAVE / NT;
-        // operand row 4 g + i of product 4 b + j is column 64 b + 16 g + 4 j + i
-        int32_t n = n0 + t / 4 * WAVE_COLUMNS + l % 16 / 4 * 16 + t % 4 * 4 + l % 4;
+      for (int32_t q = thread; q < units * all * WAVE; q += THREADS) {
+        const int32_t l = q % WAVE, t = q / WAVE % all, k = q / WAVE / all;
+        int32_t n = block0 + t / 4 * WAVE_COLUMNS + l % 16 / 4 * 16 + t % 4 * 4 + l % 4;
         n = n < out.width ? n : out.width - 1;
-        lds[q] = load_words<true>(w + n * weights.stride, k * STEP + l / 16 * N, along).words;
+        ChunkWords<T> v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = load_words<true>(w + n * weights.stride, k * UNIT + (l / 16 * 2 + h) * N, along);
+        ChunkWords<K> parts[PARTS];
+        parts_of(v, parts);
+#pragma unroll
+        for (int z = 0; z < PARTS; ++z) lds[((k * all + t) * PARTS + z) * WAVE + l] = parts[z].words;
       }
     } else {
 #pragma unroll 2
-      for (int32_t q = thread; q < steps * 4 * (NT * 4); q += THREADS) {
-        const int32_t four = q % (NT * 4), k = q / (NT * 4);         // columns 4 four .. + 3, chunk k of the width
-        const int32_t n = n0 + four * 4;
-        typename Four<T>::Wide raw[N];
+      for (int32_t q = thread; q < units * UNIT / 8 * (all * 4); q += THREADS) {
+        const int32_t four = q % (all * 4), eight = q / (all * 4);     // columns 4 four .. + 3, numbers 8 eight .. + 7 of the width
+        const int32_t n = block0 + four * 4;
+        typename Four<T>::Wide raw[8];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int32_t at = k * N + i;
-          raw[i] = four_of<true>(w + (int64_t)(at < width ? at : width - 1) * weights.stride, n < out.width ? n : out.width - 1,
-                           out.width);
+        for (int i = 0; i < 8; ++i) {
+          const int32_t at = eight * 8 + i;
+          raw[i] = four_of<true>(w + (int64_t)(at < width ? at : width - 1) * weights.stride,
+                                 n < out.width ? n : out.width - 1, out.width);
           if (at >= width) raw[i] = (typename Four<T>::Wide)(T)0.f;
         }
-        const int32_t t = four / 16 * 4 + four % 4, l = k % 4 * 16 + four % 16 / 4 * 4;
+        // f32: a lane's unit; 16 bits: half of it
+        constexpr int EIGHTS = UNIT / 8, HALVES = EIGHTS / 4;
+        const int32_t t = four / 16 * 4 + four % 4, k = eight / EIGHTS, l = eight % EIGHTS / HALVES * 16 + four % 16 / 4 * 4;
+        words4* const to = lds + (k * all + t) * PARTS * WAVE + l;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          ChunkWords<T> u;
+          ChunkWords<T> v[2];
 #pragma unroll
-          for (int i = 0; i < N; ++i) u.wide[i] = raw[i][j];
-          lds[(k / 4 * NT + t) * WAVE + l + j] = u.words;
+          for (int i = 0; i < 8; ++i) v[i / N].wide[i % N] = raw[i][j];
+          if constexpr (sizeof(T) == 4) {
+            ChunkWords<K> parts[PARTS];
+            parts_of(v, parts);
+#pragma unroll
+            for (int z = 0; z < PARTS; ++z) to[z * WAVE + j] = parts[z].words;
+          } else {
+            to[eight % HALVES * WAVE + j] = v[0].words;
+          }
         }
       }
     }
-    for (int32_t c = thread; c < NB * WAVE_COLUMNS; c += THREADS)
-      lds_bias[c] = epilogue.bias && n0 + c < out.width
-                        ? (float)static_cast<const T*>(epilogue.bias)[(int64_t)expert * out.width + n0 + c] : 0.f;
+    for (int32_t c = thread; c < across * NB * WAVE_COLUMNS; c += THREADS)
+      lds_bias[c] = epilogue.bias && block0 + c < out.width
+                        ? (float)static_cast<const T*>(epilogue.bias)[(int64_t)expert * out.width + block0 + c] : 0.f;
   };
 
-  // Rows first + i stride + 0 .. 127 for i < count, up to end.
-  const auto go = [&](int64_t first, int64_t stride, int32_t count, int64_t end) {
-    const auto row_of = [&](int32_t i) { return first + (i < count ? i : count - 1) * stride + wave * 16 + lane % 16; };
-    const auto source_of = [&](int32_t i) {
-      int64_t r = row_of(i);
-      r = r < end ? r : end - 1;
-      return source ? (int64_t)source[r] : r;
+  // 16 MT rows a wave, `apart` rows from wave to wave and `stride` from tile to tile, `count` tiles up to row `end`.
+  const auto go = [&](int32_t expert, int64_t first, int64_t apart, int64_t stride, int32_t count, int64_t end) {
+    const auto row_of = [&](int32_t i, int m) {
+      return first + (i < count ? i : count - 1) * stride + wave * apart + m * 16 + lane % 16;
     };
-    ChunkWords<T> next[S];
-    const auto fetch = [&](const T* row, int32_t k0) {
-      const T* const from = row + k0 * STEP + group * N;
+    int32_t from[MT];                 // where the rows of the tile that is fetched next come from
+    const T* row[MT];                 // and of the one that is fetched now
+    bool there[MT];
+    ChunkWords<T> next[S][MT][2];
+    const auto find = [&](int32_t i) {
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        if ((k0 + s + 1) * STEP <= width) next[s].wide = *reinterpret_cast<const typename Chunk<T>::At*>(from + s * STEP);
-        else if (k0 + s < steps) next[s] = load_words<true>(row, anew((k0 + s) * STEP + group * N), along);
+      for (int m = 0; m < MT; ++m) {
+        int64_t r = row_of(i, m);
+        r = r < end ? r : end - 1;
+        from[m] = source ? source[r] : (int32_t)r;
       }
     };
-    int64_t r0 = source_of(0), r1 = source_of(1);
-    bool there = r0 >= 0 && r0 < rows;
-    const T* row = x.at(there ? r0 : 0);
-    fetch(row, 0);
+    const auto take = [&]() {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        there[m] = (uint32_t)from[m] < (uint64_t)rows;
+        row[m] = x.at(there[m] ? from[m] : 0);
+      }
+    };
+    const auto fetch = [&](int32_t k, int s) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int32_t c = (k < units ? k : units - 1) * UNIT + (group * 2 + h) * N;
+          next[s][m][h].wide = *reinterpret_cast<const typename Chunk<T>::At*>(row[m] + (c < width - N ? c : width - N));
+        }
+    };
+    find(0);
+    take();
+    find(1);
+#pragma unroll
+    for (int s = 0; s < S; ++s) fetch(s, s);
+    __syncthreads();                  // (nobody reads the weights before any more)
+    put_weights(expert);
+    __syncthreads();
     for (int32_t i = 0; i < count; ++i) {
-      float4v sum[NT];
+      float4v sum[MT][NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-        sum[t] = *reinterpret_cast<const float4v*>(lds_bias + t / 4 * WAVE_COLUMNS + group * LANE_COLUMNS + t % 4 * 4);
-      const int64_t r = row_of(i);
-      const bool mine = r < end;
-      Columns<T> residual[NB];
+      for (int t = 0; t < NT; ++t) {
+        sum[0][t] = *reinterpret_cast<const float4v*>(lds_bias + (part * NB + t / 4) * WAVE_COLUMNS + group * LANE_COLUMNS + t % 4 * 4);
+#pragma unroll
+        for (int m = 1; m < MT; ++m) sum[m][t] = sum[0][t];
+      }
       const int32_t c0 = n0 + group * LANE_COLUMNS;
-      for (int32_t k0 = 0; k0 < steps; k0 += S) {
-        ChunkWords<T> now[S];
+      Columns<T> residual[MT][NB];
+      for (int32_t k0 = 0; k0 < units; k0 += S) {
+        // A unit's rows are fetched for the next segment, or the next tile, as soon as its products are under way.
+        const bool last = k0 + S >= units;
+        bool is[MT];
 #pragma unroll
-        for (int s = 0; s < S; ++s) now[s].words = there ? next[s].words : words4{0, 0, 0, 0};
-        if (k0 + S < steps) {
-          fetch(row, k0 + S);
-        } else {
-          there = r1 >= 0 && r1 < rows;
-          row = x.at(there ? r1 : 0);
-          fetch(row, 0);
-          r1 = source_of(i + 2);
-          if (epilogue.residual) {
-            const T* const and_ = static_cast<const T*>(epilogue.residual) + (mine ? r : end - 1) * epilogue.residual_stride;
+        for (int m = 0; m < MT; ++m) is[m] = there[m];
+        if (last) {
+          take();
+          find(i + 2);
+        }
+        if (RES && k0 == 0) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-              if (n0 + (b + 1) * WAVE_COLUMNS <= out.width) residual[b].load_whole(and_ + c0 + b * WAVE_COLUMNS);
-              else residual[b].template load<true>(and_, anew(c0 + b * WAVE_COLUMNS), out);
-            }
+          for (int m = 0; m < MT; ++m) {
+            const int64_t r = row_of(i, m);
+            const T* const and_ = static_cast<const T*>(epilogue.residual) + (r < end ? r : end - 1) * epilogue.residual_stride;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) residual[m][b].read(and_, c0 + b * WAVE_COLUMNS, out);
           }
         }
         // (the weights are read anew: they would be kept in registers through the loop, and spill)
         asm volatile("" ::: "memory");
-        const words4* const at = lds + k0 * NT * WAVE + lane;
-        const auto step = [&](int s) {
+        const words4* at = lds + (k0 * all + part * NT) * PARTS * WAVE + lane;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            ChunkWords<T> w;
-            w.words = at[(s * NT + t) * WAVE];
-            sum[t] = product(w, now[s], sum[t]);
+        for (int s = 0; s < S; ++s) {
+          if (k0 + s < units) {
+            ChunkWords<K> now[MT][PARTS];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              if (source) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) next[s][m][h].words = is[m] ? next[s][m][h].words : words4{0, 0, 0, 0};
+              }
+              if ((k0 + s + 1) * UNIT > width) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  next[s][m][h] = placed<T>(next[s][m][h], anew((k0 + s) * UNIT + (group * 2 + h) * N), along);
+              }
+              parts_of(next[s][m], now[m]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              ChunkWords<K> w[PARTS];
+#pragma unroll
+              for (int z = 0; z < PARTS; ++z) w[z].words = at[(t * PARTS + z) * WAVE];
+              products_of<K, MT>(w, now, &sum[0][t], NT);
+            }
           }
-        };
-        if (k0 + S <= steps) {
+          at += all * PARTS * WAVE;
+          fetch((last ? 0 : k0 + S) + s, s);
+        }
+      }
+      if constexpr (sizeof(T) == 4) {
+        // sums that are no numbers: again, with the f32 instructions and what is in memory
+        bool fine = true;
 #pragma unroll
-          for (int s = 0; s < S; ++s) step(s);
-        } else {
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int s = 0; s < S; ++s)
-            if (k0 + s < steps) step(s);
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) fine = fine && __builtin_isfinite(sum[m][t][j]);
+        if (__ballot(!fine)) {
+          const T* const w = weights.of(expert);
+#pragma unroll 1
+          for (int m = 0; m < MT; ++m) {
+            int64_t r = row_of(i, m);
+            r = r < end ? r : end - 1;
+            r = source ? (int64_t)source[r] : r;
+            const bool is = r >= 0 && r < rows;
+            const T* const of = x.at(is ? r : 0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              float4v again = *reinterpret_cast<const float4v*>(lds_bias + (part * NB + t / 4) * WAVE_COLUMNS + group * LANE_COLUMNS + t % 4 * 4);
+              int32_t n = anew(n0 + t / 4 * WAVE_COLUMNS + lane % 16 / 4 * 16 + t % 4 * 4 + lane % 4);
+              n = n < out.width ? n : out.width - 1;
+              for (int32_t k = 0; k < width; k += 4) {
+                const int32_t at = k + group;
+                const bool in = at < width;
+                const int64_t place = turned ? n * weights.stride + (in ? at : 0) : (in ? at : 0) * weights.stride + n;
+                again = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? w[place] : 0.f, in && is ? of[at] : 0.f, again, 0, 0, 0);
+              }
+#pragma unroll
+              for (int j = 0; j < MT; ++j)
+                if (j == m) sum[j][t] = again;
+            }
+          }
         }
       }
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        float v[LANE_COLUMNS];
+      for (int m = 0; m < MT; ++m) {
+        const int64_t r = row_of(i, m);
 #pragma unroll
-        for (int j = 0; j < LANE_COLUMNS; ++j) v[j] = sum[b * 4 + j / 4][j % 4];
-        if (mine) finish<T>(epilogue, r, anew(c0) + b * WAVE_COLUMNS, n0 + (b + 1) * WAVE_COLUMNS <= out.width, out, v, residual[b]);
+        for (int b = 0; b < NB; ++b) {
+          float v[LANE_COLUMNS];
+#pragma unroll
+          for (int j = 0; j < LANE_COLUMNS; ++j) v[j] = sum[m][b * 4 + j / 4][j % 4];
+          const int32_t c = anew(c0) + b * WAVE_COLUMNS;
+          finish_values<T>(epilogue, r, r < end, c, out, v);
+          if (RES) {
+            if (n0 + (b + 1) * WAVE_COLUMNS > out.width) residual[m][b].place(c, out);
+#pragma unroll
+            for (int j = 0; j < LANE_COLUMNS; ++j) v[j] += residual[m][b].of(j);
+          }
+          store_columns_masked<T>(epilogue, r, r < end, c, out, v);
+        }
       }
     }
   };
 
   // one layer: every so many tiles are this workgroup's; a layer per expert: a range of them
-  const uint32_t tiles = offsets ? count_tiles(offsets, experts, slots, HEIGHT) : (uint32_t)((slots + HEIGHT - 1) / HEIGHT);
+  const uint32_t tiles = offsets ? count_tiles(offsets, experts, slots, height) : (uint32_t)((slots + height - 1) / height);
   uint32_t t = offsets ? (uint32_t)((uint64_t)tiles * worker / workers) : worker;
   const uint32_t upto = offsets ? (uint32_t)((uint64_t)tiles * (worker + 1) / workers) : tiles;
   while (t < upto) {
-    TileRows tile = {0, (int64_t)t * HEIGHT, slots};
-    int64_t stride = (int64_t)workers * HEIGHT;
-    int32_t count = (int32_t)((tiles - t + workers - 1) / workers);
+    // (neighbouring waves' rows on different CUs: the last ones are shared by all)
+    TileRows tile = {0, (int64_t)worker * (16 * MT), slots};
+    int64_t apart = (int64_t)workers * (16 * MT), stride = (int64_t)workers * height;
+    int32_t count = (int32_t)((slots + stride - 1) / stride);
     if (offsets) {
-      if (!find_tile(offsets, experts, slots, t, HEIGHT, tile)) return;
-      const uint32_t left = (uint32_t)((tile.end - tile.first + HEIGHT - 1) / HEIGHT);
+      if (!find_tile(offsets, experts, slots, t, height, tile)) return;
+      const uint32_t left = (uint32_t)((tile.end - tile.first + height - 1) / height);
       count = (int32_t)(left < upto - t ? left : upto - t);
-      stride = HEIGHT;
+      apart = 16 * MT;
+      stride = height;
+      t += count;
     }
-    t = offsets ? t + count : upto;
     if (tile.expert == experts) {         // slots without an expert
-      for (int32_t i = 0; i < count; ++i) {
-        const int64_t r = tile.first + (int64_t)i * HEIGHT + wave * 16 + lane % 16;
-        if (r >= tile.end) continue;
+      for (int64_t r = tile.first + wave * 16 + lane % 16; r < tile.end && r < tile.first + (int64_t)count * height; r += 16 * WAVES / across) {
 #pragma unroll 1
         for (int b = 0; b < NB; ++b) clear_columns<T>(epilogue, r, anew(n0 + b * WAVE_COLUMNS + group * LANE_COLUMNS), out);
       }
-      continue;
+    } else {
+      go(tile.expert, tile.first, apart, stride, count, tile.end);
     }
-    __syncthreads();                      // (nobody reads the weights before any more)
-    put_weights(tile.expert);
-    __syncthreads();
-    go(tile.first, stride, count, tile.end);
+    if (!offsets) return;
   }
 }
 
 struct Fit {
-  int32_t nb, blocks, steps;
+  int32_t nb, across, blocks, units;
   int64_t lds;
 };
 Fit fit_of(int64_t width, int64_t out, int bytes) {
   Fit f;
-  const int64_t steps = ceil_div(width * bytes, 64), groups = ceil_div(out, WAVE_COLUMNS);
-  int64_t most = (MOST_LDS - 1024) / (steps * 4 * 1024);
-  const int64_t columns = bytes == 4 ? 2 : 4;         // sums and rows of more would not find room in the registers
-  most = most < columns ? most : columns;
-  f.steps = (int32_t)steps;
+  const int64_t parts = bytes == 4 ? Operand<float>::PARTS : Operand<bf16>::PARTS;
+  const int64_t units = ceil_div(width * bytes, 128), groups = ceil_div(out, WAVE_COLUMNS);
+  // columns of 64 of a workgroup: what LDS has room for, 4 at most; of a wave: what its registers have
+  int64_t most = (MOST_LDS - 1024) / (units * parts * 4 * 1024);
+  most = most < 4 ? most : 4;
+  f.units = (int32_t)units;
   f.blocks = most > 0 ? (int32_t)ceil_div(groups, most) : 1 << 30;
-  f.nb = (int32_t)ceil_div(groups, f.blocks);
-  f.lds = steps * f.nb * 4 * 1024 + f.nb * WAVE_COLUMNS * sizeof(float);
+  const int32_t columns = (int32_t)ceil_div(groups, f.blocks);
+  f.across = bytes == 4 ? (columns < 3 ? columns : 4) : 1;
+  f.nb = bytes == 4 ? 1 : (columns < 3 ? columns : 4);
+  f.lds = units * parts * f.across * f.nb * 4 * 1024 + f.across * f.nb * WAVE_COLUMNS * sizeof(float);
+  if (f.lds > MOST_LDS) f.blocks = 1 << 30;
   return f;
 }
 
 }  // namespace
 
 bool resident_fits(const ginex_weights_t* w, int64_t slots, bool routed) {
-  const Fit f = fit_of(w->width, w->out, element_bytes(w->type));
-  const int chunk = 16 / element_bytes(w->type);
-  return w->width >= chunk && w->out >= chunk && f.blocks <= 2 && slots >= 32 * HEIGHT;
+  const int bytes = element_bytes(w->type);
+  const Fit f = fit_of(w->width, w->out, bytes);
+  return w->width >= 16 / bytes && w->out >= 16 / bytes && f.blocks <= (bytes == 4 ? 4 : 2) && slots >= 4096;
 }
 
 int32_t linear_resident(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot,
                         int64_t slots, const Epilogue& epilogue, hipStream_t st) {
-  const Fit f = fit_of(w->width, w->out, element_bytes(x->type));
-  const int32_t workers = 256 * (f.lds <= MOST_LDS / 2 ? 2 : 1);
+  Fit f = fit_of(w->width, w->out, element_bytes(x->type));
+  // as many workgroups as are on the GPU at a time, those with the same rows together
+  int32_t workers = 256 * (f.lds <= MOST_LDS / 2 ? 2 : 1) / f.blocks;
+  workers = (workers + 7) / 8 * 8;
   return with_type(x->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const auto with_segment = [&](auto nb, auto s) -> int32_t {
-      constexpr int NB = decltype(nb)::value, S = decltype(s)::value;
-      hipLaunchKernelGGL((k_resident<T, NB, S>), dim3((unsigned)(workers * f.blocks)), dim3(THREADS), (unsigned)f.lds, st,
+    const auto with = [&](auto nb, auto s) -> int32_t {
+      constexpr int MT = sizeof(T) == 4 ? 2 : 1, NB = decltype(nb)::value, S = decltype(s)::value;
+      const auto kernel = epilogue.residual ? k_resident<T, MT, NB, S, true> : k_resident<T, MT, NB, S, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(workers * f.blocks)), dim3(THREADS), (unsigned)f.lds, st,
                          read_rows<T>(x), x->rows, weights_of<T>(w), w->turned, route && !by_slot ? route->source : nullptr,
                          route ? route->offsets : nullptr, w->experts, slots, (int32_t)w->width, Width::of<T>(w->out), workers,
-                         f.blocks, epilogue);
+                         f.blocks, f.across, epilogue);
       GINEX_LAUNCH_CHECK();
       return GINEX_OK;
     };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
     const auto with_columns = [&](auto nb) -> int32_t {
-      if (f.steps <= 2) return with_segment(nb, std::integral_constant<int, 2>{});
-      if (decltype(nb)::value == 4 || f.steps <= 4) return with_segment(nb, std::integral_constant<int, 4>{});
-      return with_segment(nb, std::integral_constant<int, decltype(nb)::value == 4 ? 4 : 8>{});
+      return f.units == 1 ? with(nb, one) : f.units <= 3 ? with(nb, two) : with(nb, four);
     };
-    if (f.nb == 1) return with_columns(std::integral_constant<int, 1>{});
-    if (f.nb == 2) return with_columns(std::integral_constant<int, 2>{});
-    if constexpr (sizeof(T) == 2) {
-      if (f.nb == 3) return with_columns(std::integral_constant<int, 3>{});
-      return with_columns(std::integral_constant<int, 4>{});
-    }
-    return fail(GINEX_ERR_ARG, "linear: %d columns of 64", f.nb);
+    if constexpr (sizeof(T) == 4) return with_columns(one);
+    else return f.nb == 1 ? with_columns(one) : f.nb == 2 ? with_columns(two) : with_columns(four);
   });
 }
 

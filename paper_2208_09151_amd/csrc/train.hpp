@@ -42,21 +42,11 @@ union ChunkWords {
   words4 words;
 };
 
-// The chunk of the row that begins at `row` from column c on, a multiple of N, as it is; columns behind the width are 0.
-// The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
-// others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
-// WIDE: the row has a chunk at least.
-template <bool WIDE = false, typename T>
-__device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Width w) {
-  constexpr int N = Chunk<T>::N;
-  ChunkWords<T> u;
-  if (!WIDE && w.width < N) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) u.wide[i] = c + i < w.width ? row[c + i] : (T)0.f;
-    return u;
-  }
-  const bool ends = c + N > w.width;
-  u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (ends ? w.width - N : c));
+// What was read for the chunk from column c on, from there or, if it would not end with the row, from the row's last chunk: moved
+// into its place, columns behind the width 0.
+template <typename T>
+__device__ __forceinline__ ChunkWords<T> placed(ChunkWords<T> u, int32_t c, Width w) {
+  const bool ends = c + Chunk<T>::N > w.width;
   if (w.missing) {
     words4 m = u.words;
     const int bytes = w.missing * (int)sizeof(T);
@@ -71,6 +61,23 @@ __device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Wid
 #pragma unroll
   for (int i = 0; i < 4; ++i) u.words[i] = c < w.width ? u.words[i] : 0;
   return u;
+}
+
+// The chunk of the row that begins at `row` from column c on, a multiple of N, as it is; columns behind the width are 0.
+// The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
+// others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
+// WIDE: the row has a chunk at least.
+template <bool WIDE = false, typename T>
+__device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Width w) {
+  constexpr int N = Chunk<T>::N;
+  ChunkWords<T> u;
+  if (!WIDE && w.width < N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) u.wide[i] = c + i < w.width ? row[c + i] : (T)0.f;
+    return u;
+  }
+  u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (c + N > w.width ? w.width - N : c));
+  return placed<T>(u, c, w);
 }
 
 // The same as f32.
