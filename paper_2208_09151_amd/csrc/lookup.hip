@@ -3,10 +3,10 @@
 //   out[i] = scale table[ids[i]],   dtable[v] = scale * sum over the i with ids[i] = v of dy[i]
 //
 // Both are bound by HBM.  The gradient adds nothing up by atomics, whose order would be another in every run: (id, position)
-// pairs are sorted by id, stable, and the sorted positions are cut into runs of RUN.  A group of lanes, one for every chunk of
-// 16 bytes of a row, goes through a run.  Ids that begin and end in it are written to the table's gradient; what is left of
-// those that began in front of the run or go on behind it are parts in the workspace, at most two a run.  A second launch adds
-// the parts of an id up in their order, and clears the rows that no id names.
+// pairs are sorted by id, stable, and the sorted positions are cut into runs.  A group of lanes, one for every chunk of 16
+// bytes of a row, goes through a run; what runs beside each other share is joined in LDS.  Ids that begin and end in a
+// workgroup's runs are written to the table's gradient; of others it leaves parts in the workspace, at most two.  A second launch adds the parts of an id up in their order, and
+// clears the rows that no id names.
 #include "layers.hpp"
 #include "primitives.hpp"
 
@@ -14,8 +14,7 @@ namespace ginex {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int RUN = 32;           // sorted positions of a group
-constexpr int LONG = 64;          // parts of an id that one group adds up; of more the workgroup does
+constexpr int LONG = 16;          // parts of an id that one group adds up; of more the workgroup does
 
 // ids as sorted by: what is no row of the table comes last.
 template <typename Id>
@@ -65,12 +64,21 @@ __global__ __launch_bounds__(THREADS) void k_lookup(RowsOf<const T> table, int64
 
 __device__ __forceinline__ uint32_t id_of(uint64_t word) { return (uint32_t)(word >> 32); }
 
-// A chunk of f32 sums in the workspace.
+// N f32 sums in the workspace, from column c on.
 template <int N>
-__device__ __forceinline__ void store_part(float* to, int32_t c, int32_t width, const float (&v)[N]) {
+__device__ __forceinline__ void store_part(float* to, int32_t c, Width width, const float (&v)[N]) {
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (c + n < width) to[c + n] = v[n];
+  for (int n = 0; n < N; n += 4) {
+    ChunkWords<float> u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.wide[i] = v[n + i];
+    if (c + n < width.width) store_words<true>(to, c + n, width, u);
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_part(const float* from, int32_t c, Width width, ChunkWords<float> (&v)[N / 4]) {
+#pragma unroll
+  for (int n = 0; n < N; n += 4) v[n / 4] = load_words(from, c + n, width);
 }
 
 template <typename T>
@@ -80,111 +88,161 @@ __device__ __forceinline__ void store_scaled(T* row, int32_t c, Width width, flo
   store_chunk(row, c, width, v);
 }
 
-// parts [runs x 2 x width]: of the id that began in front of the run, and of the one that goes on behind it.  named[v]: id v
-// is there.
-template <typename T>
+// A group goes through RUN sorted positions, a workgroup through as many runs beside each other as it has groups.  Ids that begin
+// and end in the workgroup's are written; of others it leaves parts [workgroups x 2 x width]: of the id that began in front, and
+// of the one that goes on.  named[v]: id v is there.
+template <typename T, int RUN>
 __global__ __launch_bounds__(THREADS) void k_lookup_sums(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
                                                          RowsOf<const T> dy, RowsOf<T> dtable, int32_t shift, Width width,
                                                          float scale, float* __restrict__ part, uint8_t* __restrict__ named) {
   constexpr int N = Chunk<T>::N, U = 8;
-  const int64_t run = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> shift;
-  const int64_t begin = run * RUN;
-  if (begin >= n) return;
+  __shared__ float heads[THREADS][N + 1];       // of every run, the sums of the id that began in front of it
+  __shared__ uint8_t head_ends[THREADS];        // and whether that ends in the run
+  const int32_t groups = THREADS >> shift, own = threadIdx.x >> shift, lane = threadIdx.x & ((1 << shift) - 1);
+  const int32_t c = ((int32_t)(blockIdx.y << shift) + lane) * N;
+  const int64_t begin = ((int64_t)blockIdx.x * groups + own) * RUN;
   const int64_t end = begin + RUN < n ? begin + RUN : n;
-  const int32_t lane = threadIdx.x & ((1 << shift) - 1), c = ((int32_t)(blockIdx.y << shift) + lane) * N;
-  const uint32_t in_front = begin > 0 ? id_of(sorted[begin - 1]) : 0xFFFFFFFFu;
+  const bool there = begin < n;
+  const uint32_t in_front = there && begin > 0 ? id_of(sorted[begin - 1]) : 0xFFFFFFFFu;
   const uint32_t behind = end < n ? id_of(sorted[end]) : 0xFFFFFFFFu;
-  float* const parts = part + run * 2 * width.width;
+  uint32_t id = there ? id_of(sorted[begin]) : 0xFFFFFFFFu;
+  const bool headed = id == in_front && id < rows;
+  bool began = !headed;                         // whether the id that is summed began in this run
   float sum[N] = {};
-  uint32_t id = id_of(sorted[begin]);
-  bool began = id != in_front;              // whether the id that is summed began in this run
-  if (id >= rows) return;
-  const auto flush = [&](bool ends) {
-    if (began && ends) {
-      if (c < width.width) store_scaled(dtable.at(id), c, width, scale, sum);
-    } else {
-      store_part(parts + (began ? width.width : 0), c, width.width, sum);
-    }
-    if (began && c == 0) named[id] = 1;
+  const auto put_head = [&](bool ends) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) heads[threadIdx.x][i] = sum[i];
+    if (lane == 0) head_ends[own] = ends;
   };
-  for (int64_t p = begin; p < end; p += U) {
-    uint64_t word[U];
-    float v[U][N];
+  const auto write = [&]() {
+    if (c < width.width) store_scaled(dtable.at(id), c, width, scale, sum);
+  };
+  if (there && id < rows) {                     // (ids without a row are the last)
+    for (int64_t p = begin; p < end; p += U) {
+      uint64_t word[U];
+      ChunkWords<T> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) word[u] = sorted[p + u < end ? p + u : end - 1];
+      for (int u = 0; u < U; ++u) word[u] = sorted[p + u < end ? p + u : end - 1];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_chunk(dy.at((uint32_t)word[u]), c, width, v[u]);
+      for (int u = 0; u < U; ++u) v[u] = load_words(dy.at((uint32_t)word[u]), c, width);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u >= end) break;
-      const uint32_t next = id_of(word[u]);
-      if (next != id) {
-        flush(true);
-        id = next;
-        began = true;
+      for (int u = 0; u < U; ++u) {
+        const uint32_t next = id_of(word[u]);
+        if (p + u < end && next != id && id < rows) {
+          if (began) {
+            write();
+            if (c == 0) named[id] = 1;
+          } else {
+            put_head(true);
+          }
+          id = next;
+          began = true;
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = 0.f;
-        if (id >= rows) return;             // ids without a row are the last
+          for (int i = 0; i < N; ++i) sum[i] = 0.f;
+        }
+        if (p + u < end) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum[i] += (float)v[u].wide[i];
+        }
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += v[u][i];
+      if (id >= rows) break;
     }
   }
-  flush(id != behind);
+  const bool goes_on = id < rows && id == behind;
+  if (id < rows && began) {
+    if (!goes_on) write();
+    if (c == 0) named[id] = 1;
+  }
+  if (id < rows && !began) put_head(!goes_on);
+  __syncthreads();
+  // The id that goes on behind this run, up to where it ends; the first run's head, too.
+  const Width of_parts = {width.width, (4 - width.width % 4) % 4};
+  const auto follow = [&](int32_t h) {
+    for (; h < groups; ++h) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += heads[(h << shift) + lane][i];
+      if (head_ends[h]) return true;
+    }
+    return false;
+  };
+  if (goes_on && began) {
+    if (follow(own + 1)) write();
+    else store_part<N>(part + (2 * (int64_t)blockIdx.x + 1) * width.width, c, of_parts, sum);
+  }
+  if (own == 0 && headed) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = heads[threadIdx.x][i];
+    if (!head_ends[0]) follow(1);
+    store_part<N>(part + 2 * (int64_t)blockIdx.x * width.width, c, of_parts, sum);
+  }
 }
 
-// The run in which the id of a part ends, at or behind run `from`.
-__device__ __forceinline__ int64_t last_run_of(const uint64_t* __restrict__ sorted, int64_t n, uint32_t id, int64_t from) {
-  int64_t lo = from * RUN, hi = n;          // sorted[lo] has the id, behind hi none does
+// The run in which an id ends that is at the end of run `from`.
+__device__ __forceinline__ int64_t last_run_of(const uint64_t* __restrict__ sorted, int64_t n, uint32_t id, int64_t from,
+                                               int32_t run_length) {
+  int64_t lo = (from + 1) * run_length - 1, hi = n;          // sorted[lo] has the id, from hi on none does
+  for (int64_t step = 4 * run_length; hi - lo > step; step *= 4) {
+    if (id_of(sorted[lo + step]) == id) {
+      lo += step;
+    } else {
+      hi = lo + step;
+      break;
+    }
+  }
   while (hi - lo > 1) {
     const int64_t mid = lo + (hi - lo) / 2;
     if (id_of(sorted[mid]) == id) lo = mid;
     else hi = mid;
   }
-  return lo / RUN;
+  return lo / run_length;
 }
 
 template <typename T>
-__global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
+__global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restrict__ sorted, int64_t n, int32_t run_length, uint32_t rows,
                                                          RowsOf<T> dtable, int32_t shift, Width width, float scale,
                                                          const float* __restrict__ part, const uint8_t* __restrict__ named) {
-  constexpr int N = Chunk<T>::N, U = 4;
+  constexpr int N = Chunk<T>::N, U = 8;
   __shared__ int64_t long_last[THREADS];
   __shared__ float sums[THREADS][N + 1];
   const int32_t groups = THREADS >> shift, lane = threadIdx.x & ((1 << shift) - 1), own = threadIdx.x >> shift;
   const int32_t c = ((int32_t)(blockIdx.y << shift) + lane) * N;
-  const int64_t runs = (n + RUN - 1) / RUN, run = (int64_t)blockIdx.x * groups + own;
+  const int64_t runs = (n + run_length - 1) / run_length, run = (int64_t)blockIdx.x * groups + own;
 
+  const Width of_parts = {width.width, (4 - width.width % 4) % 4};
   const auto add_parts = [&](float (&sum)[N], int64_t from, int64_t upto, int64_t step) {
     for (int64_t h = from; h <= upto; h += U * step) {
-      float v[U][N];
+      ChunkWords<float> v[U][N / 4];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t at = h + u * step <= upto ? h + u * step : h;
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[u][i] = c + i < width.width ? part[at * 2 * width.width + c + i] : 0.f;
-      }
+      for (int u = 0; u < U; ++u) load_part<N>(part + (h + u * step <= upto ? h + u * step : h) * 2 * width.width, c, of_parts, v[u]);
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] += h + u * step <= upto ? v[u][i] : 0.f;
+        for (int i = 0; i < N; ++i) sum[i] += h + u * step <= upto ? v[u][i / 4].wide[i % 4] : 0.f;
     }
+  };
+  const auto first_part = [&](float (&sum)[N], int64_t of) {
+    ChunkWords<float> v[N / 4];
+    load_part<N>(part + (of * 2 + 1) * width.width, c, of_parts, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = v[i / 4].wide[i % 4];
   };
 
   // an id that begins in this run and goes on behind it
   bool opens = false;
   uint32_t id = 0;
   int64_t last = -1;
-  if (run < runs && (run + 1) * RUN < n) {
-    id = id_of(sorted[(run + 1) * RUN]);
-    opens = id < rows && id_of(sorted[(run + 1) * RUN - 1]) == id && (run == 0 || id_of(sorted[run * RUN - 1]) != id);
-    if (opens) last = last_run_of(sorted, n, id, run + 1);
+  if (run < runs && (run + 1) * run_length < n) {
+    const int64_t next_end = (run + 2) * run_length;
+    id = id_of(sorted[(run + 1) * run_length]);
+    const uint32_t at_end = id_of(sorted[(run + 1) * run_length - 1]), further = id_of(sorted[next_end < n ? next_end : n - 1]);
+    const uint32_t in_front = id_of(sorted[run > 0 ? run * run_length - 1 : 0]);
+    opens = id < rows && at_end == id && (run == 0 || in_front != id);
+    if (opens) last = next_end < n && further == id ? last_run_of(sorted, n, id, run + 1, run_length) : run + 1;
   }
   const bool is_long = opens && last - run > LONG;
   if (opens && !is_long) {
     float sum[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] = c + i < width.width ? part[(run * 2 + 1) * width.width + c + i] : 0.f;
+    first_part(sum, run);
     add_parts(sum, run + 1, last, 1);
     if (c < width.width) store_scaled(dtable.at(id), c, width, scale, sum);
   }
@@ -200,12 +258,11 @@ __global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restr
     for (int i = 0; i < N; ++i) sums[threadIdx.x][i] = sum[i];
     __syncthreads();
     if (own == 0) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] = c + i < width.width ? part[(from * 2 + 1) * width.width + c + i] : 0.f;
+      first_part(sum, from);
       for (int32_t k = 0; k < groups; ++k)
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[i] += sums[(k << shift) + lane][i];
-      if (c < width.width) store_scaled(dtable.at(id_of(sorted[(from + 1) * RUN])), c, width, scale, sum);
+      if (c < width.width) store_scaled(dtable.at(id_of(sorted[(from + 1) * run_length])), c, width, scale, sum);
     }
     __syncthreads();
   }
@@ -217,6 +274,10 @@ __global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restr
     store_chunk(dtable.at(v), c, width, zero);
   }
 }
+
+// Sorted positions of a group: few where there are few groups.
+constexpr int SHORT_RUN = 8, LONG_RUN = 32;
+int64_t run_of(int64_t n) { return n < (1 << 17) ? SHORT_RUN : LONG_RUN; }
 
 struct LookupSpace {
   uint64_t *a, *b;
@@ -231,7 +292,7 @@ LookupSpace lookup_space(void* ws, int64_t n, int64_t rows, int64_t width) {
   s.a = arena.take<uint64_t>(n);
   s.b = arena.take<uint64_t>(n);
   s.hist = arena.take<uint32_t>(radix_plan(n).hist_elems);
-  s.part = arena.take<float>(ceil_div(n, RUN) * 2 * width);
+  s.part = arena.take<float>(ceil_div(n, 4 * run_of(n)) * 2 * width);         // (a workgroup has 4 runs at least)
   s.named = arena.take<uint8_t>(ceil_div(rows, 4) * 4);
   s.bytes = arena.used + 256;
   return s;
@@ -329,21 +390,24 @@ extern "C" int32_t ginex_lookup_backward(const ginex_rows_t* dy, const void* ids
   if (n > 0) GINEX_HIP(ids_64 ? sort_ids<int64_t>(ids, n, rows, s, st, &sorted) : sort_ids<int32_t>(ids, n, rows, s, st, &sorted));
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const int64_t cpr = ceil_div(dy->width, Chunk<T>::N), runs = ceil_div(n, RUN);
+    const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);
     int32_t shift = 0;
     while (shift < 6 && 1 << shift < cpr) ++shift;
     const unsigned across = (unsigned)ceil_div(cpr, 1 << shift);
     const Width width = Width::of<T>(dy->width);
+    const int32_t run_length = (int32_t)run_of(n) * (THREADS >> shift);
+    const int64_t runs = ceil_div(n, run_length);
     if (n > 0) {
-      hipLaunchKernelGGL(k_lookup_sums<T>, dim3((unsigned)ceil_div(runs, THREADS >> shift), across), dim3(THREADS), 0, st,
-                         sorted, n, (uint32_t)rows, read_rows<T>(dy), rows_of<T>(dtable), shift, width, scale, s.part, s.named);
+      const auto kernel = run_of(n) == SHORT_RUN ? k_lookup_sums<T, SHORT_RUN> : k_lookup_sums<T, LONG_RUN>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)runs, across), dim3(THREADS), 0, st, sorted, n, (uint32_t)rows, read_rows<T>(dy),
+                         rows_of<T>(dtable), shift, width, scale, s.part, s.named);
       GINEX_LAUNCH_CHECK();
     }
     // a group for every run, and enough of them for the rows that are cleared
-    int64_t groups = rows < 16384 ? rows : 16384;
+    int64_t groups = rows < 65536 ? rows : 65536;
     groups = groups > runs ? groups : runs;
-    hipLaunchKernelGGL(k_lookup_join<T>, dim3((unsigned)ceil_div(groups, THREADS >> shift), across), dim3(THREADS), 0, st, sorted,
-                       n, (uint32_t)rows, rows_of<T>(dtable), shift, width, scale, s.part, s.named);
+    hipLaunchKernelGGL(k_lookup_join<T>, dim3((unsigned)ceil_div(groups, THREADS >> shift), across), dim3(THREADS), 0, st, sorted, n,
+                       run_length, (uint32_t)rows, rows_of<T>(dtable), shift, width, scale, s.part, s.named);
     GINEX_LAUNCH_CHECK();
     return GINEX_OK;
   });
