@@ -302,7 +302,7 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
   }
 }
 
-// A group a workgroup: an expert's slots, those without one, or all rows.
+// 16 slots of one expert, or without one, or 16 rows a workgroup.
 template <typename T, bool TURNED, int WAVES>
 __global__ __launch_bounds__(WAVES* WAVE) void k_few_linear(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights,
                                                                    const int32_t* __restrict__ source,
@@ -310,19 +310,12 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_linear(RowsOf<const T> x, i
                                                                    int64_t slots, int32_t width, Width out, Epilogue e) {
   __shared__ float room[WAVES][16][PITCH];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
-  const int32_t expert = blockIdx.y;
-  int64_t begin = 0, end = slots;
+  TileRows tile = {0, (int64_t)blockIdx.y * 16, slots};
   if (offsets) {
-    if (expert < experts) {
-      begin = offsets[expert];
-      end = offsets[expert + 1];
-      bound_slots(slots, begin, end);
-    } else {
-      begin = inside(offsets[experts], slots);
-    }
+    if (!find_tile(offsets, experts, slots, blockIdx.y, 16, tile)) return;
   }
-  begin += (int64_t)blockIdx.z * 16;        // 16 rows a workgroup
-  if (begin >= end) return;
+  const int32_t expert = tile.expert;
+  const int64_t begin = tile.first, end = tile.end;
   const int32_t count = (int32_t)(end - begin < 16 ? end - begin : 16), n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
   const bool none = expert == experts;        // slots without an expert are cleared
   float4v sum[4] = {};
@@ -403,16 +396,20 @@ int32_t with_waves(int64_t width, int32_t bytes, int64_t groups, Go go) {
 
 }  // namespace
 
+int64_t few_groups(const ginex_weights_t* w, const ginex_routing_t* route, int64_t slots) {
+  const int64_t tiles = route ? most_tiles(slots, route->experts, 16) : ceil_div(slots, 16);
+  return ceil_div(w->out, WAVE_COLUMNS) * tiles;
+}
+
 int32_t linear_few(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot, int64_t slots,
                    const Epilogue& epilogue, hipStream_t st) {
   return with_type(x->type, [&](auto t) -> int32_t {
     using T = decltype(t);
-    const int64_t groups = ceil_div(w->out, WAVE_COLUMNS) * (route && slots > w->experts ? w->experts : route ? slots : 1);
+    const int64_t groups = few_groups(w, route, slots), tiles = groups / ceil_div(w->out, WAVE_COLUMNS);
     return with_waves(w->width, sizeof(T), groups, [&](auto waves) -> int32_t {
       constexpr int WAVES = decltype(waves)::value;
       const auto kernel = w->turned ? k_few_linear<T, true, WAVES> : k_few_linear<T, false, WAVES>;
-      const dim3 grid((unsigned)ceil_div(w->out, WAVE_COLUMNS), route ? (unsigned)route->experts + 1 : 1,
-                      (unsigned)ceil_div(slots, 16));
+      const dim3 grid((unsigned)ceil_div(w->out, WAVE_COLUMNS), (unsigned)tiles);
       hipLaunchKernelGGL(kernel, grid, dim3(WAVES * WAVE), 0, st, read_rows<T>(x), x->rows, weights_of<T>(w),
                          route && !by_slot ? route->source : nullptr, route ? route->offsets : nullptr, w->experts, slots,
                          (int32_t)w->width, Width::of<T>(w->out), epilogue);

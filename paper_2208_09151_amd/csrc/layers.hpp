@@ -39,17 +39,15 @@ struct Four {
   typedef Wide At __attribute__((aligned(sizeof(T))));
 };
 
-// Four neighbouring columns of a row of weights, from column n on; what is behind the last one is 0.
-template <bool WIDE = false, typename T>
-__device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t n, int32_t columns) {
-  typename Four<T>::Wide v;
-  if (!WIDE && columns < 4) {
-#pragma unroll
-    for (int l = 0; l < 4; ++l) v[l] = n + l < columns ? row[n + l] : (T)0.f;
-    return v;
-  }
-  const int32_t over = n + 4 - columns;       // the last ones are read so that they end with the row, and moved
-  v = *reinterpret_cast<const typename Four<T>::At*>(row + (over > 0 ? columns - 4 : n));
+// Four neighbouring columns of a row of weights, from column n on; what is behind the last one is 0.  The last ones are read so
+// that they end with the row, and moved.
+template <typename T>
+__device__ __forceinline__ typename Four<T>::Wide four_read(const T* row, int32_t n, int32_t columns) {
+  return *reinterpret_cast<const typename Four<T>::At*>(row + (n + 4 > columns ? columns - 4 : n));
+}
+template <typename T>
+__device__ __forceinline__ typename Four<T>::Wide four_placed(typename Four<T>::Wide v, int32_t n, int32_t columns) {
+  const int32_t over = n + 4 - columns;
   if (over > 0) {
 #pragma unroll
     for (int l = 0; l < 4; ++l) {
@@ -60,6 +58,16 @@ __device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t 
     }
   }
   return v;
+}
+template <bool WIDE = false, typename T>
+__device__ __forceinline__ typename Four<T>::Wide four_of(const T* row, int32_t n, int32_t columns) {
+  if (!WIDE && columns < 4) {
+    typename Four<T>::Wide v;
+#pragma unroll
+    for (int l = 0; l < 4; ++l) v[l] = n + l < columns ? row[n + l] : (T)0.f;
+    return v;
+  }
+  return four_placed<T>(four_read(row, n, columns), n, columns);
 }
 
 // What happens to the sums of a linear layer.
@@ -75,13 +83,13 @@ struct Epilogue {
   int32_t activation;
 };
 
-// A linear layer of up to FEW_ROWS rows or slots.
-constexpr int64_t FEW_ROWS = GINEX_MAX_FEW_ROWS;
+// A linear layer of few rows, 16 of them and 64 columns to a workgroup.
+int64_t few_groups(const ginex_weights_t* weights, const ginex_routing_t* route, int64_t slots);
 int32_t linear_few(const ginex_rows_t* x, const ginex_weights_t* weights, const ginex_routing_t* route, bool by_slot,
                    int64_t slots, const Epilogue& epilogue, hipStream_t st);
 
 // A linear layer of many rows whose weights find room in LDS; false: not for these sizes.
-bool resident_fits(const ginex_weights_t* weights, int64_t slots, bool routed);
+bool resident_fits(const ginex_weights_t* weights, int64_t slots);
 int32_t linear_resident(const ginex_rows_t* x, const ginex_weights_t* weights, const ginex_routing_t* route, bool by_slot,
                         int64_t slots, const Epilogue& epilogue, hipStream_t st);
 

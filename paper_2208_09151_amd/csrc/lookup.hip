@@ -95,7 +95,7 @@ template <typename T, int RUN>
 __global__ __launch_bounds__(THREADS) void k_lookup_sums(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
                                                          RowsOf<const T> dy, RowsOf<T> dtable, int32_t shift, Width width,
                                                          float scale, float* __restrict__ part, uint8_t* __restrict__ named) {
-  constexpr int N = Chunk<T>::N, U = 8;
+  constexpr int N = Chunk<T>::N, U = 4;
   __shared__ float heads[THREADS][N + 1];       // of every run, the sums of the id that began in front of it
   __shared__ uint8_t head_ends[THREADS];        // and whether that ends in the run
   const int32_t groups = THREADS >> shift, own = threadIdx.x >> shift, lane = threadIdx.x & ((1 << shift) - 1);
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(THREADS) void k_lookup_join(const uint64_t* __restr
 }
 
 // Sorted positions of a group: few where there are few groups.
-constexpr int SHORT_RUN = 8, LONG_RUN = 32;
+constexpr int SHORT_RUN = 8, LONG_RUN = 16;
 int64_t run_of(int64_t n) { return n < (1 << 17) ? SHORT_RUN : LONG_RUN; }
 
 struct LookupSpace {

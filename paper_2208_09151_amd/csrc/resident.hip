@@ -7,68 +7,13 @@
 // per expert: the tiles of all experts are numbered, a workgroup has a range of them, and changes its weights where the expert
 // changes.
 #include "epilogue.hpp"
+#include "parts.hpp"
 
 namespace ginex {
 namespace {
 
 constexpr int WAVES = 8, THREADS = WAVES * WAVE;
 constexpr int MOST_LDS = 160 * 1024;
-
-// Rows are taken in units of 128 bytes, of which lane l has the 32 bytes from 32 (l / 16) on.  16-bit numbers are two operands of the matrix instructions as they are.  f32 is a sum of three bf16, each the rounded rest of
-// those before it (8 bits of significand each, the rest exact), of whose products the six largest count: what is left out is
-// below 2^-26 of a product, an eighth of what f32's rounding of a sum may lose.  Six bf16 instructions take 96 cycles where the f32
-// ones take 256 (820 000 x 256 -> 256: THE-TERMS us instead of 954).  What is no number, or none in bf16, leaves a sum that is
-// none, and such a tile is computed again with the f32 instructions.
-template <typename T>
-struct Operand {
-  static constexpr int PARTS = 2;
-  typedef T Kind;
-};
-template <>
-struct Operand<float> {
-  static constexpr int PARTS = 3;
-  typedef bf16 Kind;
-};
-
-// A lane's 32 bytes, as operands.
-template <typename T>
-__device__ __forceinline__ void parts_of(const ChunkWords<T> (&from)[2], ChunkWords<T> (&to)[2]) {
-  to[0] = from[0];
-  to[1] = from[1];
-}
-__device__ __forceinline__ void parts_of(const ChunkWords<float> (&from)[2], ChunkWords<bf16> (&to)[3]) {
-  typedef float pair __attribute__((ext_vector_type(2)));
-  typedef bf16 half_pair __attribute__((ext_vector_type(2)));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    pair v = {from[i / 2].wide[i % 2 * 2], from[i / 2].wide[i % 2 * 2 + 1]};
-#pragma unroll
-    for (int z = 0; z < 3; ++z) {
-      const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half_pair));
-      to[z].words[i] = two;
-      v[0] -= __uint_as_float(two << 16);
-      v[1] -= __uint_as_float(two & 0xFFFF0000u);
-    }
-  }
-}
-
-// The products of a unit of weights with one of each of MT x 16 rows.
-template <typename T, int MT>
-__device__ __forceinline__ void products_of(const ChunkWords<T> (&w)[2], const ChunkWords<T> (&x)[MT][2], float4v* sum, int apart) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-#pragma unroll
-    for (int m = 0; m < MT; ++m) sum[m * apart] = product(w[k], x[m][k], sum[m * apart]);
-}
-template <typename T, int MT>
-__device__ __forceinline__ void products_of(const ChunkWords<T> (&w)[3], const ChunkWords<T> (&x)[MT][3], float4v* sum, int apart) {
-  // (the smallest first)
-  constexpr int of_w[6] = {2, 1, 0, 1, 0, 0}, of_x[6] = {0, 1, 2, 0, 1, 0};
-#pragma unroll
-  for (int k = 0; k < 6; ++k)
-#pragma unroll
-    for (int m = 0; m < MT; ++m) sum[m * apart] = product(w[of_w[k]], x[m][of_x[k]], sum[m * apart]);
-}
 
 // NB x 64 columns, a chunk of columns and of width at least; rows are fetched S units ahead, MT x 16 of
 // them to a wave.  A wave waits for the oldest of its loads alone, so none of them, and no store, stands behind a branch
@@ -259,15 +204,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_resident(RowsOf<const T> x, int6
         }
       }
       if constexpr (sizeof(T) == 4) {
-        // sums that are no numbers: again, with the f32 instructions and what is in memory
-        bool fine = true;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) fine = fine && __builtin_isfinite(sum[m][t][j]);
-        if (__ballot(!fine)) {
+        if (any_none<MT * NT>(&sum[0][0])) {
           const T* const w = weights.of(expert);
 #pragma unroll 1
           for (int m = 0; m < MT; ++m) {
@@ -275,21 +212,17 @@ __global__ __launch_bounds__(THREADS, 2) void k_resident(RowsOf<const T> x, int6
             r = r < end ? r : end - 1;
             r = source ? (int64_t)source[r] : r;
             const bool is = r >= 0 && r < rows;
-            const T* const of = x.at(is ? r : 0);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-              float4v again = *reinterpret_cast<const float4v*>(lds_bias + (part * NB + t / 4) * WAVE_COLUMNS + group * LANE_COLUMNS + t % 4 * 4);
               int32_t n = anew(n0 + t / 4 * WAVE_COLUMNS + lane % 16 / 4 * 16 + t % 4 * 4 + lane % 4);
               n = n < out.width ? n : out.width - 1;
-              for (int32_t k = 0; k < width; k += 4) {
-                const int32_t at = k + group;
-                const bool in = at < width;
-                const int64_t place = turned ? n * weights.stride + (in ? at : 0) : (in ? at : 0) * weights.stride + n;
-                again = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? w[place] : 0.f, in && is ? of[at] : 0.f, again, 0, 0, 0);
-              }
+              const float4v start =
+                  *reinterpret_cast<const float4v*>(lds_bias + (part * NB + t / 4) * WAVE_COLUMNS + group * LANE_COLUMNS + t % 4 * 4);
+              const float4v again = sums_again(x.at(is ? r : 0), is, w + (turned ? n * weights.stride : n),
+                                               turned ? 1 : weights.stride, width, start);
 #pragma unroll
               for (int j = 0; j < MT; ++j)
-                if (j == m) sum[j][t] = again;
+                if (j == m) sum[j][t] = with_again(sum[j][t], again);
             }
           }
         }
@@ -367,10 +300,14 @@ Fit fit_of(int64_t width, int64_t out, int bytes) {
 
 }  // namespace
 
-bool resident_fits(const ginex_weights_t* w, int64_t slots, bool routed) {
+// Where the rows are many enough to pay for the weights' way into LDS (us of a call, this and tiles: bf16, 256 x 256, 60 000 rows
+// 25.5 and 21.1, 100 000 42.5 and 39.6, 177 000 56.5 and 61.6, 820 000 200 and 268; 8 experts, 152 000 slots, 256 x 128 41 and 34; 32
+// experts, 600 000 slots, 128 x 128 81 and 94; f16, 300 000 x 100, 47 out 30 and 39; f32, 128 x 128, 60 000 rows 28.6 and 25.0, 152 000
+// slots of 8 experts, 256 x 128 88 and 100; 820 000, 256 x 256 710 and 739).
+bool resident_fits(const ginex_weights_t* w, int64_t slots) {
   const int bytes = element_bytes(w->type);
   const Fit f = fit_of(w->width, w->out, bytes);
-  return w->width >= 16 / bytes && w->out >= 16 / bytes && f.blocks <= (bytes == 4 ? 4 : 2) && slots >= 4096;
+  return w->width >= 16 / bytes && w->out >= 16 / bytes && f.blocks <= (bytes == 4 ? 4 : 2) && slots >= (bytes == 4 ? 1 << 17 : 160000);
 }
 
 int32_t linear_resident(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot,

@@ -63,6 +63,14 @@ __device__ __forceinline__ ChunkWords<T> placed(ChunkWords<T> u, int32_t c, Widt
   return u;
 }
 
+// The load alone, of a row that has a chunk at least: for `placed` once it is there.
+template <typename T>
+__device__ __forceinline__ ChunkWords<T> read_words(const T* row, int32_t c, Width w) {
+  ChunkWords<T> u;
+  u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (c + Chunk<T>::N > w.width ? w.width - Chunk<T>::N : c));
+  return u;
+}
+
 // The chunk of the row that begins at `row` from column c on, a multiple of N, as it is; columns behind the width are 0.
 // The last chunk of a row that N does not divide is read so that it ends with the row, in the same instruction as all
 // others, and moved into its place: element by element it was a second trip to memory for nearly every wave.
@@ -76,8 +84,7 @@ __device__ __forceinline__ ChunkWords<T> load_words(const T* row, int32_t c, Wid
     for (int i = 0; i < N; ++i) u.wide[i] = c + i < w.width ? row[c + i] : (T)0.f;
     return u;
   }
-  u.wide = *reinterpret_cast<const typename Chunk<T>::At*>(row + (c + N > w.width ? w.width - N : c));
-  return placed<T>(u, c, w);
+  return placed<T>(read_words(row, c, w), c, w);
 }
 
 // The same as f32.
