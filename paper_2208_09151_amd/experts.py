@@ -1,7 +1,7 @@
 """A layer of experts on gathered rows, and a small training run over it: sampling, changesets, the feature
 cache and the gather in front, the training operators behind.
 
-  python -m paper_2208_09151_amd.experts [--config 1] [--steps 40]
+  python -m paper_2208_09151_amd.experts [--config 1] [--steps 40] [--blocks 0]
 
 ``ExpertLayer`` sends every row to the experts its router likes best, one linear layer and an activation
 each, and adds their answers up by the router's weights.  What the backward pass needs of the rows and of
@@ -9,7 +9,10 @@ the activations' inputs is kept in 8 bits (8.25 with the scales, instead of 32):
 expert, as the weight gradient looks them up by the route.  The experts' answers are kept as they are, for the
 gradient of the router's weights.  The products of forward pass and input gradient are torch's, an expert at a
 time, and need the experts' sizes on the host: the layer waits for the GPU once and cannot be captured into a
-graph.
+graph.  ``ExpertLayer.answer`` is its form for a few rows, without gradients and without a wait.
+
+``Block`` is a residual block with a layer of experts inside whose products are ``linear``'s, which looks rows up by the route
+and waits for nothing.
 """
 from __future__ import annotations
 
@@ -20,6 +23,7 @@ import sys
 
 import torch
 
+from .layers import expert_layer, layer_norm, linear, lookup
 from .training import (Activation, Combine, Compressed, Route, _first_derivative, activate, combine,  # noqa: F401
                        compress, dispatch, dispatch_backward, route, weight_gradient)
 
@@ -85,25 +89,66 @@ class ExpertLayer(torch.nn.Module):
         return combine(y, r, weights)
 
 
-class Classifier(torch.nn.Module):
-    """An expert layer on all sampled rows, the mean over a seed's first-hop neighbours, and a linear head."""
+    @torch.no_grad()
+    def answer(self, x):
+        """The layer for up to 64 rows, in two launches; no expert is ever full."""
+        return expert_layer(x, self.router.weight, self.weight, self.top, self.activation)
 
-    def __init__(self, width, hidden, classes, experts):
+
+class Block(torch.nn.Module):
+    """x + down(experts(norm(x))): layer norm, ``top`` of ``experts`` linear layers with a bias and an activation, their sum by
+    the router's weights, and a linear layer back to ``width`` with x as its residual."""
+
+    def __init__(self, width, hidden, experts, top=2, activation="gelu"):
+        super().__init__()
+        self.experts, self.top, self.activation = experts, top, activation
+        self.norm_weight = torch.nn.Parameter(torch.ones(width))
+        self.norm_bias = torch.nn.Parameter(torch.zeros(width))
+        self.router = torch.nn.Linear(width, experts, bias=False)
+        self.up = torch.nn.Parameter(torch.randn(experts, width, hidden) / math.sqrt(width))
+        self.up_bias = torch.nn.Parameter(torch.zeros(experts, hidden))
+        self.down = torch.nn.Linear(hidden, width)
+
+    def forward(self, x):
+        n = layer_norm(x, self.norm_weight, self.norm_bias)
+        best, chosen = torch.topk(self.router(n).float(), self.top, dim=1)
+        r = route(chosen, self.experts)
+        h = linear(n, self.up, self.up_bias, self.activation, route=r)
+        h = combine(h, r, torch.softmax(best, dim=1))
+        return linear(h, self.down.weight.t(), self.down.bias, residual=x)
+
+    @torch.no_grad()
+    def answer(self, x):
+        """The block for up to 64 rows."""
+        n = layer_norm(x, self.norm_weight, self.norm_bias)
+        h = expert_layer(n, self.router.weight, self.up, self.top, self.activation, self.up_bias)
+        return linear(h, self.down.weight.t(), self.down.bias, residual=x)
+
+
+class Classifier(torch.nn.Module):
+    """An expert layer on all sampled rows, ``blocks`` residual blocks, the mean over a seed's first-hop neighbours, and a linear
+    head."""
+
+    def __init__(self, width, hidden, classes, experts, blocks=0):
         super().__init__()
         self.layer = ExpertLayer(width, hidden, experts, capacity=2.0)
         self.head = torch.nn.Linear(2 * hidden, classes)
+        self.blocks = torch.nn.ModuleList(Block(hidden, 2 * hidden, experts) for _ in range(blocks))
 
     def forward(self, x, rowptr, col):
         h = self.layer(x)
+        for block in self.blocks:
+            h = block(h)
         seeds = rowptr.numel() - 1
         count = (rowptr[1:] - rowptr[:-1])
         of = torch.repeat_interleave(torch.arange(seeds, device=x.device), count)
         around = torch.zeros((seeds, h.shape[1]), dtype=h.dtype, device=x.device)
-        around = around.index_add(0, of, h[col.long()]) / count.clamp(min=1)[:, None]
+        rows = lookup(h, col) if len(self.blocks) else h[col.long()]        # (lookup's gradient adds up in one order)
+        around = around.index_add(0, of, rows) / count.clamp(min=1)[:, None]
         return self.head(torch.cat([h[:seeds], around], 1))
 
 
-def train(config=1, steps=40, hidden=64, experts=8, classes=8, rate=0.02, report=print):
+def train(config=1, steps=40, hidden=64, experts=8, classes=8, rate=0.02, report=print, blocks=0):
     """Trains the classifier on the batches of a synthetic workload, one superbatch after the other; the
     label of a node is its largest feature of the first ``classes``.  Returns the losses."""
     import paper_2208_09151_amd as ginex
@@ -118,7 +163,7 @@ def train(config=1, steps=40, hidden=64, experts=8, classes=8, rate=0.02, report
     nodes = train_nodes(cfg.num_nodes, cfg.train_frac, cfg.seed, "cuda")
     with torch.random.fork_rng(devices=[]):
         torch.random.default_generator.manual_seed(0)       # (torch.manual_seed would seed the GPU's, too)
-        model = Classifier(cfg.feat_dim, hidden, classes, experts).cuda()
+        model = Classifier(cfg.feat_dim, hidden, classes, experts, blocks).cuda()
     adam = torch.optim.Adam(model.parameters(), lr=rate)
     losses = []
     while len(losses) < steps:
@@ -151,8 +196,9 @@ def main():
     ap.add_argument("--steps", type=int, default=40)
     ap.add_argument("--hidden", type=int, default=64)
     ap.add_argument("--experts", type=int, default=8)
+    ap.add_argument("--blocks", type=int, default=0)
     args = ap.parse_args()
-    losses = train(args.config, args.steps, args.hidden, args.experts)
+    losses = train(args.config, args.steps, args.hidden, args.experts, blocks=args.blocks)
     print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f} in {len(losses)} steps")
 
 

@@ -61,15 +61,18 @@ class Linear(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, residual, activation, route, slots, made):
-        y, kept = linear(x, weight, bias, activation, residual, route, slots, keep=True) if activation is not None or made is not None \
-            else (linear(x, weight, bias, None, residual, route, slots), None)
+        kept = None
+        if activation is not None or made is not None:
+            y, kept = linear(x, weight, bias, activation, residual, route, slots, keep=True)
+        else:
+            y = linear(x, weight, bias, None, residual, route, slots)
         if made is not None:
             made.append(kept)
         rows = compress(x) if ctx.needs_input_grad[1] else None
         saved = [weight]
-        for k in (rows, kept if activation is not None else None):
+        for k in (rows, None if activation is None else kept):
             saved += [None, None] if k is None else [k.codes, k.scales]
-        ctx.save_for_backward(*saved, *(route._tensors() if route is not None else ()))
+        ctx.save_for_backward(*saved, *(() if route is None else route._tensors()))
         ctx.widths, ctx.activation, ctx.slots = (x.shape[1], y.shape[1]), activation, slots
         ctx.bias_type = None if bias is None else bias.dtype
         return y
