@@ -137,3 +137,18 @@ def load():
             fn.argtypes = args
         _lib = lib
     return _lib
+
+
+def quick():
+    """The compiled calls of csrc/quick.cpp, or None where they are not built, or older than their sources."""
+    path = os.path.join(_PKG, "_quick.so")
+    root = os.path.dirname(_PKG)
+    sources = [os.path.join(_PKG, "csrc", "quick.cpp")] + [os.path.join(root, "include", f)
+                                                            for f in ("ginex.h", "ginex_train.h", "ginex_layers.h")]
+    if not os.path.exists(path) or any(os.path.getmtime(s) > os.path.getmtime(path) for s in sources if os.path.exists(s)):
+        return None
+    try:
+        from . import _quick
+    except ImportError:
+        return None
+    return _quick

@@ -15,6 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libginex.so")
+QUICK = os.path.join(PKG, "_quick.so")
 SOURCES = ["core.cpp", "gather.hip", "sampler.hip", "changeset.hip", "neighbor_cache.hip",
            "static_policy.hip", "route.hip", "rows.hip", "codes.hip", "weights.hip", "linear.hip", "resident.hip", "few.hip",
            "bias.hip", "norm.hip", "lookup.hip"]
@@ -37,12 +38,31 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_quick() -> None:
+    """The layers' calls without the interpreter's part (csrc/quick.cpp), against the installed torch.  Without it the Python
+    names do the same."""
+    try:
+        import sysconfig
+
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError:
+        return
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           *(f"-isystem{p}" for p in include), os.path.join(CSRC, "quick.cpp"), "-o", QUICK, "-L", lib,
+                           "-ltorch", "-ltorch_cpu", "-lc10", "-ltorch_python", "-L", PKG, "-lginex", "-Wl,-rpath,$ORIGIN"])
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=4) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
     subprocess.check_call(cmd)
+    _build_quick()
     if verbose:
         print("built", LIB)
     return LIB

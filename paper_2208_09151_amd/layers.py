@@ -18,10 +18,26 @@ import torch
 from . import _lib
 from ._lib import WeightsDesc
 from .api import GinexError, _check
-from .training import (_TYPES, Compressed, Route, _activation, _dense, _first_derivative, _here, _out, _overwritten, _recorded,
-                       _rows, _space, _stream, _with, activate_backward, compress, dispatch_backward, weight_gradient)
+from .training import (_TYPES, ACTIVATIONS, Compressed, Route, _activation, _dense, _first_derivative, _here, _out, _overwritten,
+                       _raw_stream, _recorded, _rows, _space, _stream, _with, activate_backward, compress, dispatch_backward, weight_gradient)
 
 FEW_ROWS, FEW_TOP = 64, 16      # of expert_layer
+
+# The plain case of a call without the interpreter's part: False until it has been looked for, None where there is none.
+_quick = False
+_NO_ROUTE = (None, None, None)
+
+
+def _quick_for(x):
+    """(the compiled calls, current GPU, its stream) for a call on ``x``, or None."""
+    global _quick
+    if _quick is False:
+        _lib.load()
+        _quick = _lib.quick() if _raw_stream is not None else None
+    if _quick is None or not getattr(x, "is_cuda", False):
+        return None
+    device = torch._C._cuda_getDevice()
+    return _quick, device, _raw_stream(device)
 
 
 def _layer_weights(weight, like, experts):
@@ -112,6 +128,13 @@ def linear(x, weight, bias=None, activation=None, residual=None, route: Route = 
     slots', [rows * top, out]: those of ``x`` [rows, width] by the route, or (``slots``) of ``x`` [rows * top, width] as they
     are; weights and biases are the experts', and slots without a row are 0.  ``keep``: (result, what the activation is applied
     to in 8 bits, for activate_backward).  ``out`` may be ``residual``."""
+    if out is None and not keep and (activation is None or activation in ACTIVATIONS):
+        at = _quick_for(x)
+        got = at and at[0].linear(at[1], at[2], x, weight, bias, 0 if activation is None else ACTIVATIONS[activation], residual,
+                                  *(_NO_ROUTE if route is None else route._tensors()), bool(slots))
+        if got:
+            _check(got[0])
+            return got[1]
     desc = _rows(x, "x")
     experts = None if route is None else route.experts
     if _any_grad(x, weight, bias, residual):
@@ -143,6 +166,8 @@ def linear_backward(grad, weight, route: Route = None, out=None):
     activate_backward); with a route it is the slots' and so is the result, which dispatch_backward adds up by rows."""
     if not isinstance(weight, torch.Tensor) or weight.dim() < 2:
         raise ValueError("weight: expected a tensor [width, out] or [experts, width, out]")
+    if not torch.is_grad_enabled():
+        return linear(grad, weight.mT, route=route, slots=route is not None, out=out)
     with torch.no_grad():
         return linear(grad, weight.mT, route=route, slots=route is not None, out=out)
 
@@ -150,6 +175,12 @@ def linear_backward(grad, weight, route: Route = None, out=None):
 def bias_gradient(grad, route: Route = None, out=None, workspace=None):
     """ginex_bias_gradient: the sum of ``grad``'s rows, f32 [width]; with a route the sums of the experts' slots, [experts,
     width]."""
+    if out is None and workspace is None:
+        at = _quick_for(grad)
+        got = at and at[0].bias_gradient(at[1], at[2], grad, *(_NO_ROUTE if route is None else route._tensors()))
+        if got:
+            _check(got[0])
+            return got[1]
     lib = _lib.load()
     desc = _rows(grad, "grad")
     experts = 1 if route is None else route.experts
@@ -171,6 +202,13 @@ def expert_layer(x, router, weight, top, activation=None, bias=None, out=None, w
     """ginex_expert_layer: a whole layer of experts for up to 64 rows: the ``top`` experts of the largest scores
     ``x router^T`` (``router`` [experts, width]), and the sum of their answers activation(x weight + bias) by the softmax of
     those scores.  It has no gradient."""
+    if out is None and workspace is None and (activation is None or activation in ACTIVATIONS):
+        at = _quick_for(x)
+        got = at and at[0].expert_layer(at[1], at[2], x, router, weight, bias, top,
+                                        0 if activation is None else ACTIVATIONS[activation])
+        if got:
+            _check(got[0])
+            return got[1]
     lib = _lib.load()
     desc, rdesc = _rows(x, "x"), _rows(router, "router")
     if _any_grad(x, router, weight, bias):
@@ -214,6 +252,12 @@ class LayerNorm(torch.autograd.Function):
 def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
     """ginex_layer_norm over the rows of ``x``; with ``stats`` also f32 [rows, 2], mean and 1 / sqrt(variance + eps) of every
     row, for layer_norm_backward.  ``out`` may be ``x``."""
+    if out is None:
+        at = _quick_for(x)
+        got = at and at[0].layer_norm(at[1], at[2], x, weight, bias, eps, bool(stats))
+        if got:
+            _check(got[0])
+            return got[1:] if stats else got[1]
     desc = _rows(x, "x")
     if _any_grad(x, weight, bias):
         _recorded(out)
@@ -231,6 +275,12 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
 def layer_norm_backward(grad, x, stats, weight=None, vectors=True, out=None, workspace=None):
     """ginex_layer_norm_backward: the gradients of ``x``, of the weight and of the bias (f32 [width]; None with ``vectors``
     False).  ``out`` may be ``grad``."""
+    if out is None and workspace is None and vectors:
+        at = _quick_for(grad)
+        got = at and at[0].layer_norm_backward(at[1], at[2], grad, x, stats, weight)
+        if got:
+            _check(got[0])
+            return got[1:]
     lib = _lib.load()
     desc, xdesc = _rows(grad, "grad"), _rows(x, "x")
     _dense(stats, "stats", (xdesc.rows, 2), torch.float32)
@@ -278,6 +328,12 @@ class Lookup(torch.autograd.Function):
 
 def lookup(table, ids, scale=1.0, out=None):
     """ginex_lookup: ``scale`` times the rows ``ids`` (int32 or int64) of ``table``; 0 for an id outside of it."""
+    if out is None:
+        at = _quick_for(table)
+        got = at and at[0].lookup(at[1], at[2], table, ids, scale)
+        if got:
+            _check(got[0])
+            return got[1]
     desc = _rows(table, "table")
     wide = _ids(ids)
     if _any_grad(table):
@@ -290,6 +346,12 @@ def lookup(table, ids, scale=1.0, out=None):
 
 def lookup_backward(grad, ids, rows, scale=1.0, out=None, workspace=None):
     """ginex_lookup_backward: the gradient of a table of ``rows`` rows, of ``grad``'s type."""
+    if out is None and workspace is None:
+        at = _quick_for(grad)
+        got = at and at[0].lookup_backward(at[1], at[2], grad, ids, rows, scale)
+        if got:
+            _check(got[0])
+            return got[1]
     lib = _lib.load()
     desc = _rows(grad, "grad")
     wide = _ids(ids)
