@@ -65,17 +65,12 @@ struct Plan {
   float* part;          // [rows x top x out]
 };
 
-// A workgroup a row.  Products in f64 are exact for all types, so what is chosen does not depend on how a sum is rounded
-// (but for scores that are equal to 2^-50 or so).
+// The scores of one row.  Products in f64 are exact for all types, so what is chosen does not depend on how a sum is rounded
+// (but for scores that are equal to 2^-50 or so).  Called by ROUTE_THREADS.
 template <typename T>
-__global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
-                                                       int32_t top, Width width, Plan plan, int32_t tiles) {
-  constexpr int N = Chunk<T>::N, U = 4, EACH = GINEX_MAX_EXPERTS / WAVE;
-  __shared__ double scores[GINEX_MAX_EXPERTS];
+__device__ __forceinline__ void few_scores(const T* row, RowsOf<const T> router, int32_t experts, Width width, double* scores) {
+  constexpr int N = Chunk<T>::N, U = 4;
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
-  const T* const row = x.at(blockIdx.x);
-  if (blockIdx.x == 0)
-    for (int32_t i = threadIdx.x; i < tiles; i += ROUTE_THREADS) plan.done[i] = 0;
   for (int32_t e0 = wave; e0 < experts; e0 += U * ROUTE_WAVES) {
     double sum[U] = {};
     // two chunks of U experts in flight
@@ -102,12 +97,16 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, 
     for (int u = 0; u < U; ++u)
       if (lane == WAVE - 1 && e0 + u * ROUTE_WAVES < experts) scores[e0 + u * ROUTE_WAVES] = sum[u];
   }
-  __syncthreads();
-  if (wave > 0) return;
+}
+
+// A wave's choice by the scores: lane j gets choice j and its share.
+__device__ __forceinline__ void few_choices(const double* scores, int32_t experts, int32_t top, int32_t& mine, float& share) {
+  constexpr int EACH = GINEX_MAX_EXPERTS / WAVE;
+  const int lane = lane_id();
   uint64_t rank[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) rank[i] = lane + i * WAVE < experts ? rank_of(scores[lane + i * WAVE]) : 0;
-  int32_t mine = 0;           // lane j has choice j
+  mine = 0;
   for (int32_t j = 0; j < top; ++j) {
     uint64_t best = rank[0];
     uint32_t at = lane;
@@ -128,24 +127,41 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, 
   }
   const double score = scores[mine], most = __shfl(score, 0, WAVE);
   const double weight = lane < top ? exp(score - most) : 0.0, total = __shfl(sum_to_last(weight), WAVE - 1, WAVE);
-  if (lane < top) {
-    plan.chosen[(int64_t)blockIdx.x * top + lane] = mine;
-    plan.share[(int64_t)blockIdx.x * top + lane] = (float)(weight / total);
+  share = (float)(weight / total);
+}
+
+// A workgroup a row.
+template <typename T>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
+                                                             int32_t top, Width width, Plan plan, int32_t tiles) {
+  __shared__ double scores[GINEX_MAX_EXPERTS];
+  if (blockIdx.x == 0)
+    for (int32_t i = threadIdx.x; i < tiles; i += ROUTE_THREADS) plan.done[i] = 0;
+  few_scores(x.at(blockIdx.x), router, experts, width, scores);
+  __syncthreads();
+  if (threadIdx.x >= WAVE) return;
+  int32_t mine;
+  float share;
+  few_choices(scores, experts, top, mine, share);
+  if (lane_id() < top) {
+    plan.chosen[(int64_t)blockIdx.x * top + lane_id()] = mine;
+    plan.share[(int64_t)blockIdx.x * top + lane_id()] = share;
   }
 }
 
 // Rows of one expert and their sums: x[row(i)] W for i < count <= 16; of column 4 (lane % 16) + j of the workgroup's in operand j.
-// `row_of(i)` is the row of x, negative for a row of zeros.
-template <typename T, bool TURNED, int WAVES, typename RowOf>
-__device__ __forceinline__ void few_sums(RowsOf<const T> x, const T* __restrict__ w, int64_t stride, int32_t width, Width out,
-                                         int32_t n0, int32_t count, RowOf row_of, float4v (&sum)[4]) {
+// `row_of(i)` is the row of x, negative for a row of zeros.  `wave` of the `waves` that share the width.
+template <typename T, bool TURNED, typename RowOf>
+__device__ __forceinline__ void few_sums(int wave, int waves, RowsOf<const T> x, const T* __restrict__ w,
+                                         int64_t stride, int32_t width, Width out, int32_t n0, int32_t count, RowOf row_of,
+                                         float4v (&sum)[4]) {
   constexpr int N = Chunk<T>::N, STEP = 4 * N, UNIT = 2 * STEP;       // a unit is 128 bytes of a row
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), group = lane / 16;
+  const int lane = lane_id(), group = lane / 16;
   const Width along = {width, (int32_t)((width + N - 1) / N * N - width)};
   const int64_t r = row_of(lane % 16 < count ? lane % 16 : 0);
   const T* const row = x.at(r >= 0 ? r : 0);
   const int32_t n = n0 + lane % 16 * 4;
-  for (int32_t k0 = wave * UNIT; k0 < width; k0 += WAVES * UNIT) {
+  for (int32_t k0 = wave * UNIT; k0 < width; k0 += waves * UNIT) {
     ChunkWords<T> fa[2], fb[2][4];
     typename Four<T>::Wide raw[2][N];
 #pragma unroll
@@ -209,7 +225,7 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
   __shared__ float room[WAVES][16][PITCH];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   int32_t expert, count;
-  if (rows == 1) {                  // a row's experts are all different
+  if (rows == 1) {                  // (a row's experts are all different)
     if (blockIdx.z > 0) return;
     expert = plan.chosen[blockIdx.y];
     if (threadIdx.x == 0) list[0] = blockIdx.y;
@@ -251,8 +267,8 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
   }
   const int32_t n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
   float4v sum[4] = {};
-  few_sums<T, TURNED, WAVES>(x, weights.of(expert), weights.stride, width, out, n0, count,
-                             [&](int32_t i) { return (int64_t)(list[i] / top); }, sum);
+  few_sums<T, TURNED>(__builtin_amdgcn_readfirstlane(wave), WAVES, x, weights.of(expert), weights.stride, width, out, n0,
+                      count, [&](int32_t i) { return (int64_t)(list[i] / top); }, sum);
   const float b = bias && c < out.width ? (float)bias[(int64_t)expert * out.width + c] : 0.f;
   float v[16 / WAVES];
   join_waves<WAVES>(sum, room, v);
@@ -302,6 +318,50 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
   }
 }
 
+// One row, in one launch: every workgroup finds the row's experts by itself and has 64 columns of all of them, a part of its waves
+// for each.  It costs the router's bytes once a workgroup, and spares a launch and the meeting of the workgroups.
+constexpr int MOST_OF_ONE = 2;
+template <typename T, bool TURNED>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_few_one(RowsOf<const T> x, RowsOf<const T> router, int32_t experts, int32_t top,
+                                                           Width along, WeightsOf<T> weights,
+                                                           const T* __restrict__ bias, Width out, int32_t activation, T* y) {
+  __shared__ double scores[GINEX_MAX_EXPERTS];
+  __shared__ int32_t chosen[MOST_OF_ONE];
+  __shared__ float shares[MOST_OF_ONE], room[ROUTE_WAVES][WAVE_COLUMNS];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int32_t n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
+  few_scores(x.at(0), router, experts, along, scores);
+  __syncthreads();
+  if (wave == 0) {
+    int32_t mine;
+    float share;
+    few_choices(scores, experts, top, mine, share);
+    if (lane < top) {
+      chosen[lane] = mine;
+      shares[lane] = share;
+    }
+  }
+  __syncthreads();
+  const int32_t each = ROUTE_WAVES / top, j = wave / each;      // `each` waves an expert
+  float4v sum[4] = {};
+  few_sums<T, TURNED>(wave % each, each, x, weights.of(__builtin_amdgcn_readfirstlane(chosen[j])), weights.stride, along.width, out,
+                      n0, 1, [](int32_t) { return (int64_t)0; }, sum);
+  if (lane % 16 == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<float4v*>(&room[wave][lane / 16 * 16 + 4 * i]) = float4v{sum[0][i], sum[1][i], sum[2][i], sum[3][i]};
+  }
+  __syncthreads();
+  if (wave > 0 || c >= out.width) return;
+  float total = 0.f;
+  for (int32_t k = 0; k < top; ++k) {
+    float z = bias ? (float)bias[(int64_t)chosen[k] * out.width + c] : 0.f;
+    for (int32_t w = 0; w < each; ++w) z += room[k * each + w][lane];
+    total = fmaf(shares[k], activated_by<sizeof(T) == 4>(activation, z), total);
+  }
+  y[c] = (T)total;
+}
+
 // 16 slots of one expert, or without one, or 16 rows a workgroup.
 template <typename T, bool TURNED, int WAVES>
 __global__ __launch_bounds__(WAVES* WAVE) void k_few_linear(RowsOf<const T> x, int64_t rows, WeightsOf<T> weights,
@@ -320,12 +380,13 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_linear(RowsOf<const T> x, i
   const bool none = expert == experts;        // slots without an expert are cleared
   float4v sum[4] = {};
   if (!none)
-    few_sums<T, TURNED, WAVES>(x, weights.of(expert), weights.stride, width, out, n0, count,
-                               [&](int32_t i) -> int64_t {
-                                 const int64_t r = source ? (int64_t)source[begin + i] : begin + i;
-                                 return r < rows ? r : -1;
-                               },
-                               sum);
+    few_sums<T, TURNED>(__builtin_amdgcn_readfirstlane(wave), WAVES, x, weights.of(expert), weights.stride, width, out, n0,
+                        count,
+                        [&](int32_t i) -> int64_t {
+                          const int64_t r = source ? (int64_t)source[begin + i] : begin + i;
+                          return r < rows ? r : -1;
+                        },
+                        sum);
   const float b = !none && e.bias && c < out.width
                       ? (float)static_cast<const T*>(e.bias)[(int64_t)expert * out.width + c] : 0.f;
   float v[16 / WAVES];
@@ -456,6 +517,18 @@ extern "C" int32_t ginex_expert_layer(const ginex_rows_t* x, const ginex_rows_t*
     using T = decltype(t);
     const int32_t rows = (int32_t)x->rows, pairs = rows * top;
     const int32_t tiles = (int32_t)ceil_div(weights->out, WAVE_COLUMNS);
+    // One row that has one or two experts in one launch, where what a workgroup reads of router and weights is little: 1024 ->
+    // 1024 of 64 experts, one a row, f16 10.8 us instead of 14.6, two 14.4 (15.6), 256 -> 256 of 8, two a row, 9.0 (12.3); but
+    // 2048 -> 2048 of 32, two a row, 25.0 (23.4), and eight a row of 256 -> 256 18.0 (15.7).
+    const int64_t bytes = sizeof(T), of_one = (weights->experts + (int64_t)top * WAVE_COLUMNS) * weights->width * bytes;
+    if (rows == 1 && top <= MOST_OF_ONE && of_one <= 384 * 1024) {
+      const auto one = weights->turned ? k_few_one<T, true> : k_few_one<T, false>;
+      hipLaunchKernelGGL(one, dim3((unsigned)tiles), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
+                         weights->experts, top, Width::of<T>(x->width), weights_of<T>(weights),
+                         static_cast<const T*>(bias), Width::of<T>(weights->out), activation, static_cast<T*>(y->data));
+      GINEX_LAUNCH_CHECK();
+      return GINEX_OK;
+    }
     hipLaunchKernelGGL(k_few_route<T>, dim3((unsigned)rows), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
                        weights->experts, top, Width::of<T>(x->width), space.plan, tiles);
     GINEX_LAUNCH_CHECK();
