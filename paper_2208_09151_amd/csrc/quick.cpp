@@ -86,6 +86,10 @@ bool vector_of(PyObject* o, int device, at::ScalarType type, int64_t rows, int64
 bool routing_of(PyObject* offsets, PyObject* slot, PyObject* source, int device, ginex_routing_t& r) {
   at::Tensor o, s, f;
   if (!plain(offsets, device, o) || !plain(slot, device, s) || !plain(source, device, f)) return false;
+  if (o.scalar_type() != at::kLong || s.scalar_type() != at::kInt || f.scalar_type() != at::kInt) return false;
+  if (!o.is_contiguous() || !s.is_contiguous() || !f.is_contiguous()) return false;
+  if (o.dim() != 1 || o.numel() < 2 || o.numel() - 1 > GINEX_MAX_EXPERTS || s.dim() != 2 || s.size(1) > INT32_MAX) return false;
+  if (f.dim() != 1 || f.numel() != s.numel()) return false;
   r = {s.size(0), (int32_t)s.size(1), (int32_t)(o.numel() - 1), static_cast<int64_t*>(o.data_ptr()),
        static_cast<int32_t*>(s.data_ptr()), static_cast<int32_t*>(f.data_ptr())};
   return true;
@@ -96,6 +100,13 @@ at::Tensor space(size_t bytes, const at::Tensor& like) {
 }
 
 void* stream_of(PyObject* o) { return PyLong_AsVoidPtr(o); }
+
+bool number_of(PyObject* o, int64_t most, int64_t& v) {
+  if (!PyLong_Check(o)) return false;
+  int overflow = 0;
+  v = PyLong_AsLongLongAndOverflow(o, &overflow);
+  return overflow == 0 && v >= 0 && v <= most;
+}
 
 PyObject* answer(int32_t rc, std::initializer_list<at::Tensor> results) {
   PyObject* const tuple = PyTuple_New((Py_ssize_t)results.size() + 1);
@@ -127,6 +138,8 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     ginex_routing_t route;
     const void* bias;
     const bool routed = a[7] != Py_None, by_slot = a[10] == Py_True;
+    int64_t activation;
+    if (!number_of(a[5], INT32_MAX, activation)) Py_RETURN_NONE;
     if (!plain(a[2], device, x) || !plain(a[3], device, weight) || !rows_of(x, from)) Py_RETURN_NONE;
     if (!weights_of(weight, routed ? 3 : 2, x.scalar_type(), w)) Py_RETURN_NONE;
     if (routed && !routing_of(a[7], a[8], a[9], device, route)) Py_RETURN_NONE;
@@ -140,9 +153,10 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!routed && by_slot) Py_RETURN_NONE;
     const at::Tensor y = at::empty({slots, w.out}, x.options());
     rows_of(y, to);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_linear(&from, &w, bias, (int32_t)PyLong_AsLong(a[5]), has_residual ? &and_ : nullptr,
-                                    routed ? &route : nullptr, by_slot, &to, nullptr, stream_of(a[1]));
+      return ginex_linear(&from, &w, bias, (int32_t)activation, has_residual ? &and_ : nullptr, routed ? &route : nullptr,
+                          by_slot, &to, nullptr, stream);
     });
     return answer(rc, {y});
   });
@@ -164,9 +178,10 @@ PyObject* bias_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::TensorOptions f32 = grad.options().dtype(at::kFloat);
     const at::Tensor out = routed ? at::empty({route.experts, from.width}, f32) : at::empty({from.width}, f32);
     const at::Tensor ws = space(need, grad);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_bias_gradient(&from, routed ? &route : nullptr, static_cast<float*>(out.data_ptr()), ws.data_ptr(),
-                                           ws.numel(), stream_of(a[1]));
+      return ginex_bias_gradient(&from, routed ? &route : nullptr, static_cast<float*>(out.data_ptr()), ws.data_ptr(), ws.numel(),
+                                 stream);
     });
     return answer(rc, {out});
   });
@@ -185,14 +200,15 @@ PyObject* expert_layer(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!rows_of(x, from) || !rows_of(router, by) || router.scalar_type() != x.scalar_type()) Py_RETURN_NONE;
     if (!weights_of(weight, 3, x.scalar_type(), w)) Py_RETURN_NONE;
     if (!vector_of(a[5], device, x.scalar_type(), w.experts, w.out, 2, bias)) Py_RETURN_NONE;
-    const int32_t top = (int32_t)PyLong_AsLong(a[6]);
-    const size_t need = ginex_expert_layer_workspace_bytes(from.rows, top, w.experts, w.width, w.out);
+    int64_t top, activation;
+    if (!number_of(a[6], GINEX_MAX_FEW_TOP, top) || !number_of(a[7], INT32_MAX, activation)) Py_RETURN_NONE;
+    const size_t need = ginex_expert_layer_workspace_bytes(from.rows, (int32_t)top, w.experts, w.width, w.out);
     if (need == 0) Py_RETURN_NONE;
     const at::Tensor y = at::empty({from.rows, w.out}, x.options()), ws = space(need, x);
     rows_of(y, to);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_expert_layer(&from, &by, &w, bias, top, (int32_t)PyLong_AsLong(a[7]), &to, ws.data_ptr(), ws.numel(),
-                                          stream_of(a[1]));
+      return ginex_expert_layer(&from, &by, &w, bias, (int32_t)top, (int32_t)activation, &to, ws.data_ptr(), ws.numel(), stream);
     });
     return answer(rc, {y});
   });
@@ -213,9 +229,10 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     rows_of(y, to);
     const bool stats = a[6] == Py_True;
     const at::Tensor kept = stats ? at::empty({from.rows, 2}, x.options().dtype(at::kFloat)) : at::Tensor();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[5]);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_layer_norm(&from, weight, bias, (float)PyFloat_AS_DOUBLE(a[5]), &to,
-                                        stats ? static_cast<float*>(kept.data_ptr()) : nullptr, stream_of(a[1]));
+      return ginex_layer_norm(&from, weight, bias, eps, &to, stats ? static_cast<float*>(kept.data_ptr()) : nullptr, stream);
     });
     return stats ? answer(rc, {y, kept}) : answer(rc, {y});
   });
@@ -241,10 +258,11 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor dx = at::empty({from.rows, from.width}, x.options()), dweight = at::empty({from.width}, f32);
     const at::Tensor dbias = at::empty({from.width}, f32), ws = space(need, x);
     rows_of(dx, to);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
       return ginex_layer_norm_backward(&dy, &from, static_cast<float*>(stats.data_ptr()), weight, &to,
-                                                 static_cast<float*>(dweight.data_ptr()), static_cast<float*>(dbias.data_ptr()),
-                                                 ws.data_ptr(), ws.numel(), stream_of(a[1]));
+                                       static_cast<float*>(dweight.data_ptr()), static_cast<float*>(dbias.data_ptr()),
+                                       ws.data_ptr(), ws.numel(), stream);
     });
     return answer(rc, {dx, dweight, dbias});
   });
@@ -265,9 +283,10 @@ PyObject* lookup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!plain(a[2], device, table) || !ids_of(a[3], device, ids) || !rows_of(table, from) || !PyFloat_Check(a[4])) Py_RETURN_NONE;
     const at::Tensor out = at::empty({ids.numel(), from.width}, table.options());
     rows_of(out, to);
+    const float scale = (float)PyFloat_AS_DOUBLE(a[4]);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_lookup(&from, ids.data_ptr(), ids.scalar_type() == at::kLong, (float)PyFloat_AS_DOUBLE(a[4]), &to,
-                                    stream_of(a[1]));
+      return ginex_lookup(&from, ids.data_ptr(), ids.scalar_type() == at::kLong, scale, &to, stream);
     });
     return answer(rc, {out});
   });
@@ -280,17 +299,18 @@ PyObject* lookup_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int device = (int)PyLong_AsLong(a[0]);
     at::Tensor grad, ids;
     ginex_rows_t dy, to;
-    if (!plain(a[2], device, grad) || !ids_of(a[3], device, ids) || !rows_of(grad, dy) || !PyLong_Check(a[4]) || !PyFloat_Check(a[5]))
-      Py_RETURN_NONE;
-    const int64_t rows = PyLong_AsLongLong(a[4]);
-    if (ids.numel() != dy.rows) Py_RETURN_NONE;
+    int64_t rows;
+    if (!plain(a[2], device, grad) || !ids_of(a[3], device, ids) || !rows_of(grad, dy) || !PyFloat_Check(a[5])) Py_RETURN_NONE;
+    if (!number_of(a[4], INT64_MAX, rows) || ids.numel() != dy.rows) Py_RETURN_NONE;
     const size_t need = ginex_lookup_backward_workspace_bytes(dy.rows, rows, dy.width);
     if (need == 0) Py_RETURN_NONE;
     const at::Tensor out = at::empty({rows, dy.width}, grad.options()), ws = space(need, grad);
     rows_of(out, to);
+    const float scale = (float)PyFloat_AS_DOUBLE(a[5]);
+    void* const stream = stream_of(a[1]);
     const int32_t rc = unlocked([&] {
-      return ginex_lookup_backward(&dy, ids.data_ptr(), ids.scalar_type() == at::kLong, (float)PyFloat_AS_DOUBLE(a[5]), &to,
-                                             ws.data_ptr(), ws.numel(), stream_of(a[1]));
+      return ginex_lookup_backward(&dy, ids.data_ptr(), ids.scalar_type() == at::kLong, scale, &to, ws.data_ptr(), ws.numel(),
+                                   stream);
     });
     return answer(rc, {out});
   });

@@ -33,7 +33,7 @@ def reference(x, router, w, top, activation, bias, dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("turned", [False, True])
 @pytest.mark.parametrize("rows, width, out, experts, top, activation", [
-    (1, 1, 1, 1, 1, None), (1, 64, 64, 8, 2, "silu"), (1, 333, 70, 64, 16, "gelu"), (2, 5, 3, 3, 3, "relu"),
+    (1, 1, 1, 1, 1, None), (1, 64, 64, 8, 2, "silu"), (1, 1000, 70, 20, 1, "gelu"), (1, 100, 200, 3, 2, None), (1, 600, 70, 300, 2, "relu"), (1, 333, 70, 64, 16, "gelu"), (2, 5, 3, 3, 3, "relu"),
     (7, 100, 130, 1024, 4, "gelu"), (17, 1000, 33, 5, 2, "silu"), (48, 200, 65, 2, 2, "gelu"), (64, 96, 40, 70, 16, None)])
 def test_sizes(g, rows, width, out, experts, top, activation, turned, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows + width + experts)
