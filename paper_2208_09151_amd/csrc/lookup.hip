@@ -27,6 +27,50 @@ struct IdsWithPositions {
   }
 };
 
+// Few ids: the place of one is the number of those in front of it, which a workgroup counts for 64 of them, a lane each, its waves
+// for a part of all ids each.  It is one launch, where sorting by digits takes three or more for every one (us of a whole gradient, with
+// it and by digits: 64 ids of 1000 rows x 64 12.4 and 27.0, 4000 of 100 000 x 128 34 and 59, 8000 x 64 38 and 58, but 16 000 of 100 rows
+// 46 and 30).
+constexpr int PLACE_THREADS = 1024, PLACE_WAVES = PLACE_THREADS / WAVE, PLACE_STEP = 4096;
+constexpr int64_t MOST_PLACED = 8192;
+
+template <typename Id>
+__global__ __launch_bounds__(PLACE_THREADS) void k_lookup_places(IdsWithPositions<Id> in, int32_t n, uint64_t* __restrict__ sorted,
+                                                                 uint32_t* __restrict__ named, int64_t named_words) {
+  __shared__ __align__(16) uint32_t all[PLACE_STEP];
+  __shared__ uint32_t room[PLACE_WAVES][WAVE];
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  for (int64_t i = (int64_t)blockIdx.x * PLACE_THREADS + threadIdx.x; i < named_words; i += (int64_t)gridDim.x * PLACE_THREADS)
+    named[i] = 0;
+  const int32_t mine = blockIdx.x * WAVE + lane;
+  const uint64_t key = in(mine < n ? mine : n - 1);
+  uint32_t count = 0;
+  for (int32_t first = 0; first < n; first += PLACE_STEP) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PLACE_STEP / PLACE_THREADS; ++i) {
+      const int32_t j = first + i * PLACE_THREADS + threadIdx.x;
+      all[i * PLACE_THREADS + threadIdx.x] = j < n ? (uint32_t)(in(j) >> 32) : ~0u;         // (behind all)
+    }
+    __syncthreads();
+    const int32_t left = n - first < PLACE_STEP ? n - first : PLACE_STEP;
+    const int32_t each = ((left + 4 * PLACE_WAVES - 1) / (4 * PLACE_WAVES)) * 4;
+    const int32_t from = wave * each, to = from + each < PLACE_STEP ? from + each : PLACE_STEP;
+#pragma unroll 4
+    for (int32_t j = from; j < to; j += 4) {
+      const words4 id = *reinterpret_cast<const words4*>(&all[j]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) count += ((uint64_t)id[k] << 32 | (uint32_t)(first + j + k)) < key ? 1 : 0;
+    }
+  }
+  room[wave][lane] = count;
+  __syncthreads();
+  if (wave > 0 || mine >= n) return;
+  uint32_t place = 0;
+  for (int w = 0; w < PLACE_WAVES; ++w) place += room[w][lane];
+  sorted[place] = key;
+}
+
 // U chunks a thread, THREADS apart; ids first, then rows, then stores.
 template <typename T, typename Id>
 __global__ __launch_bounds__(THREADS) void k_lookup(RowsOf<const T> table, int64_t rows, const Id* __restrict__ ids,
@@ -315,6 +359,16 @@ int32_t check_ids(const void* ids, int32_t ids_64, int64_t n) {
 
 template <typename Id>
 hipError_t sort_ids(const void* ids, int64_t n, int64_t rows, const LookupSpace& s, hipStream_t st, uint64_t** sorted) {
+  const int64_t words = ceil_div(rows, 4);
+  if (n > 0 && n <= MOST_PLACED) {
+    hipLaunchKernelGGL(k_lookup_places<Id>, dim3((unsigned)ceil_div(n, WAVE)), dim3(PLACE_THREADS), 0, st,
+                       IdsWithPositions<Id>{static_cast<const Id*>(ids), (uint32_t)rows}, (int32_t)n, s.a,
+                       reinterpret_cast<uint32_t*>(s.named), words);
+    *sorted = s.a;
+    return hipGetLastError();
+  }
+  if (hipError_t e = fill_async(reinterpret_cast<uint32_t*>(s.named), words, 0u, st)) return e;
+  if (n == 0) return hipSuccess;
   int bits = 1;
   while (bits < 32 && rows >> bits) ++bits;         // (of the value `rows`, too)
   const int passes = radix_passes(bits, n);
@@ -385,9 +439,9 @@ extern "C" int32_t ginex_lookup_backward(const ginex_rows_t* dy, const void* ids
   if (ws_bytes < s.bytes) return fail(GINEX_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", s.bytes, ws_bytes);
   if (rows == 0) return GINEX_OK;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  GINEX_HIP(fill_async(reinterpret_cast<uint32_t*>(s.named), ceil_div(rows, 4), 0u, st));
   uint64_t* sorted = nullptr;
-  if (n > 0) GINEX_HIP(ids_64 ? sort_ids<int64_t>(ids, n, rows, s, st, &sorted) : sort_ids<int32_t>(ids, n, rows, s, st, &sorted));
+  GINEX_HIP(ids_64 ? sort_ids<int64_t>(ids, n, rows, s, st, &sorted)
+                   : sort_ids<int32_t>(ids, n, rows, s, st, &sorted));
   return with_type(dy->type, [&](auto t) -> int32_t {
     using T = decltype(t);
     const int64_t cpr = ceil_div(dy->width, Chunk<T>::N);

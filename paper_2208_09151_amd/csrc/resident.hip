@@ -303,11 +303,13 @@ Fit fit_of(int64_t width, int64_t out, int bytes) {
 // Where the rows are many enough to pay for the weights' way into LDS (us of a call, this and tiles: bf16, 256 x 256, 60 000 rows
 // 25.5 and 21.1, 100 000 42.5 and 39.6, 177 000 56.5 and 61.6, 820 000 200 and 268; 8 experts, 152 000 slots, 256 x 128 41 and 34; 32
 // experts, 600 000 slots, 128 x 128 81 and 94; f16, 300 000 x 100, 47 out 30 and 39; f32, 128 x 128, 60 000 rows 28.6 and 25.0, 152 000
-// slots of 8 experts, 256 x 128 88 and 100; 820 000, 256 x 256 710 and 739).
+// slots of 8 experts, 256 x 128 88 and 100; 820 000, 256 x 256 710 and 739), and with each expert's anew: bf16 and f32, 162 000 slots,
+// 256 x 128, of 256 experts 65 and 54, 129 and 137, of 1024 117 and 72, 232 and 151; 600 000, 128 x 128, of 256 99 and 117, 238 and 263.
 bool resident_fits(const ginex_weights_t* w, int64_t slots) {
   const int bytes = element_bytes(w->type);
   const Fit f = fit_of(w->width, w->out, bytes);
-  return w->width >= 16 / bytes && w->out >= 16 / bytes && f.blocks <= (bytes == 4 ? 4 : 2) && slots >= (bytes == 4 ? 1 << 17 : 160000);
+  return w->width >= 16 / bytes && w->out >= 16 / bytes && f.blocks <= (bytes == 4 ? 4 : 2) &&
+         slots >= (bytes == 4 ? (1 << 17) + 512 * (int64_t)w->experts : 160000 + 400 * (int64_t)w->experts);
 }
 
 int32_t linear_resident(const ginex_rows_t* x, const ginex_weights_t* w, const ginex_routing_t* route, bool by_slot,
