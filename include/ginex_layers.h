@@ -31,11 +31,13 @@ typedef struct ginex_weights {
   int32_t type;          /* GINEX_F32, _BF16, _F16 */
 } ginex_weights_t;
 
-/* y[s, :] = f(x[s, :] W + bias) + residual[s, :], products summed in f32, the rest in f32, rounded once.  bias [experts x
- * out], of x's type, may be NULL (0), and so may residual.  Without a route s is a row, weights->experts is 1.  With one s is
- * a slot, W and bias are its expert's, and x[s] is x[source[s]] (by_slot 0; x has `rows` rows) or x[s] itself (by_slot 1;
- * rows * top); a slot without a row counts as a row of zeros, and y's rows from offsets[experts] on are cleared.  kept not
- * NULL: what f is applied to, in 8 bits (for ginex_activate_backward); cleared rows are codes of 0.  y may be residual. */
+/* y[s, :] = f(x[s, :] W + bias) + residual[s, :], products summed in f32, the rest in f32, rounded once.  f32 factors may be
+ * taken as three bf16 each: a product is then good to 2^-24 of itself, as a rounded one is, and what a factor has below 2^-133
+ * is left out.  bias [experts x out], of x's type, may be NULL (0), and so may residual.  Without a route s is a row,
+ * weights->experts is 1.  With one s is a slot, W and bias are its expert's, and x[s] is x[source[s]] (by_slot 0; x has `rows`
+ * rows) or x[s] itself (by_slot 1; rows * top); a slot without a row counts as a row of zeros, and y's rows from
+ * offsets[experts] on are cleared.  kept not NULL: what f is applied to, in 8 bits (for ginex_activate_backward); cleared rows
+ * are codes of 0.  y may be residual. */
 int32_t ginex_linear(const ginex_rows_t* x /*host struct*/, const ginex_weights_t* weights /*host struct*/, const void* bias,
                      int32_t activation, const ginex_rows_t* residual /*host struct or NULL*/,
                      const ginex_routing_t* route /*host struct or NULL*/, int32_t by_slot,

@@ -9,6 +9,10 @@
 // time; weights with dense columns are turned over in registers).  The waves' sums meet in LDS.  In a layer of experts each
 // leaves f(..) of its pairs in the workspace, and of the workgroups of the same columns the one that comes last adds them up,
 // in the order of j.
+//
+// One row, 1024 -> 1024 bf16, 7.2 us as a linear layer, 14.2 through two of 64 experts: latency.  48 rows through four of 32
+// experts, 500 -> 777 f16, 9.5 and 27 us, of which the weights' 25 MB would take 5; rows of 777 elements begin at any 2 bytes (768
+// columns: 28 instead of 37 for both).
 #include "activations.hpp"
 #include "codes.hpp"
 #include "layers.hpp"

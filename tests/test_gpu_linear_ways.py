@@ -128,3 +128,22 @@ def test_graphs(g, rows, width, out):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, g.linear(x, w, None, "gelu"))
+
+
+@pytest.mark.parametrize("rows, width, out", [FEW[2], TILES[3], TILES[6], RESIDENT[2], RESIDENT[6]])
+def test_f32_of_all_magnitudes(g, rows, width, out):
+    """Products of large and small numbers, and rows whose parts are beyond bf16's ends: a factor loses less than 2^-133."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    for of_x, of_w in [(2.0 ** -118, 2.0 ** 60), (2.0 ** 118, 2.0 ** -100), (2.0 ** 60, 2.0 ** -120)]:
+        x = rows_of(gen, rows, width, torch.float32, by=of_x)
+        w = weights_of(gen, (width, out), torch.float32, False) * of_w
+        want, off, _ = plain(x, w, None, None, None, torch.float32)
+        lost = 2.0 ** -133 * (x.double().abs().sum(1, keepdim=True) + w.double().abs().sum(0))
+        near(g.linear(x, w), want, rounded(want, off + lost, torch.float32))
+    # the largest numbers, which are none in bf16
+    most = torch.finfo(torch.float32).max
+    x = rows_of(gen, rows, width, torch.float32)
+    w = weights_of(gen, (width, out), torch.float32, False) * 2.0 ** -20
+    x[3, width // 2] = x[rows - 1, 0] = most
+    want, off, _ = plain(x, w, None, None, None, torch.float32)
+    near(g.linear(x, w), want, rounded(want, off, torch.float32))
