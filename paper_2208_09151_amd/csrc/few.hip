@@ -10,9 +10,9 @@
 // leaves f(..) of its pairs in the workspace, and of the workgroups of the same columns the one that comes last adds them up,
 // in the order of j.
 //
-// One row, 1024 -> 1024 bf16, 7.2 us as a linear layer, 14.2 through two of 64 experts: latency.  48 rows through four of 32
-// experts, 500 -> 777 f16, 9.5 and 27 us, of which the weights' 25 MB would take 5; rows of 777 elements begin at any 2 bytes (768
-// columns: 28 instead of 37 for both).
+// One row, 1024 -> 1024 f16, 7.2 us as a linear layer, 12.7 through two of 64 experts: latency.  48 rows through four of 32
+// experts, 500 -> 777 f16, 26.4 us for both, of which the weights' 25 MB would take 5; rows of 777 elements begin at any 2 bytes (768
+// columns: 20.9).
 #include "activations.hpp"
 #include "codes.hpp"
 #include "layers.hpp"
@@ -22,7 +22,6 @@ namespace {
 
 constexpr int ROUTE_THREADS = 1024, ROUTE_WAVES = ROUTE_THREADS / WAVE;
 constexpr int PITCH = WAVE_COLUMNS + 4;                   // of a row of sums in LDS: 16 rows of 4 words use every bank once
-constexpr int MOST_PAIRS = GINEX_MAX_FEW_ROWS * GINEX_MAX_FEW_TOP;
 
 // The sum over a wave, in its last lane: lane by lane inside rows of 16 (DPP), then across them.
 template <int CTRL, int ROWS>
@@ -103,9 +102,11 @@ __device__ __forceinline__ void few_scores(const T* row, RowsOf<const T> router,
   }
 }
 
-// A wave's choice by the scores: lane j gets choice j and its share.
+// A wave's choice by the scores, EACH a lane at most: lane j gets choice j and its share.  (A wave that comes by once waits for its
+// instructions more than for anything else, so that what a call does not need is not there: 48 rows, four of 32 experts each, take
+// 35.4 us with EACH 1 and 37.7 with 16.)
+template <int EACH>
 __device__ __forceinline__ void few_choices(const double* scores, int32_t experts, int32_t top, int32_t& mine, float& share) {
-  constexpr int EACH = GINEX_MAX_EXPERTS / WAVE;
   const int lane = lane_id();
   uint64_t rank[EACH];
 #pragma unroll
@@ -120,22 +121,29 @@ __device__ __forceinline__ void few_choices(const double* scores, int32_t expert
         best = rank[i];
         at = lane + i * WAVE;
       }
-    // the largest rank, its upper half first, and of those that have it the first expert
+    // the largest rank, its upper half first, and of those that have it the first expert; mostly the upper half tells
     const uint32_t hi = most_of_wave((uint32_t)(best >> 32));
-    const uint32_t lo = most_of_wave(best >> 32 == hi ? (uint32_t)best : 0);
-    at = ~most_of_wave(best == ((uint64_t)hi << 32 | lo) ? ~at : 0);
+    uint64_t who = __ballot(best >> 32 == hi);
+    if (who & (who - 1)) {
+      const uint32_t lo = most_of_wave(best >> 32 == hi ? (uint32_t)best : 0);
+      who = __ballot(best == ((uint64_t)hi << 32 | lo));
+      if (who & (who - 1)) who = __ballot(at == ~most_of_wave(who >> lane & 1 ? ~at : 0));
+    }
+    at = of_lane(at, __ffsll((unsigned long long)who) - 1);
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
       if (i * WAVE < experts && at == (uint32_t)(lane + i * WAVE)) rank[i] = 0;
     if (lane == j) mine = (int32_t)at;
   }
-  const double score = scores[mine], most = __shfl(score, 0, WAVE);
-  const double weight = lane < top ? exp(score - most) : 0.0, total = __shfl(sum_to_last(weight), WAVE - 1, WAVE);
+  // 2^t by the f32 instruction, of t's fraction: good to 2^-22
+  const double score = scores[mine], far = (score - __shfl(score, 0, WAVE)) * 1.4426950408889634;
+  const double t = far < -1000.0 ? -1000.0 : far, whole = rint(t);
+  const double weight = lane < top ? ldexp((double)__builtin_amdgcn_exp2f((float)(t - whole)), (int)whole) : 0.0, total = __shfl(sum_to_last(weight), WAVE - 1, WAVE);
   share = (float)(weight / total);
 }
 
 // A workgroup a row.
-template <typename T>
+template <typename T, int EACH>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, RowsOf<const T> router, int32_t experts,
                                                              int32_t top, Width width, Plan plan, int32_t tiles) {
   __shared__ double scores[GINEX_MAX_EXPERTS];
@@ -146,7 +154,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_few_route(RowsOf<const T> x, 
   if (threadIdx.x >= WAVE) return;
   int32_t mine;
   float share;
-  few_choices(scores, experts, top, mine, share);
+  few_choices<EACH>(scores, experts, top, mine, share);
   if (lane_id() < top) {
     plan.chosen[(int64_t)blockIdx.x * top + lane_id()] = mine;
     plan.share[(int64_t)blockIdx.x * top + lane_id()] = share;
@@ -217,58 +225,45 @@ __device__ __forceinline__ void join_waves(const float4v (&sum)[4], float (*room
   }
 }
 
+// A workgroup has 64 columns (x) of an expert's 16 pairs (z).  Which expert (y): each has its own workgroups, or, where there are
+// fewer pairs than experts, each pair has, and those of an expert's first pair do the work.
 template <typename T, bool TURNED, int WAVES>
 __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, int32_t pairs, int32_t top, int32_t rows,
-                                                                    WeightsOf<T> weights, const T* __restrict__ bias,
-                                                                    int32_t width, Width out, int32_t activation, Plan plan,
-                                                                    RowsOf<T> y) {
-  constexpr int THREADS = WAVES * WAVE;
-  __shared__ uint32_t used[GINEX_MAX_EXPERTS / 32];
-  __shared__ int32_t chosen[MOST_PAIRS], list[16];      // the experts of all pairs, and the workgroup's pairs
+                                                             WeightsOf<T> weights, int32_t by_pair,
+                                                             const T* __restrict__ bias, int32_t width, Width out,
+                                                             int32_t activation, Plan plan, RowsOf<T> y) {
+  __shared__ int32_t lists[WAVES][16];
   __shared__ int32_t is_last;
   __shared__ float room[WAVES][16][PITCH];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
-  int32_t expert, count;
-  if (rows == 1) {                  // (a row's experts are all different)
-    if (blockIdx.z > 0) return;
-    expert = plan.chosen[blockIdx.y];
-    if (threadIdx.x == 0) list[0] = blockIdx.y;
-    count = 1;
-    __syncthreads();
-  } else {
-    // the experts that are chosen at all: the workgroup has the blockIdx.y-th of them
-    if (threadIdx.x < GINEX_MAX_EXPERTS / 32) used[threadIdx.x] = 0;
-    __syncthreads();
+  const int32_t expert = by_pair ? plan.chosen[blockIdx.y] : (int32_t)blockIdx.y;
+  // every wave finds its pairs in their order
+  int32_t* const list = lists[wave];
+  int32_t have = -(int32_t)blockIdx.z * 16;
+  for (int32_t p0 = 0; p0 < pairs; p0 += 4 * WAVE) {
+    int32_t of_pair[4];
 #pragma unroll
-    for (int i = 0; i < MOST_PAIRS / THREADS; ++i) {
-      const int32_t p = threadIdx.x + i * THREADS;
-      if (p < pairs) {
-        const int32_t e = plan.chosen[p];
-        chosen[p] = e;
-        atomicOr(&used[e / 32], 1u << e % 32);
-      }
+    for (int k = 0; k < 4; ++k) {
+      const int32_t p = p0 + k * WAVE + lane;
+      of_pair[k] = plan.chosen[p < pairs ? p : pairs - 1];
     }
-    __syncthreads();
-    const uint32_t word = lane < GINEX_MAX_EXPERTS / 32 ? used[lane] : 0;
-    const uint32_t upto = wave_inclusive_scan((uint32_t)__popc(word));
-    if (blockIdx.y >= of_lane(upto, WAVE - 1)) return;
-    const int at = __ffsll((unsigned long long)__ballot(upto > blockIdx.y)) - 1;
-    uint32_t bits = of_lane(word, at);
-    for (uint32_t skip = blockIdx.y - (of_lane(upto, at) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
-    expert = at * 32 + __ffs((int)bits) - 1;
-    // its pairs in their order, of which this workgroup has 16; every wave finds them
-    int32_t have = -(int32_t)blockIdx.z * 16;
-    for (int32_t p0 = 0; p0 < pairs; p0 += WAVE) {
-      const bool is = p0 + lane < pairs && chosen[p0 + lane] == expert;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int32_t p = p0 + k * WAVE + lane;
+      const bool is = p < pairs && of_pair[k] == expert;
       const uint64_t who = __ballot(is);
+      if (who == 0) continue;
+      if (by_pair && p0 + k * WAVE + __ffsll((unsigned long long)who) - 1 < (int32_t)blockIdx.y) return;
       const int32_t place = have + __popcll(who & (((uint64_t)1 << lane) - 1));
-      if (is && wave == 0 && place >= 0 && place < 16) list[place] = p0 + lane;
+      if (is && place >= 0 && place < 16) list[place] = p;
       have += __popcll(who);
     }
-    if (have <= 0) return;
-    count = have < 16 ? have : 16;
-    __syncthreads();
   }
+  if (have <= 0) return;                    // (the same for all waves)
+  const int32_t count = have < 16 ? have : 16;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();          // lanes read what others of their wave have written
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   const int32_t n0 = blockIdx.x * WAVE_COLUMNS, c = n0 + lane;
   float4v sum[4] = {};
   few_sums<T, TURNED>(__builtin_amdgcn_readfirstlane(wave), WAVES, x, weights.of(expert), weights.stride, width, out, n0,
@@ -284,11 +279,12 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   // The last workgroup of these columns to come here finds what the others have left, whichever die they were on: stores and
-  // loads of that go past the dies' caches, and every wave waits for its stores before one thread counts its pairs.
+  // loads of that go past the dies' caches, and every wave waits for its stores before one thread counts its pairs.  So the
+  // count itself has nothing to write back or to invalidate, which would cost 3 to 8 us.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)
-    is_last = (int32_t)__hip_atomic_fetch_add(plan.done + blockIdx.x, (uint32_t)count, __ATOMIC_ACQ_REL,
+    is_last = (int32_t)__hip_atomic_fetch_add(plan.done + blockIdx.x, (uint32_t)count, __ATOMIC_RELAXED,
                                               __HIP_MEMORY_SCOPE_AGENT) + count == pairs;
   __syncthreads();
   if (!is_last || c >= out.width) return;
@@ -325,7 +321,7 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
 // One row, in one launch: every workgroup finds the row's experts by itself and has 64 columns of all of them, a part of its waves
 // for each.  It costs the router's bytes once a workgroup, and spares a launch and the meeting of the workgroups.
 constexpr int MOST_OF_ONE = 2;
-template <typename T, bool TURNED>
+template <typename T, bool TURNED, int EACH>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_few_one(RowsOf<const T> x, RowsOf<const T> router, int32_t experts, int32_t top,
                                                            Width along, WeightsOf<T> weights,
                                                            const T* __restrict__ bias, Width out, int32_t activation, T* y) {
@@ -339,7 +335,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_few_one(RowsOf<const T> x, Ro
   if (wave == 0) {
     int32_t mine;
     float share;
-    few_choices(scores, experts, top, mine, share);
+    few_choices<EACH>(scores, experts, top, mine, share);
     if (lane < top) {
       chosen[lane] = mine;
       shares[lane] = share;
@@ -449,6 +445,14 @@ int32_t check_few(int64_t rows, int32_t top, int32_t experts, int64_t width, int
   return GINEX_OK;
 }
 
+// Calls `go` with how many experts a lane has.
+template <typename Go>
+int32_t with_each(int32_t experts, Go go) {
+  if (experts <= WAVE) return go(std::integral_constant<int, 1>{});
+  if (experts <= 4 * WAVE) return go(std::integral_constant<int, 4>{});
+  return go(std::integral_constant<int, GINEX_MAX_EXPERTS / WAVE>{});
+}
+
 // Calls `go` with the waves of a workgroup: as many as the width has units of 128 bytes, 4, 8, or 16 where there are few
 // workgroups.
 template <typename Go>
@@ -522,27 +526,34 @@ extern "C" int32_t ginex_expert_layer(const ginex_rows_t* x, const ginex_rows_t*
     const int32_t rows = (int32_t)x->rows, pairs = rows * top;
     const int32_t tiles = (int32_t)ceil_div(weights->out, WAVE_COLUMNS);
     // One row that has one or two experts in one launch, where what a workgroup reads of router and weights is little: 1024 ->
-    // 1024 of 64 experts, one a row, f16 10.8 us instead of 14.6, two 14.4 (15.6), 256 -> 256 of 8, two a row, 9.0 (12.3); but
-    // 2048 -> 2048 of 32, two a row, 25.0 (23.4), and eight a row of 256 -> 256 18.0 (15.7).
+    // 1024 of 64 experts, one a row, f16 9.8 us instead of 14.1, two 12.7 (14.3), 256 -> 256 of 8, two a row, 7.5 (11.2); but
+    // 2048 -> 2048 of 32, two a row, 23.4 (22.3), and eight a row of 256 -> 256 18.0 (15.7).
     const int64_t bytes = sizeof(T), of_one = (weights->experts + (int64_t)top * WAVE_COLUMNS) * weights->width * bytes;
     if (rows == 1 && top <= MOST_OF_ONE && of_one <= 384 * 1024) {
-      const auto one = weights->turned ? k_few_one<T, true> : k_few_one<T, false>;
-      hipLaunchKernelGGL(one, dim3((unsigned)tiles), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
-                         weights->experts, top, Width::of<T>(x->width), weights_of<T>(weights),
-                         static_cast<const T*>(bias), Width::of<T>(weights->out), activation, static_cast<T*>(y->data));
+      return with_each(weights->experts, [&](auto of_lane) -> int32_t {
+        constexpr int EACH = decltype(of_lane)::value;
+        const auto one = weights->turned ? k_few_one<T, true, EACH> : k_few_one<T, false, EACH>;
+        hipLaunchKernelGGL(one, dim3((unsigned)tiles), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
+                           weights->experts, top, Width::of<T>(x->width), weights_of<T>(weights),
+                           static_cast<const T*>(bias), Width::of<T>(weights->out), activation, static_cast<T*>(y->data));
+        GINEX_LAUNCH_CHECK();
+        return GINEX_OK;
+      });
+    }
+    const int32_t routed = with_each(weights->experts, [&](auto of_lane) -> int32_t {
+      hipLaunchKernelGGL((k_few_route<T, decltype(of_lane)::value>), dim3((unsigned)rows), dim3(ROUTE_THREADS), 0, st,
+                         read_rows<T>(x), read_rows<T>(router), weights->experts, top, Width::of<T>(x->width), space.plan, tiles);
       GINEX_LAUNCH_CHECK();
       return GINEX_OK;
-    }
-    hipLaunchKernelGGL(k_few_route<T>, dim3((unsigned)rows), dim3(ROUTE_THREADS), 0, st, read_rows<T>(x), read_rows<T>(router),
-                       weights->experts, top, Width::of<T>(x->width), space.plan, tiles);
-    GINEX_LAUNCH_CHECK();
+    });
+    if (routed) return routed;
     const int32_t most = pairs < weights->experts ? pairs : weights->experts;
     return with_waves(weights->width, sizeof(T), (int64_t)tiles * most, [&](auto waves) -> int32_t {
       constexpr int WAVES = decltype(waves)::value;
       const auto kernel = weights->turned ? k_few_experts<T, true, WAVES> : k_few_experts<T, false, WAVES>;
       const dim3 grid((unsigned)tiles, (unsigned)most, (unsigned)ceil_div(rows, 16));
       hipLaunchKernelGGL(kernel, grid, dim3(WAVES * WAVE), 0, st, read_rows<T>(x), pairs, top, rows, weights_of<T>(weights),
-                         static_cast<const T*>(bias), (int32_t)weights->width, Width::of<T>(weights->out), activation,
+                         (int32_t)(most < weights->experts), static_cast<const T*>(bias), (int32_t)weights->width, Width::of<T>(weights->out), activation,
                          space.plan, rows_of<T>(y));
       GINEX_LAUNCH_CHECK();
       return GINEX_OK;
