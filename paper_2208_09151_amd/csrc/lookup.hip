@@ -45,6 +45,7 @@ __global__ __launch_bounds__(PLACE_THREADS) void k_lookup_places(IdsWithPosition
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   for (int64_t i = (int64_t)blockIdx.x * PLACE_THREADS + threadIdx.x; i < named_words; i += (int64_t)gridDim.x * PLACE_THREADS)
     named[i] = 0;
+  if ((int64_t)blockIdx.x * WAVE >= n) return;          // (one that only clears)
   const int32_t mine = blockIdx.x * WAVE + lane;
   const uint64_t key = in(mine < n ? mine : n - 1);
   uint32_t count = 0;
@@ -364,7 +365,10 @@ template <typename Id>
 hipError_t sort_ids(const void* ids, int64_t n, int64_t rows, const LookupSpace& s, hipStream_t st, uint64_t** sorted) {
   const int64_t words = ceil_div(rows, 4);
   if (n > 0 && n <= MOST_PLACED) {
-    hipLaunchKernelGGL(k_lookup_places<Id>, dim3((unsigned)ceil_div(n, WAVE)), dim3(PLACE_THREADS), 0, st,
+    int64_t groups = ceil_div(words, 4 * PLACE_THREADS);        // enough to clear a large table's marks
+    groups = groups < 2048 ? groups : 2048;
+    groups = groups > ceil_div(n, WAVE) ? groups : ceil_div(n, WAVE);
+    hipLaunchKernelGGL(k_lookup_places<Id>, dim3((unsigned)groups), dim3(PLACE_THREADS), 0, st,
                        IdsWithPositions<Id>{static_cast<const Id*>(ids), (uint32_t)rows}, (int32_t)n, s.a,
                        reinterpret_cast<uint32_t*>(s.named), words);
     *sorted = s.a;

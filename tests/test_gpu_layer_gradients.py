@@ -255,3 +255,42 @@ def test_training_with_blocks(g):
     from paper_2208_09151_amd.experts import train
     first, second = (train(config=1, steps=3, report=None, blocks=1) for _ in range(2))
     assert len(first) == 3 and all(l == l for l in first) and first[0] == second[0]
+
+
+@pytest.mark.parametrize("rows", [40, 700])
+def test_a_step_with_its_gradients_in_a_graph(g, rows):
+    """Lookup, layer norm, a layer of experts and one for all with a residual, captured with their backward passes."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    table = rows_of(gen, 50, 32, torch.float32).requires_grad_()
+    gain, shift = (torch.randn(32, generator=gen, device="cuda").requires_grad_() for _ in range(2))
+    w3 = (torch.randn((4, 32, 24), generator=gen, device="cuda") / 6).requires_grad_()
+    b3 = torch.randn((4, 24), generator=gen, device="cuda").requires_grad_()
+    w = (torch.randn((24, 32), generator=gen, device="cuda") / 5).requires_grad_()
+    leaves = (table, gain, shift, w3, b3, w)
+    ids = torch.randint(0, 50, (rows,), generator=gen, device="cuda")
+    chosen = torch.randint(-1, 4, (rows, 2), generator=gen, device="cuda")
+    share = torch.rand((rows, 2), generator=gen, device="cuda")
+    dy = rows_of(gen, rows, 32, torch.float32)
+
+    def step():
+        h = g.lookup(table, ids)
+        r = g.route(chosen, 4)
+        z = g.linear(g.layer_norm(h, gain, shift), w3, b3, "gelu", route=r)
+        y = g.linear(g.combine(z, r, share), w, None, "silu", h)
+        return (y.detach(), *torch.autograd.grad(y, leaves, dy))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        ids.copy_(torch.randint(0, 50, (rows,), generator=gen, device="cuda"))
+        chosen.copy_(torch.randint(-1, 4, (rows, 2), generator=gen, device="cuda"))
+        dy.copy_(rows_of(gen, rows, 32, torch.float32))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))

@@ -39,7 +39,8 @@ def check(g, table, dy, ids, scale):
 @pytest.mark.parametrize("rows, ids, width", [
     (1, 1, 1), (1, 100, 5), (7, 0, 33), (0, 9, 8), (5, 31, 64), (5, 32, 7), (40, 33, 100), (300, 5000, 128), (3000, 200, 16),
     (70000, 20000, 24), (17, 9000, 300), (100, 3000, 1000), (2, 40000, 9),
-    (50, 64, 8), (50, 65, 8), (1000, 4096, 8), (9, 4097, 16), (3000, 8192, 8), (3000, 8193, 8)])
+    (50, 64, 8), (50, 65, 8), (1000, 4096, 8), (9, 4097, 16), (3000, 8192, 8), (3000, 8193, 8),
+    (3_000_000, 5, 3), (2_000_003, 700, 2)])
 def test_sizes(g, rows, ids, width, wide, dtype):
     gen = torch.Generator(device="cuda").manual_seed(rows + ids + width)
     at = torch.randint(-1, rows + 1, (ids,), generator=gen, device="cuda")
