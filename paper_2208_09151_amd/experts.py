@@ -23,7 +23,7 @@ import sys
 
 import torch
 
-from .layers import expert_layer, layer_norm, linear, lookup
+from .layers import expert_layer, layer_norm, linear, lookup, lookup_backward
 from .training import (Activation, Combine, Compressed, Route, _first_derivative, activate, combine,  # noqa: F401
                        compress, dispatch, dispatch_backward, route, weight_gradient)
 
@@ -125,6 +125,20 @@ class Block(torch.nn.Module):
         return linear(h, self.down.weight.t(), self.down.bias, residual=x)
 
 
+class SumOfRows(torch.autograd.Function):
+    """out[s] = the sum of the rows r with of[r] = s: what lookup's gradient does, and lookup is its gradient."""
+
+    @staticmethod
+    def forward(ctx, rows, of, sums):
+        ctx.save_for_backward(of)
+        return lookup_backward(rows, of, sums)
+
+    @staticmethod
+    @_first_derivative
+    def backward(ctx, grad):
+        return lookup(grad.contiguous(), *ctx.saved_tensors), None, None
+
+
 class Classifier(torch.nn.Module):
     """An expert layer on all sampled rows, ``blocks`` residual blocks, the mean over a seed's first-hop neighbours, and a linear
     head."""
@@ -142,9 +156,11 @@ class Classifier(torch.nn.Module):
         seeds = rowptr.numel() - 1
         count = (rowptr[1:] - rowptr[:-1])
         of = torch.repeat_interleave(torch.arange(seeds, device=x.device), count)
-        around = torch.zeros((seeds, h.shape[1]), dtype=h.dtype, device=x.device)
-        rows = lookup(h, col) if len(self.blocks) else h[col.long()]        # (lookup's gradient adds up in one order)
-        around = around.index_add(0, of, rows) / count.clamp(min=1)[:, None]
+        if len(self.blocks):                # (these add up in one order, both ways)
+            around = SumOfRows.apply(lookup(h, col), of, seeds)
+        else:
+            around = torch.zeros((seeds, h.shape[1]), dtype=h.dtype, device=x.device).index_add(0, of, h[col.long()])
+        around = around / count.clamp(min=1)[:, None]
         return self.head(torch.cat([h[:seeds], around], 1))
 
 

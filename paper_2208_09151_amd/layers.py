@@ -168,7 +168,7 @@ def linear_backward(grad, weight, route: Route = None, out=None):
     activate_backward); with a route it is the slots' and so is the result, which dispatch_backward adds up by rows."""
     if not isinstance(weight, torch.Tensor) or weight.dim() < 2:
         raise ValueError("weight: expected a tensor [width, out] or [experts, width, out]")
-    if not torch.is_grad_enabled():
+    if not (torch.is_grad_enabled() and (weight.requires_grad or getattr(grad, "requires_grad", False))):
         return linear(grad, weight.mT, route=route, slots=route is not None, out=out)
     with torch.no_grad():
         return linear(grad, weight.mT, route=route, slots=route is not None, out=out)

@@ -294,3 +294,15 @@ def test_a_step_with_its_gradients_in_a_graph(g, rows):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+def test_sums_of_neighbours(g):
+    """Sums of rows and their gradients, exact for whole numbers."""
+    from paper_2208_09151_amd.experts import SumOfRows
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randint(-9, 9, (300, 20), generator=gen, device="cuda").float().requires_grad_()
+    of = torch.sort(torch.randint(0, 40, (300,), generator=gen, device="cuda"))[0]
+    dy = torch.randint(-9, 9, (41, 20), generator=gen, device="cuda").float()
+    y = SumOfRows.apply(rows, of, 41)
+    assert torch.equal(y, torch.zeros((41, 20), device="cuda").index_add(0, of, rows.detach()))
+    assert torch.equal(torch.autograd.grad(y, rows, dy)[0], dy[of])
