@@ -1,13 +1,15 @@
 // The calls of the layers' Python names for the plain case, without the interpreter's part: tensors' descriptors are made and
 // outputs allocated here.  Every function gives None for whatever it does not take (tensors elsewhere, other types or shapes, a
-// gradient that is to be recorded, subclasses of tensors), and the Python names go on with what they do without it; nothing is
-// refused here.  The call's status comes with the result, for the Python name to raise what the library says.
+// gradient that is to be recorded, a tangent of forward mode, tensors with a __torch_dispatch__ of their own), and the Python names
+// go on with what they do without it; nothing is refused here.  The call's status comes with the result, for the Python name to
+// raise what the library says.
 //
 // Measured on the host, us of a call without and with it: linear 12.8 and 5.3, expert_layer 15.2 and 7.8, layer norm 10.6 and 5.2, its
 // gradients 16.9 and 9.5, lookup 8.1 and 4.1, its gradient 23.7 and 19.1 (a dozen launches).
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -15,12 +17,15 @@
 
 namespace {
 
+// A tensor that carries a tangent of forward mode (there is one level of those).
+bool has_tangent(const at::Tensor& t) { return c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined(); }
+
 // A tensor that is used as it is: in the memory of GPU `device`, with no gradient to record.
 bool plain(PyObject* o, int device, at::Tensor& t) {
   if (!THPVariable_Check(o)) return false;
   t = THPVariable_Unpack(o);
   return t.is_cuda() && t.get_device() == device && t.layout() == at::kStrided && !t.key_set().has(c10::DispatchKey::Python) &&
-         !t.is_neg() && !(t.requires_grad() && c10::GradMode::is_enabled());
+         !t.is_neg() && !(t.requires_grad() && c10::GradMode::is_enabled()) && !has_tangent(t);
 }
 
 // Other threads run while the library does.

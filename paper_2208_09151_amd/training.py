@@ -6,7 +6,8 @@ last one is dense; any stride from row to row will do.  Every call enqueues on t
 returns at once.
 
 dispatch, combine and activate keep autograd's graph where it is recorded; their gradients are the calls that are made for
-them.  Results of those, and codes, are constants to autograd.
+them.  Results of those, and codes, are constants to autograd.  Tensors that carry a tangent of forward mode are refused
+everywhere, and so are such gradients in a backward pass.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ import functools
 from dataclasses import dataclass, field
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import CodesDesc, RoutingDesc, RowsDesc
@@ -36,6 +38,14 @@ def _stream(device=None):
     return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
+def _no_tangent(t, what):
+    """The kernels read a tensor's values, and what they give would count as a constant to forward mode (which no_grad leaves
+    on, and which is off inside of an autograd function)."""
+    if forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled() and isinstance(t, torch.Tensor) \
+            and forward_ad.unpack_dual(t).tangent is not None:
+        raise RuntimeError(f"{what}: no tangent of forward mode goes through this call")
+
+
 def _here(t, what, dtype=None):
     """A tensor in the memory of the current GPU."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -44,6 +54,7 @@ def _here(t, what, dtype=None):
         raise ValueError(f"{what}: on {t.device}, which is not the current GPU")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    _no_tangent(t, what)
     return t
 
 
@@ -117,6 +128,8 @@ def _first_derivative(backward):
     def checked(ctx, *grads):
         if torch.is_grad_enabled():
             raise RuntimeError(f"{type(ctx).__name__}: there is no second derivative (create_graph=True asks for one)")
+        for grad in grads:
+            _no_tangent(grad, type(ctx).__name__)
         return backward(ctx, *grads)
     return checked
 
