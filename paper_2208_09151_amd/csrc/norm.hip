@@ -281,24 +281,43 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward_long(RowsOf<const T> 
   }
 }
 
-// Columns of long rows: a thread's chunk over every gridDim.y-th row.  (x's mean is taken as it was rounded: what is left of it
-// would be another pass over the row.)
+// What is left of long rows when their means, as they were rounded, are taken away: rests[r] is the mean of that.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void k_norm_rests(RowsOf<const T> x, const float* __restrict__ stats, Width width,
+                                                        float per_width, float* __restrict__ rests) {
+  constexpr int N = Chunk<T>::N, STEP = THREADS * N;
+  __shared__ float room[2][WAVES][4];
+  const int64_t r = blockIdx.x;
+  const float mean = stats[2 * r];
+  float sum[1] = {};
+  for (int32_t c = threadIdx.x * N; c < width.width; c += STEP) {
+    float u[N];
+    load_chunk(x.at(r), c, width, u);
+#pragma unroll
+    for (int n = 0; n < N; ++n) sum[0] += c + n < width.width ? u[n] - mean : 0.f;
+  }
+  sums_of_row<1, true>(sum, THREADS, room, 0);
+  if (threadIdx.x == 0) rests[r] = sum[0] * per_width;
+}
+
+// Columns of long rows: a thread's chunk over every gridDim.y-th row.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void k_norm_columns(RowsOf<const T> dy, RowsOf<const T> x,
-                                                          const float* __restrict__ stats, int64_t rows, Width width,
-                                                          float* __restrict__ part) {
+                                                          const float* __restrict__ stats, const float* __restrict__ rests,
+                                                          int64_t rows, Width width, float* __restrict__ part) {
   constexpr int N = Chunk<T>::N;
   const int32_t c = (blockIdx.x * THREADS + threadIdx.x) * N;
   if (c >= width.width) return;
   float dw[N] = {}, db[N] = {};
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
     const float2 of_row = *reinterpret_cast<const float2*>(stats + 2 * r);
+    const float rest = rests[r];
     float u[N], g[N];
     load_chunk(x.at(r), c, width, u);
     load_chunk(dy.at(r), c, width, g);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      dw[n] = fmaf(g[n], (u[n] - of_row.x) * of_row.y, dw[n]);
+      dw[n] = fmaf(g[n], ((u[n] - of_row.x) - rest) * of_row.y, dw[n]);
       db[n] += g[n];
     }
   }
@@ -336,13 +355,16 @@ int64_t parts_of_norm(int64_t rows, const Deal& d) {
   const int64_t groups = d.whole ? rows : ceil_div(rows, THREADS >> d.shift);
   return groups < 1 ? 1 : (groups < MOST_PARTS ? groups : MOST_PARTS);
 }
+// Parts, and behind them a number for each of long rows.
 size_t norm_space(int64_t rows, int64_t width) {
-  int64_t parts = 0;
+  int64_t parts = 0, rests = 0;
   for (int chunk = 4; chunk <= 8; chunk += 4) {
-    const int64_t p = parts_of_norm(rows, deal_of(width, chunk));
+    const Deal d = deal_of(width, chunk);
+    const int64_t p = parts_of_norm(rows, d);
     parts = p > parts ? p : parts;
+    rests = d.is_long ? rows : rests;
   }
-  return (size_t)(parts * 2 * width) * sizeof(float) + 256;
+  return (size_t)(parts * 2 * width + rests) * sizeof(float) + 256;
 }
 
 template <typename Go>
@@ -454,13 +476,21 @@ extern "C" int32_t ginex_layer_norm_backward(const ginex_rows_t* dy, const ginex
         GINEX_LAUNCH_CHECK();
         return GINEX_OK;
       }
+      const int64_t step = (int64_t)1 << 23;
       // (the columns first: dx may be dy)
       if (part) {
+        float* const rests = part + parts * 2 * x->width;
+        for (int64_t r = 0; r < x->rows; r += step) {
+          const int64_t rows = x->rows - r < step ? x->rows - r : step;
+          hipLaunchKernelGGL(k_norm_rests<T>, dim3((unsigned)rows), dim3(THREADS), 0, st,
+                             RowsOf<const T>{read_rows<T>(x).data + r * x->stride, x->stride}, stats + 2 * r, width, per_width,
+                             rests + r);
+          GINEX_LAUNCH_CHECK();
+        }
         hipLaunchKernelGGL(k_norm_columns<T>, dim3((unsigned)ceil_div(x->width, THREADS * Chunk<T>::N), (unsigned)parts),
-                           dim3(THREADS), 0, st, read_rows<T>(dy), read_rows<T>(x), stats, x->rows, width, part);
+                           dim3(THREADS), 0, st, read_rows<T>(dy), read_rows<T>(x), stats, rests, x->rows, width, part);
         GINEX_LAUNCH_CHECK();
       }
-      const int64_t step = (int64_t)1 << 23;
       for (int64_t r = 0; r < x->rows; r += step) {
         const int64_t rows = x->rows - r < step ? x->rows - r : step;
         hipLaunchKernelGGL(k_norm_backward_long<T>, dim3((unsigned)rows), dim3(THREADS), 0, st,
