@@ -138,17 +138,19 @@ __device__ __forceinline__ void store_scaled(T* row, int32_t c, Width width, flo
 
 // A group goes through RUN sorted positions, a workgroup through as many runs beside each other as it has groups.  Ids that begin
 // and end in the workgroup's are written; of others it leaves parts [workgroups x 2 x width]: of the id that began in front, and
-// of the one that goes on.  named[v]: id v is there.
+// of the one that goes on.  named[v]: id v is there.  The launch's first workgroup is number `first`.
 template <typename T, int RUN>
 __global__ __launch_bounds__(THREADS) void k_lookup_sums(const uint64_t* __restrict__ sorted, int64_t n, uint32_t rows,
                                                          RowsOf<const T> dy, RowsOf<T> dtable, int32_t shift, Width width,
-                                                         float scale, float* __restrict__ part, uint8_t* __restrict__ named) {
+                                                         float scale, float* __restrict__ part, uint8_t* __restrict__ named,
+                                                         int64_t first) {
   constexpr int N = Chunk<T>::N, U = 4;
   __shared__ float heads[THREADS][N + 1];       // of every run, the sums of the id that began in front of it
   __shared__ uint8_t head_ends[THREADS];        // and whether that ends in the run
   const int32_t groups = THREADS >> shift, own = threadIdx.x >> shift, lane = threadIdx.x & ((1 << shift) - 1);
   const int32_t c = ((int32_t)(blockIdx.y << shift) + lane) * N;
-  const int64_t begin = ((int64_t)blockIdx.x * groups + own) * RUN;
+  const int64_t block = first + blockIdx.x;
+  const int64_t begin = (block * groups + own) * RUN;
   const int64_t end = begin + RUN < n ? begin + RUN : n;
   const bool there = begin < n;
   const uint32_t in_front = there && begin > 0 ? id_of(sorted[begin - 1]) : 0xFFFFFFFFu;
@@ -215,13 +217,13 @@ __global__ __launch_bounds__(THREADS) void k_lookup_sums(const uint64_t* __restr
   };
   if (goes_on && began) {
     if (follow(own + 1)) write();
-    else store_part<N>(part + (2 * (int64_t)blockIdx.x + 1) * width.width, c, of_parts, sum);
+    else store_part<N>(part + (2 * block + 1) * width.width, c, of_parts, sum);
   }
   if (own == 0 && headed) {
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = heads[threadIdx.x][i];
     if (!head_ends[0]) follow(1);
-    store_part<N>(part + 2 * (int64_t)blockIdx.x * width.width, c, of_parts, sum);
+    store_part<N>(part + 2 * block * width.width, c, of_parts, sum);
   }
 }
 
@@ -347,7 +349,6 @@ LookupSpace lookup_space(void* ws, int64_t n, int64_t rows, int64_t width) {
 }
 
 int32_t check_lookup_sizes(int64_t ids, int64_t rows, int64_t width) {
-  // (a launch has fewer than 2^32 threads)
   if (ids < 0 || ids > ((int64_t)1 << 30)) return fail(GINEX_ERR_ARG, "ids=%lld (0..2^30)", (long long)ids);
   if (rows < 0 || rows >= ((int64_t)1 << 31)) return fail(GINEX_ERR_ARG, "rows=%lld", (long long)rows);
   if (width < 1 || width > GINEX_MAX_WIDTH) return fail(GINEX_ERR_ARG, "width=%lld (1..%d)", (long long)width, GINEX_MAX_WIDTH);
@@ -458,10 +459,12 @@ extern "C" int32_t ginex_lookup_backward(const ginex_rows_t* dy, const void* ids
     const Width width = Width::of<T>(dy->width);
     const int32_t run_length = (int32_t)run_of(n) * (THREADS >> shift);
     const int64_t runs = ceil_div(n, run_length);
-    if (n > 0) {
-      const auto kernel = run_of(n) == SHORT_RUN ? k_lookup_sums<T, SHORT_RUN> : k_lookup_sums<T, LONG_RUN>;
-      hipLaunchKernelGGL(kernel, dim3((unsigned)runs, across), dim3(THREADS), 0, st, sorted, n, (uint32_t)rows, read_rows<T>(dy),
-                         rows_of<T>(dtable), shift, width, scale, s.part, s.named);
+    const auto kernel = run_of(n) == SHORT_RUN ? k_lookup_sums<T, SHORT_RUN> : k_lookup_sums<T, LONG_RUN>;
+    const int64_t step = (int64_t)1 << 23;        // (a launch has fewer than 2^32 threads)
+    for (int64_t first = 0; first < runs; first += step) {
+      const int64_t count = runs - first < step ? runs - first : step;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)count, across), dim3(THREADS), 0, st, sorted, n, (uint32_t)rows, read_rows<T>(dy),
+                         rows_of<T>(dtable), shift, width, scale, s.part, s.named, first);
       GINEX_LAUNCH_CHECK();
     }
     // a group for every run, and enough of them for the rows that are cleared
