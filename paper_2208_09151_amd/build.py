@@ -8,6 +8,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -40,7 +41,7 @@ def _compile(src: str) -> str:
 
 def _build_quick() -> None:
     """The layers' calls without the interpreter's part (csrc/quick.cpp), against the installed torch.  Without it the Python
-    names do the same."""
+    names do the same, so that a compiler that is missing or does not get through is told and is no error."""
     try:
         import sysconfig
 
@@ -50,10 +51,19 @@ def _build_quick() -> None:
         return
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
-                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                           *(f"-isystem{p}" for p in include), os.path.join(CSRC, "quick.cpp"), "-o", QUICK, "-L", lib,
-                           "-ltorch", "-ltorch_cpu", "-lc10", "-ltorch_python", "-L", PKG, "-lginex", "-Wl,-rpath,$ORIGIN"])
+    made = f"{QUICK[:-3]}.{os.getpid()}.so"         # (in its place once it is whole)
+    command = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{p}" for p in include),
+               os.path.join(CSRC, "quick.cpp"), "-o", made, "-L", lib, "-ltorch", "-ltorch_cpu", "-lc10", "-ltorch_python",
+               "-L", PKG, "-lginex", "-Wl,-rpath,$ORIGIN"]
+    try:
+        subprocess.check_call(command)
+        os.replace(made, QUICK)
+    except (OSError, subprocess.CalledProcessError) as e:
+        warnings.warn(f"the layers' compiled calls are not built, their Python names do without: {e}")
+        for half_or_old in (made, QUICK):
+            if os.path.exists(half_or_old):
+                os.remove(half_or_old)
 
 
 def build(verbose: bool = False) -> str:
