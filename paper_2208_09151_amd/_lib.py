@@ -139,14 +139,27 @@ def load():
     return _lib
 
 
+def quick_is_for() -> str:
+    """The interpreter and the torch that csrc/quick.cpp is compiled against, as its build writes them into it: it uses torch's
+    classes as their headers describe them, and another torch may have others."""
+    import sys
+
+    import torch
+    return f"ginex calls for {sys.implementation.cache_tag}, torch {torch.__version__}, {torch.version.git_version}"
+
+
 def quick():
-    """The compiled calls of csrc/quick.cpp, or None where they are not built, or older than their sources."""
+    """The compiled calls of csrc/quick.cpp, or None where they are not built, older than their sources, or built against another
+    torch."""
     path = os.path.join(_PKG, "_quick.so")
     root = os.path.dirname(_PKG)
     sources = [os.path.join(_PKG, "csrc", "quick.cpp")] + [os.path.join(root, "include", f)
                                                             for f in ("ginex.h", "ginex_train.h", "ginex_layers.h")]
     if not os.path.exists(path) or any(os.path.getmtime(s) > os.path.getmtime(path) for s in sources if os.path.exists(s)):
         return None
+    with open(path, "rb") as f:
+        if quick_is_for().encode() + b"\0" not in f.read():
+            return None
     try:
         from . import _quick
     except ImportError:

@@ -47,13 +47,16 @@ def _build_quick() -> None:
 
         import torch
         from torch.utils import cpp_extension
+
+        from ._lib import quick_is_for
     except ImportError:
         return
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], os.path.join(ROOT, "include")]
     made = f"{QUICK[:-3]}.{os.getpid()}.so"         # (in its place once it is whole)
     command = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
-               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{p}" for p in include),
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DGINEX_QUICK_IS_FOR="{quick_is_for()}"',
+               *(f"-isystem{p}" for p in include),
                os.path.join(CSRC, "quick.cpp"), "-o", made, "-L", lib, "-ltorch", "-ltorch_cpu", "-lc10", "-ltorch_python",
                "-L", PKG, "-lginex", "-Wl,-rpath,$ORIGIN"]
     try:

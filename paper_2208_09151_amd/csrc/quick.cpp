@@ -15,6 +15,9 @@
 
 #include "ginex_layers.h"
 
+// What this is compiled against; the Python side looks for it in the file before it loads it.
+extern "C" __attribute__((used, visibility("default"))) const char ginex_quick_is_for[] = GINEX_QUICK_IS_FOR;
+
 namespace {
 
 // A tensor that carries a tangent of forward mode (there is one level of those).

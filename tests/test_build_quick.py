@@ -40,3 +40,15 @@ def test_no_compiler_or_none_that_gets_through(place, monkeypatch, error, there)
     with pytest.warns(UserWarning, match="not built"):
         b._build_quick()
     assert os.listdir(place) == []
+
+
+@pytest.mark.parametrize("name, value", [("__version__", "2.10.1+rocm7.0"), ("__version__", "2.10"), ("git_version", "0" * 40)])
+def test_one_for_another_torch_is_not_loaded(monkeypatch, name, value):
+    """Whatever the times of the files say: compiled calls use torch's classes as they were described to them."""
+    import torch
+
+    from paper_2208_09151_amd import _lib
+    if _lib.quick() is None:
+        pytest.skip("the compiled calls are not built")
+    monkeypatch.setattr(torch if name == "__version__" else torch.version, name, value)
+    assert _lib.quick() is None
