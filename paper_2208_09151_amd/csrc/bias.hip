@@ -122,7 +122,7 @@ extern "C" int32_t ginex_bias_gradient(const ginex_rows_t* dy, const ginex_routi
     });
     if (rc) return rc;
   }
-  // (a tile too many of a single sum's is not written)
+  // (of a single sum's tiles one may have no rows: its part is zeros, and is not read)
   const int64_t parts = route ? cut.tiles : ceil_div(dy->rows, cut.height);
   GINEX_HIP(join_async(part, offsets, experts, dy->rows, cut.height, parts, (int32_t)dy->width, (int32_t)dy->width, dbias,
                        nullptr, st));

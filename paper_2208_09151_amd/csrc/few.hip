@@ -280,7 +280,9 @@ __global__ __launch_bounds__(WAVES* WAVE) void k_few_experts(RowsOf<const T> x, 
   }
   // The last workgroup of these columns to come here finds what the others have left, whichever die they were on: stores and
   // loads of that go past the dies' caches, and every wave waits for its stores before one thread counts its pairs.  So the
-  // count itself has nothing to write back or to invalidate, which would cost 3 to 8 us.
+  // count itself has nothing to write back or to invalidate, which would cost 3 to 8 us.  This rests on the instructions, not on the
+  // language, whose relaxed accesses order nothing between them: on gfx950 a relaxed access of agent scope is one with sc1 set,
+  // and a store of that kind is counted by vmcnt until it is where all dies see it.  A test reads the listing for both.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0)

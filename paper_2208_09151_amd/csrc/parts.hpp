@@ -6,11 +6,12 @@
 namespace ginex {
 
 // Rows are taken in units of 128 bytes, of which a lane has 32.  16-bit numbers are two operands of the matrix instructions as they
-// are.  f32 is a sum of three bf16, each the rounded rest of those before it: x = h + m + l with |m| <= 2^-8 |x| and |l| <= 2^-9 |m|,
-// exactly as long as l is not below 2^-133, the least bf16.  Of the nine products the six largest count; the others are 2^-24 of
-// the whole at most, no more than a rounding of it to f32, and the smallest are added first.  Six bf16 instructions take 96 cycles
-// where the f32 ones take 256 (820 000 x 256 -> 256: 700 us instead of 954).  What is no number, or none in bf16, leaves a sum that
-// is none, and such a sum is computed again with the f32 instructions.
+// are.  f32 is a sum of three bf16, each the rounded rest of those before it: x = h + m + l with |m| <= 2^-8 |x| and
+// |l| <= 2^-17 |x| (h leaves at most 2^-8 of x's power of two, and m has the 8 upper bits of that),
+// exactly as long as l is not below 2^-133, the least bf16.  Of the nine products the six largest count; the others are
+// 2 * 2^-8 * 2^-17 + 2^-34 of the whole at most, no more than a rounding of it to f32, and the smallest are added first.  Six bf16
+// instructions take 96 cycles where the f32 ones take 256 (820 000 x 256 -> 256: 700 us instead of 954).  What is no number, or none
+// in bf16, leaves a sum that is none, and such a sum is computed again with the f32 instructions.
 template <typename T>
 struct Operand {
   static constexpr int PARTS = 2;

@@ -2,14 +2,16 @@
 //
 // Such a layer is bound by HBM: a row of 256 numbers through 256 columns is 256 products a number.  A workgroup puts the weights
 // of its columns into LDS once, in the order in which the matrix instructions take them (a wave reads 1 KB in a row, no bank
-// twice), and goes through tiles of 128 rows.  A wave has 16 of them and all columns, so a row is read by one wave alone, from
-// HBM into the registers of the matrix instructions, a segment ahead of the products, and no wave waits for another.  A layer
-// per expert: the tiles of all experts are numbered, a workgroup has a range of them, and changes its weights where the expert
-// changes.
+// twice), and goes through tiles of rows, which come from HBM into the registers of the matrix instructions, a segment ahead of
+// the products; no wave waits for another.  In 16 bits a wave has 16 rows and all of the workgroup's columns, so that one wave alone
+// reads a row of up to 256 columns.  Of f32's three parts LDS has room for 64 columns of 256 numbers: four workgroups, which follow
+// each other on one die, read a row for 256 columns, and each cuts it into its parts.  A layer per expert: the tiles of all experts
+// are numbered, a workgroup has a range of them, and changes its weights where the expert changes.
 //
-// 177 000 x 256 -> 256 bf16 with gelu and residual 79 us, 3.4 TB/s of rows read and written: the epilogue's vector work is not
-// hidden behind the loads.  820 000 x 256 -> 256 f32 700 us, 2.4 TB/s and 920 TFLOP/s of bf16 products: the matrix cores, fed by
-// the vector unit that cuts the rows into their parts.
+// 177 000 x 256 -> 256 bf16 with gelu and residual 80 us: 52 for the rows, 10 for the residual and 18 for gelu on the vector unit, which
+// the loads do not hide (relu: 2).  The 52 are a start of some 12 us and rounds of 32 768 rows of 7 each, the last as long as the
+// others (196 608 rows 52.5, one more 58.8; 820 000 194, 4.3 TB/s).  820 000 x 256 -> 256 f32 700 us, 2.4 TB/s and 920 TFLOP/s of bf16
+// products: the matrix cores, and the vector unit that cuts every row four times.
 #include "epilogue.hpp"
 #include "parts.hpp"
 

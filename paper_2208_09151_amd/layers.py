@@ -14,6 +14,7 @@ was recorded outside of the capture hold the same leaves meanwhile (autograd wou
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import torch
@@ -29,6 +30,7 @@ FEW_ROWS, FEW_TOP = 64, 16      # of expert_layer
 # The plain case of a call without the interpreter's part: False until it has been looked for, None where there is none.
 _quick = False
 _NO_ROUTE = (None, None, None)
+_AS_IT_IS = contextlib.nullcontext()
 
 
 def _quick_for(x):
@@ -169,9 +171,8 @@ def linear_backward(grad, weight, route: Route = None, out=None):
     activate_backward); with a route it is the slots' and so is the result, which dispatch_backward adds up by rows."""
     if not isinstance(weight, torch.Tensor) or weight.dim() < 2:
         raise ValueError("weight: expected a tensor [width, out] or [experts, width, out]")
-    if not (torch.is_grad_enabled() and (weight.requires_grad or getattr(grad, "requires_grad", False))):
-        return linear(grad, weight.mT, route=route, slots=route is not None, out=out)
-    with torch.no_grad():
+    recorded = torch.is_grad_enabled() and (weight.requires_grad or getattr(grad, "requires_grad", False))
+    with torch.no_grad() if recorded else _AS_IT_IS:
         return linear(grad, weight.mT, route=route, slots=route is not None, out=out)
 
 
