@@ -54,6 +54,8 @@ def _here(t, what, dtype=None):
         raise ValueError(f"{what}: on {t.device}, which is not the current GPU")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: expected dtype {dtype}, got {t.dtype}")
+    if t.is_neg():
+        raise ValueError(f"{what}: in memory with the other sign (see Tensor.resolve_neg)")
     _no_tangent(t, what)
     return t
 
