@@ -9,8 +9,9 @@
 // neighbouring columns of one row: bias, activation, residual, codes and rounding are done in registers and stored in whole
 // chunks.
 //
-// Bound by the matrix cores where width and columns are many, by HBM where they are few: 50 000 x 1024 -> 1024 bf16 180 us, 583
-// TFLOP/s; 152 000 slots of 8 experts, 256 -> 128 bf16 32 us, 3.6 TB/s of rows read and written.  The loads of a step are issued
+// Bound by LDS and two barriers a step, which feed the matrix cores, where width and columns are many, by HBM where they are few:
+// 50 000 x 1024 -> 1024 bf16 180 us, 583 TFLOP/s (198 where torch's product takes 144 on the same inputs; f32, with six products
+// for an operand that is brought, 662 and 875); 152 000 slots of 8 experts, 256 -> 128 bf16 32 us, 3.6 TB/s of rows read and written.  The loads of a step are issued
 // before the products of the one in front of it, with nothing between that depends on them (no branch, no arithmetic on what they
 // bring), because a wave can only wait for its oldest loads: with the mending of ends right behind each load the first of these
 // took 338 us.

@@ -281,7 +281,9 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward_long(RowsOf<const T> 
   }
 }
 
-// What is left of long rows when their means, as they were rounded, are taken away: rests[r] is the mean of that.
+// What is left of long rows when their means, as they were rounded, are taken away: rests[r] is the mean of that.  Without it dweight
+// of rows at 10 000 +- 0.1 was off by 0.3 % of itself.  12 us of the 103 that the gradients of 3000 x 6000 f32 take, 74 of 628 for
+// 13 120 x 16 000 bf16.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void k_norm_rests(RowsOf<const T> x, const float* __restrict__ stats, Width width,
                                                         float per_width, float* __restrict__ rests) {
