@@ -8,7 +8,7 @@ Every call enqueues on the current stream and returns at once.
 
 linear, layer_norm and lookup keep autograd's graph where it is recorded.  linear keeps its rows and what its activation is
 applied to in 8 bits; layer_norm keeps its rows as they are.  expert_layer has no gradient and refuses to be recorded.
-Tensors that carry a tangent of forward mode are refused.
+What the calls for gradients give is a constant to autograd.  Tensors that carry a tangent of forward mode are refused everywhere.
 A graph may capture a step with its backward pass: ask for the gradients by torch.autograd.grad, and let no graph of autograd that
 was recorded outside of the capture hold the same leaves meanwhile (autograd would wait for the stream that it was recorded on).
 """
